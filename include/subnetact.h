@@ -57,7 +57,8 @@ typedef enum {
 
 typedef enum { SNA_FAMILY_TINY = 0, SNA_FAMILY_RESNET = 1, SNA_FAMILY_MBV3 = 2,
                SNA_FAMILY_TRANSFORMER = 3 } sna_family;
-typedef enum { SNA_DTYPE_FP32 = 0, SNA_DTYPE_BF16 = 1 } sna_dtype;
+typedef enum { SNA_DTYPE_FP32 = 0, SNA_DTYPE_BF16 = 1,
+               SNA_DTYPE_FP16 = 2 /* autoregressive serving only */ } sna_dtype;
 typedef enum { SNA_ACT_NONE = 0, SNA_ACT_RELU = 1, SNA_ACT_HSWISH = 2, SNA_ACT_GELU = 3 } sna_act;
 
 /*
@@ -337,6 +338,61 @@ const char* sna_profile_class_name(int32_t kclass);
  * cap - 1 bytes plus a NUL into buf (host memory, may be NULL) and returns the
  * full length, or -1 on error. */
 int64_t sna_profile_read_launches(sna_supernet* net, char* buf, int64_t cap);
+
+/* ---- autoregressive serving over a paged key / value cache -------------------------------------
+ *
+ * A step brings n_tokens rows of new tokens for n_seqs sequences: rows starts[b] .. starts[b + 1] - 1
+ * belong to sequence b, of which lens[b] tokens are cached once these are in, so that its new token i
+ * has position lens[b] - (starts[b + 1] - starts[b]) + i.  Position p of sequence b lies in slot
+ * p % page_size of page page_table[b][p / page_size].  starts, lens and page_table are device memory
+ * and never read by the host.  The kernels stay within the rows, table columns and pages named here
+ * whatever these arrays hold: a token without a page of the pool is not stored, and what attention
+ * returns for such a sequence is unspecified.
+ *
+ * Calls are stateless, enqueue on `hip_stream` and may be captured into a graph (the sizes and bounds
+ * are the graph's, the arrays' contents are read by every replay).  Device pointers of rows and pages
+ * are aligned to 16 bytes and their strides, in elements, are multiples of 8. */
+typedef struct {
+  void* k_pages_dev;              /* [n_pages][kv_heads][page_size][head_dim], dense within a page */
+  void* v_pages_dev;              /* [n_pages][kv_heads][head_dim][page_size]: transposed, as the matrix operand reads it */
+  int64_t k_page_stride, v_page_stride;        /* elements between pages (the layers of a pool may take turns) */
+  int32_t n_pages, kv_heads;
+  int32_t page_size;              /* a power of two, 16 .. 1024 */
+  int32_t head_dim;               /* 64 or 128 */
+  int32_t dtype;                  /* SNA_DTYPE_BF16 or SNA_DTYPE_FP16, of the pages and of every row */
+} sna_paged_cache;
+
+typedef struct {
+  const int32_t* starts_dev;      /* [n_seqs + 1], rising from 0 to n_tokens; a sequence may bring none */
+  const int32_t* lens_dev;        /* [n_seqs] */
+  const int32_t* page_table_dev;  /* [n_seqs][table_width]; entries behind a sequence's last page are not used */
+  int64_t table_stride;           /* elements between the table's rows */
+  int32_t n_seqs, n_tokens, table_width;
+  int32_t max_new, max_len;       /* bounds on the new tokens and the length of any sequence: they choose the launch */
+} sna_paged_batch;
+
+typedef struct { void* dev; int64_t token_stride, head_stride; } sna_rows;   /* [n_tokens][heads][head_dim] */
+
+/* Appends the step's keys and values to the cache and returns its queries, both as attention takes them:
+ * q and k are normalised per head where q_norm_dev / k_norm_dev (fp32 [head_dim]; both or neither) are
+ * given, x * rsqrt(mean(x^2) + eps) * norm, and their leading rot_dim elements rotated by
+ * position * inv_freq_dev[i] (fp32 [rot_dim / 2], angles formed in 64 bits), pair i being elements i and
+ * i + rot_dim / 2, or 2 i and 2 i + 1 where `interleaved`.  One rounding, at the end.  rot_dim is a
+ * multiple of 16, at most head_dim; 0: no rotation.  q_out may be q.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE (a size out of range), SNA_E_CFG_ALIGN (alignment, strides), SNA_E_HIP. */
+sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, const sna_rows* q,
+                         const sna_rows* k, const sna_rows* v, const sna_rows* q_out, const float* inv_freq_dev,
+                         int32_t rot_dim, int32_t interleaved, const float* q_norm_dev, const float* k_norm_dev, float eps,
+                         void* hip_stream);
+
+/* out = softmax(scale * q k^T) v over each sequence's cached keys, causal: a token of position p sees the
+ * keys of positions p - window + 1 .. p (window 0: all up to p).  Query head i reads key / value head
+ * i / (q_heads / kv_heads).  Statistics and sums are fp32, the probabilities of a product are rounded to
+ * the element type, the result once more.  A token that sees no key (its position is negative) gives zeros.
+ * Slots that no visible key of the sequence lies in may hold anything.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_HIP. */
+sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
+                               const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* hip_stream);
 
 const char* sna_last_error(void);
 

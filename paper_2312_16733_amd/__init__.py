@@ -11,3 +11,16 @@ from .binding import (ArchDesc, SubnetCfgC, Supernet, lib, library_path, arch_de
 __all__ = ["ArchDesc", "SubnetCfgC", "Supernet", "lib", "library_path", "arch_desc_from_spec",
            "tensor_infos", "norm_infos", "pack_weights", "pack_stats", "cfg_to_c",
            "supernet_load", "subnet_forward", "SnaError"]
+
+# Autoregressive serving: needs torch, which the rest of the package's import does not
+_SERVING = ("PagedCache", "PagedBatch", "kv_append", "paged_attention")
+__all__ += _SERVING
+
+
+def __getattr__(name):
+    if name in _SERVING:
+        from . import serving
+        for n in _SERVING:
+            globals()[n] = getattr(serving, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -6,7 +6,7 @@ import numpy as np
 
 MAX_STAGES, MAX_DEPTH, NAME_LEN, N_KCLASS = 8, 16, 48, 12
 FAMILY = {"tiny": 0, "resnet": 1, "mbv3": 2, "transformer": 3}
-DTYPE = {"fp32": 0, "bf16": 1}
+DTYPE = {"fp32": 0, "bf16": 1, "fp16": 2}
 ACT = {"none": 0, "relu": 1, "hswish": 2, "gelu": 3}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -49,6 +49,22 @@ class TensorInfo(C.Structure):
 
 class NormInfo(C.Structure):
     _fields_ = [("name", C.c_char * NAME_LEN), ("channels", C.c_int32), ("offset", C.c_int32)]
+
+
+class PagedCacheC(C.Structure):
+    _fields_ = [("k_pages_dev", C.c_void_p), ("v_pages_dev", C.c_void_p), ("k_page_stride", C.c_int64),
+                ("v_page_stride", C.c_int64), ("n_pages", C.c_int32), ("kv_heads", C.c_int32),
+                ("page_size", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class PagedBatchC(C.Structure):
+    _fields_ = [("starts_dev", C.c_void_p), ("lens_dev", C.c_void_p), ("page_table_dev", C.c_void_p),
+                ("table_stride", C.c_int64), ("n_seqs", C.c_int32), ("n_tokens", C.c_int32),
+                ("table_width", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32)]
+
+
+class RowsC(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 def library_path() -> str:
@@ -100,6 +116,10 @@ def lib():
     L.sna_profile_read.restype = i32
     L.sna_profile_class_name.argtypes = [i32]; L.sna_profile_class_name.restype = C.c_char_p
     L.sna_profile_read_launches.argtypes = [vp, C.c_char_p, i64]; L.sna_profile_read_launches.restype = i64
+    cp, bp, rp = C.POINTER(PagedCacheC), C.POINTER(PagedBatchC), C.POINTER(RowsC)
+    L.sna_kv_append.argtypes = [cp, bp, i32, rp, rp, rp, rp, vp, i32, i32, vp, vp, C.c_float, vp]
+    L.sna_kv_append.restype = i32
+    L.sna_paged_attention.argtypes = [cp, bp, i32, rp, rp, C.c_float, i32, vp]; L.sna_paged_attention.restype = i32
     _lib = L
     return L
 

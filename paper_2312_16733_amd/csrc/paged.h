@@ -1,0 +1,119 @@
+// What the autoregressive serving kernels share: the step's sequences, the paged key / value cache, 16-bit element types.
+#pragma once
+#include "common.h"
+
+namespace sna {
+
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+
+// Element types: eight of them are one 16-byte access and one operand of the matrix instructions.
+struct Bf16 {
+  typedef __attribute__((ext_vector_type(8))) __bf16 v8;
+  static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {     // 16 x 16 += 16 x 32 by 32 x 16
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+#endif
+    return c;
+  }
+};
+struct Fp16 {
+  typedef __attribute__((ext_vector_type(8))) _Float16 v8;
+  static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+#endif
+    return c;
+  }
+};
+template <class T>
+__device__ __forceinline__ f32x8 to_f32(u32x4 u) { return __builtin_convertvector(__builtin_bit_cast(typename T::v8, u), f32x8); }
+template <class T>
+__device__ __forceinline__ u32x4 to_16(f32x8 x) { return __builtin_bit_cast(u32x4, __builtin_convertvector(x, typename T::v8)); }   // to the nearest, ties to even
+
+// The rows of a step.  Sequence b brings rows starts[b] .. starts[b + 1] - 1; with them lens[b] of its tokens are cached.
+// The arrays are the device's: what they hold is not known to the host, so every use below is clamped to what the host
+// does know (T rows, `width` table columns, n_pages pages), and wrong contents give wrong results, never a wild access.
+struct PagedSeqs {
+  const int* starts; const int* lens; const int* table;
+  int B, T, width, tstride;
+};
+struct PagedKV {
+  char* k; char* v;                  // [page][head][slot][dim], [page][head][dim][slot]
+  long kstride, vstride;             // bytes between pages
+  int n_pages, lps, heads;           // lps: log2(slots of a page)
+};
+struct Seq { int row0, n, len; };    // first row, new tokens, cached tokens with them
+
+__device__ __forceinline__ int clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
+__device__ __forceinline__ Seq sequence(const PagedSeqs& s, int b) {
+  const int r0 = clamped(s.starts[b], 0, s.T), r1 = clamped(s.starts[b + 1], 0, s.T);
+  return Seq{r0, max(r1 - r0, 0), clamped(s.lens[b], 0, 1 << 30)};
+}
+// The largest i of [0, n) with f(i) <= x, for a rising f with f(0) <= x: 64 places at a time, one of them a lane, so that
+// up to 64 sequences cost one round trip to memory and up to 4096 two.
+template <class F>
+__device__ __forceinline__ int last_at_most(int n, int x, F f) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
+    const bool in = lane == 0 || (i < hi && f(i < hi ? i : lo) <= x);
+    lo += (__popcll(__ballot(in)) - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Over the four lanes that share lane % 16
+__device__ __forceinline__ float max_of_4(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#endif
+  return v;
+}
+__device__ __forceinline__ float sum_of_4(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+#endif
+  return v;
+}
+
+struct AppendArgs {
+  PagedSeqs s;
+  PagedKV kv;
+  const char *q, *k, *v;
+  char* qo;
+  const float *inv_freq, *q_norm, *k_norm;
+  long q_t, q_h, k_t, k_h, v_t, v_h, o_t, o_h;   // bytes between tokens / heads
+  int Hq, half;                                  // half: rotated pairs of a head
+  float eps;
+  int interleaved, one;                          // one: every sequence brings exactly one token
+  int q_parts, k_parts;                          // filled by the launcher
+};
+hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, hipStream_t s);
+
+struct PagedAttnArgs {
+  PagedSeqs s;
+  PagedKV kv;
+  const char* q;
+  char* o;
+  long q_t, q_h, o_t, o_h;                       // bytes between tokens / heads
+  int G;                                         // query heads of a key / value head
+  int window;                                    // keys that a token sees, its own among them; INT_MAX: all
+  float scale2;                                  // scale * log2(e)
+  int max_new;
+  int tpt;                                       // filled by the launcher: tokens of a tile of rows
+  FastDiv by_tpt;
+};
+hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
+
+}  // namespace sna

@@ -1,0 +1,231 @@
+"""Autoregressive serving operators on the GPU against their definitions in 64 bits."""
+import pytest
+import torch
+
+import paper_2312_16733_amd as sna
+import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def parts(s):
+    cache = sna.PagedCache(s["k_pages"], s["v_pages"])
+    batch = sna.PagedBatch(s["starts"], s["lens"], s["table"], s["max_new"], s["max_len"])
+    return cache, batch
+
+
+def within(got, want, err, what):
+    assert torch.isfinite(got.float()).all(), f"{what}: not finite"
+    off = (got.double() - want).abs()
+    worst = (off / err).nan_to_num(nan=0.0).max().item()               # an exact zero has no error allowed, and is 0 / 0
+    print(f"{what}: {worst:.3f} of the bound", flush=True)
+    assert (off <= err).all(), f"{what}: {worst} of the bound"
+
+
+# (length, new tokens) of every sequence
+STEPS = {
+    "one token": [(1, 1)],
+    "decode": [(300, 1), (16, 1), (17, 1), (1, 1), (64, 1), (65, 1), (129, 1)],
+    "some idle": [(40, 0), (33, 1), (0, 0), (64, 0), (200, 1)],
+    "drafts": [(77, 5), (5, 5), (130, 4), (64, 1), (100, 0), (16, 2)],
+    "chunks": [(83, 83), (150, 37), (64, 64), (301, 17), (9, 1)],
+    "long chunk": [(700, 333), (50, 1), (611, 20)],
+}
+HEADS = [(12, 12, 64), (8, 1, 64), (9, 3, 64), (32, 8, 128), (7, 1, 128), (16, 16, 128)]
+
+
+# ---------------------------------------------------------------- append
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("step", STEPS)
+@pytest.mark.parametrize("heads,page,rot,interleaved,norm", [
+    ((12, 12, 64), 16, 64, False, False), ((9, 3, 64), 32, 32, True, True), ((32, 8, 128), 16, 128, True, False),
+    ((7, 1, 128), 64, 48, False, True), ((40, 8, 128), 16, 64, False, True), ((8, 1, 64), 128, 0, False, True)])
+def test_append(dtype, step, heads, page, rot, interleaved, norm):
+    s = ref.make(STEPS[step], *heads, page, ref.DT[dtype], seed=3, layers=2)
+    g = torch.Generator().manual_seed(5)
+    D = heads[2]
+    inv = (10000.0 ** (-torch.arange(0, rot, 2).double() / rot)).float().cuda() if rot else None
+    w = [torch.rand(D, generator=g).cuda() + 0.5 if norm else None for _ in range(2)]
+    (wq, eq), (wk, ek), wv = ref.append(s, inv, interleaved, *w, eps=1e-5)
+    old_k, old_v = s["k_pages"].clone(), s["v_pages"].clone()
+    cache, batch = parts(s)
+    batch.validate(cache, s["q"].shape[0])
+    q = sna.kv_append(cache, batch, s["q"], s["k"], s["v"], inv_freq=inv, interleaved=interleaved, q_norm=w[0], k_norm=w[1], eps=1e-5)
+    within(q, wq, eq, "q")
+    row, touched_k, touched_v = 0, torch.zeros_like(old_k, dtype=torch.bool), torch.zeros_like(old_v, dtype=torch.bool)
+    for b, (l, n) in enumerate(s["seqs"]):
+        pos = torch.arange(l - n, l, device="cuda")
+        page_of, slot = s["table"][b, pos // page].long(), pos % page
+        if n:
+            within(s["k_pages"][page_of, :, slot], wk[row: row + n], ek[row: row + n], f"k of sequence {b}")
+            assert torch.equal(s["v_pages"][page_of, :, :, slot], wv[row: row + n])
+            touched_k[page_of, :, slot] = True
+            touched_v[page_of, :, :, slot] = True
+        row += n
+    # nothing else in the pool has changed, bit for bit
+    for new, old, touched in ((s["k_pages"], old_k, touched_k), (s["v_pages"], old_v, touched_v)):
+        assert torch.equal(new.view(torch.int16)[~touched], old.view(torch.int16)[~touched])
+
+
+def test_append_far_positions_and_in_place():
+    """Angles of positions past 10^5, where a 32-bit product would be off by 1e-2 radians; q written over itself."""
+    s = ref.make([(131071, 1), (131072, 3), (100003, 2)], 16, 2, 128, 64, torch.float16, seed=4, junk=False)
+    inv = (10000.0 ** (-torch.arange(0, 128, 2).double() / 128)).float().cuda()
+    (wq, eq), (wk, ek), _ = ref.append(s, inv)
+    cache, batch = parts(s)
+    q = sna.kv_append(cache, batch, s["q"], s["k"], s["v"], inv_freq=inv, out=s["q"])
+    assert q is s["q"]
+    within(q, wq, eq, "q")
+    within(s["k_pages"][s["table"][1, 131071 // 64].long(), :, 131071 % 64], wk[3], ek[3], "k")
+
+
+def test_append_without_a_page():
+    """Tokens whose page is none of the pool's, or behind the table, leave the pool as it is; q is returned all the same."""
+    s = ref.make([(40, 20), (33, 1), (50, 3)], 4, 2, 64, 16, torch.bfloat16, seed=6)
+    s["table"][0, 1:3] = torch.tensor([-1, 2 ** 31 - 1], dtype=torch.int32)
+    s["table"][1, 2] = s["n_pages"]
+    s["lens"][2] = 10 ** 9
+    old = s["k_pages"].clone(), s["v_pages"].clone()
+    cache, batch = parts(s)
+    q = sna.kv_append(cache, batch, s["q"], s["k"], s["v"])
+    torch.cuda.synchronize()
+    assert torch.equal(q, s["q"])
+    assert torch.equal(s["k_pages"].view(torch.int16), old[0].view(torch.int16)) and torch.equal(s["v_pages"].view(torch.int16), old[1].view(torch.int16))
+
+
+# ---------------------------------------------------------------- attention
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("step", STEPS)
+@pytest.mark.parametrize("heads,page,window", [(HEADS[0], 16, 0), (HEADS[1], 32, 20), (HEADS[2], 16, 0), (HEADS[3], 16, 100), (HEADS[4], 64, 0),
+                                               (HEADS[3], 128, 0), (HEADS[5], 16, 1), ((64, 1, 128), 32, 0)])
+def test_attention(dtype, step, heads, page, window):
+    s = ref.make(STEPS[step], *heads, page, ref.DT[dtype], seed=7)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, window)
+    within(sna.paged_attention(cache, batch, s["q"], window=window), want, err, "out")
+
+
+@pytest.mark.parametrize("heads,page,seqs,window", [
+    ((32, 8, 128), 16, [(5000, 1), (3, 1), (9001, 1)], 0), ((32, 8, 128), 64, [(20011, 1)], 0), ((12, 12, 64), 16, [(4097, 1), (1500, 1)], 0),
+    ((8, 1, 64), 32, [(30000, 9)], 0), ((32, 8, 128), 16, [(9000, 5), (100, 3), (7777, 2)], 3001), ((8, 2, 128), 64, [(6000, 1200), (3000, 1), (50, 50)], 0),
+    ((16, 4, 64), 16, [(2500, 600), (4100, 40), (900, 1), (1, 1)], 1000), ((7, 1, 128), 32, [(3001, 700)], 0)])
+def test_attention_over_long_caches(heads, page, seqs, window):
+    s = ref.make(seqs, *heads, page, torch.bfloat16, seed=8)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, window)
+    within(sna.paged_attention(cache, batch, s["q"], window=window), want, err, "out")
+
+
+def test_attention_scale_strides_and_layers():
+    """A scale of its own, rows of q inside a wider projection, an output with heads outside tokens, a pool whose layers take turns."""
+    s = ref.make([(90, 4), (33, 33), (200, 1)], 8, 2, 128, 16, torch.bfloat16, seed=9, layers=3)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, scale=0.25)
+    out = torch.full((8, s["q"].shape[0], 128), 7.0, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    assert sna.paged_attention(cache, batch, s["q"], scale=0.25, out=out) is out
+    within(out, want, err, "out")
+
+
+def test_attention_of_large_scores():
+    """Scores of several hundred: the running maximum has to keep every exponential in range, whichever tile it comes from."""
+    s = ref.make([(700, 3), (1300, 1)], 8, 2, 64, 16, torch.float16, seed=10)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, scale=20.0)
+    within(sna.paged_attention(cache, batch, s["q"], scale=20.0), want, err, "out")
+
+
+def test_attention_without_keys_and_unused_rows():
+    """A sequence shorter than its new tokens: those of negative positions see nothing and give zeros; rows of no sequence stay."""
+    s = ref.make([(40, 40), (30, 2)], 4, 2, 64, 16, torch.bfloat16, seed=11)
+    s["lens"][0] = 25
+    cache, batch = parts(s)
+    out = torch.full_like(s["q"].contiguous(), 3.0)
+    sna.paged_attention(cache, batch, s["q"], out=out)
+    assert (out[:15] == 0).all()
+    t = dict(s, seqs=[(25, 25), (30, 2)], q=s["q"][15:])
+    want, err = ref.attention(t)
+    within(out[15:], want, err, "the others")
+
+
+@pytest.mark.parametrize("heads,seqs", [((8, 2, 128), [(100, 1), (60, 3)]), ((8, 2, 128), [(300, 90), (500, 1)])])
+def test_attention_with_bad_pages(heads, seqs):
+    """Pages that are none, lengths beyond the table: whatever comes back for those sequences, the others are right."""
+    s = ref.make(seqs + [(70, 1)], *heads, 16, torch.bfloat16, seed=12)
+    cache, batch = parts(s)
+    want, err = ref.attention(s)
+    s["table"][0, 1] = -5
+    s["table"][0, 2] = 2 ** 31 - 1
+    s["lens"][1] = 10 ** 9
+    out = sna.paged_attention(cache, batch, s["q"])
+    torch.cuda.synchronize()
+    within(out[-1:], want[-1:], err[-1:], "the last sequence")
+
+
+def test_attention_past_32_bit_offsets():
+    """Pages beyond 4 GiB of the pool."""
+    page, H, D = 64, 8, 128
+    n = (5 << 30) // (H * page * D * 2)
+    kp = torch.empty(n, H, page, D, dtype=torch.bfloat16, device="cuda")
+    vp = torch.empty(n, H, D, page, dtype=torch.bfloat16, device="cuda")
+    seqs = [(200, 1), (130, 7)]
+    s = ref.make(seqs, 32, H, D, page, torch.bfloat16, seed=13)
+    ids = [[n - 1, 1, n - 3, n - 2], [n - 5, 2, n - 4]]
+    for b, row in enumerate(ids):
+        old = s["table"][b, : len(row)].long()
+        kp[row], vp[row] = s["k_pages"][old], s["v_pages"][old]
+        s["table"][b, : len(row)] = torch.tensor(row, dtype=torch.int32, device="cuda")
+    s["k_pages"], s["v_pages"] = kp, vp
+    cache, batch = parts(s)
+    (_, _), (wk, ek), wv = ref.append(s)
+    sna.kv_append(cache, batch, s["q"], s["k"], s["v"])
+    within(kp[n - 2, :, 199 - 192], wk[0], ek[0], "k")
+    assert torch.equal(vp[n - 2, :, :, 199 - 192], wv[0])
+    want, err = ref.attention(s)
+    within(sna.paged_attention(cache, batch, s["q"]), want, err, "out")
+
+
+def test_step_on_another_stream_and_in_a_graph():
+    """Append and attention captured once and replayed as the sequences grow, between eager calls, against eager results."""
+    s = ref.make([(100, 1), (37, 1), (64, 1)], 8, 2, 64, 16, torch.bfloat16, seed=14, fill=0.0, junk=False)
+    for b in range(3):                                                 # room to grow
+        s["table"][b, -2:] = torch.arange(2, device="cuda", dtype=torch.int32) + 2 * b
+    s["k_pages"] = torch.cat((s["k_pages"], s["k_pages"])).contiguous()
+    s["v_pages"] = torch.cat((s["v_pages"], s["v_pages"])).contiguous()
+    s["table"][:, -2:] += s["n_pages"]
+    for b, (l, _) in enumerate(s["seqs"]):
+        first = -(-l // 16)
+        s["table"][b, first: first + 2] = s["table"][b, -2:].clone()
+    s["max_len"] = 120
+    cache, batch = parts(s)
+    inv = (10000.0 ** (-torch.arange(0, 64, 2).double() / 64)).float().cuda()
+
+    def step():
+        q = sna.kv_append(cache, batch, s["q"], s["k"], s["v"], inv_freq=inv)
+        return q, sna.paged_attention(cache, batch, q)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gq, gout = step()
+    for i in range(4):
+        s["lens"] += 1
+        k0, v0 = s["k_pages"].clone(), s["v_pages"].clone()
+        q, out = step()
+        q, out, k1, v1 = q.clone(), out.clone(), s["k_pages"].clone(), s["v_pages"].clone()
+        s["k_pages"].copy_(k0)
+        s["v_pages"].copy_(v0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(gq, q) and torch.equal(gout, out) and torch.equal(s["k_pages"], k1) and torch.equal(s["v_pages"], v1)
+        t = dict(s, seqs=[(int(l), 1) for l in s["lens"].tolist()], q=q)
+        want, err = ref.attention(t)
+        within(out, want, err, f"step {i}")
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        again = sna.paged_attention(cache, batch, q, stream=other)
+        torch.cuda.current_stream().wait_stream(other)
+        assert torch.equal(again, out)

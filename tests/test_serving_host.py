@@ -1,0 +1,100 @@
+"""What the serving operators refuse, without a GPU: the C entries check every argument before anything is enqueued."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2312_16733_amd as sna
+from paper_2312_16733_amd import serving
+from paper_2312_16733_amd.binding import PagedBatchC, PagedCacheC, RowsC
+
+NULL, RANGE, ALIGN = -1, -3, -4
+AT = 1 << 20                                                           # a made-up device address: never read by the host
+
+
+def cache(**k):
+    d = dict(k_pages_dev=AT, v_pages_dev=AT, k_page_stride=2 * 16 * 64, v_page_stride=2 * 16 * 64, n_pages=9, kv_heads=2, page_size=16, head_dim=64, dtype=1)
+    return PagedCacheC(**{**d, **k})
+
+
+def batch(**k):
+    d = dict(starts_dev=AT, lens_dev=AT, page_table_dev=AT, table_stride=4, n_seqs=3, n_tokens=5, table_width=4, max_new=3, max_len=60)
+    return PagedBatchC(**{**d, **k})
+
+
+def rows(dev=AT, token_stride=512, head_stride=64):
+    return RowsC(dev, token_stride, head_stride)
+
+
+def attention(c=None, b=None, heads=4, q=None, out=None, scale=0.1, window=0):
+    return sna.lib().sna_paged_attention(c or cache(), b or batch(), heads, q or rows(), out or rows(), scale, window, None)
+
+
+def append(c=None, b=None, heads=4, q=None, k=None, v=None, out=None, inv=AT, rot=64, qn=None, kn=None):
+    return sna.lib().sna_kv_append(c or cache(), b or batch(), heads, q or rows(), k or rows(), v or rows(), out or rows(), inv, rot, 0, qn, kn, 1e-6, None)
+
+
+CACHES = [(dict(k_pages_dev=None), NULL), (dict(v_pages_dev=None), NULL), (dict(dtype=0), RANGE), (dict(dtype=3), RANGE), (dict(head_dim=96), RANGE),
+          (dict(page_size=8), RANGE), (dict(page_size=48), RANGE), (dict(page_size=2048), RANGE), (dict(n_pages=0), RANGE), (dict(kv_heads=0), RANGE),
+          (dict(k_page_stride=2 * 16 * 64 - 8), RANGE), (dict(v_page_stride=0), RANGE), (dict(k_pages_dev=AT + 8), ALIGN), (dict(v_page_stride=2 * 16 * 64 + 4), ALIGN)]
+BATCHES = [(dict(starts_dev=None), NULL), (dict(lens_dev=None), NULL), (dict(page_table_dev=None), NULL), (dict(n_seqs=-1), RANGE), (dict(n_tokens=-1), RANGE),
+           (dict(table_width=0), RANGE), (dict(max_new=0), RANGE), (dict(max_new=6), RANGE), (dict(max_new=1), RANGE), (dict(max_len=2), RANGE), (dict(table_stride=-1), RANGE)]
+
+
+@pytest.mark.parametrize("call", [append, attention])
+def test_caches_and_batches_are_refused(call):
+    for bad, status in CACHES:
+        assert call(c=cache(**bad)) == status, bad
+        assert sna.lib().sna_last_error()
+    for bad, status in BATCHES:
+        assert call(b=batch(**bad)) == status, bad
+    for heads in (0, 3, -2, 130):
+        assert call(heads=heads) == RANGE, heads
+
+
+def test_rows_are_refused():
+    for bad, status in ((rows(dev=None), NULL), (rows(dev=AT + 2), ALIGN), (rows(token_stride=511), ALIGN), (rows(head_stride=4), ALIGN)):
+        assert attention(q=bad) == status and attention(out=bad) == status
+        for name in ("q", "k", "v", "out"):
+            assert append(**{name: bad}) == status, name
+    assert attention(window=-1) == RANGE
+    for rot in (-16, 8, 72, 80):
+        assert append(rot=rot) == RANGE
+    assert append(inv=None) == NULL
+    assert append(qn=AT) == NULL and append(kn=AT) == NULL
+
+
+def test_a_step_without_tokens_is_no_launch():
+    for none in (dict(n_seqs=0, n_tokens=0), dict(n_tokens=0)):
+        assert append(b=batch(**none)) == 0 and attention(b=batch(**none)) == 0
+
+
+def test_tensors_are_refused():
+    k, v = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 64, 16, dtype=torch.bfloat16)
+    for bad in ((k[0], v), (k, k), (k, v.half()), (k.float(), v.float()), (k, v)):                   # the last: not on a GPU
+        with pytest.raises(ValueError):
+            sna.PagedCache(*bad)
+    n = torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        sna.PagedBatch(n, n[:2], torch.zeros(2, 4, dtype=torch.int32), 1, 1)                        # not on a GPU
+
+
+class _Cpu:                                                            # what validate() looks at
+    page_size, n_pages = 16, 9
+
+
+def test_validate_finds_what_does_not_fit():
+    def of(starts, lens, table, max_new=4, max_len=64):
+        b = serving.PagedBatch.__new__(serving.PagedBatch)
+        b.starts, b.lens, b.page_table = (torch.tensor(x, dtype=torch.int32) for x in (starts, lens, table))
+        b.max_new, b.max_len = max_new, max_len
+        return b
+
+    good = dict(starts=[0, 1, 1, 5], lens=[17, 0, 33], table=[[0, 8, -1, -1], [-1] * 4, [3, 4, 5, 99]])
+    of(**good).validate(_Cpu, 5)
+    for bad in (dict(starts=[1, 1, 1, 5]), dict(starts=[0, 2, 1, 5]), dict(starts=[0, 1, 1, 4]), dict(lens=[17, 0, 65]), dict(lens=[17, 0, 3]), dict(lens=[17, 16, 33]),
+                dict(table=[[0, 9, -1, -1], [-1] * 4, [3, 4, 5, 99]]), dict(max_new=3), dict(max_len=32), dict(lens=[17, 0, 49])):
+        with pytest.raises(ValueError):
+            of(**{**good, **bad}).validate(_Cpu, 5)
+    with pytest.raises(ValueError):
+        of([0, 1], [65], [[1, 2, 3, 4]], max_len=99).validate(_Cpu, 1)
