@@ -394,6 +394,21 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
 sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
                                const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* hip_stream);
 
+/* Verification of drafted tokens: sequence b drafted tokens[b][0 .. n_draft[b] - 1] (n_draft_dev NULL: all n_steps).
+ * target[b][i] (fp32 [vocab], dense) are the target's probabilities of the token at drafted place i, given those before it,
+ * and target[b][n_draft[b]] of the one after the last; draft[b][i] are those that drafted token i was drawn from, or NULL
+ * where the drafts were chosen without chance (probability 1).  Draft i is accepted while uniforms[b][i] * draft < target,
+ * both at that token.  out[b]: the accepted ones; then one token drawn with uniforms[b][n_steps] (of [0, 1)) by running sums
+ * in token order: at the first draft not accepted from max(target - draft, 0) (without chance: from the target's other
+ * tokens), or from the target where that leaves nothing or all are accepted; then -1.  accepted[b]: how many.  Products,
+ * differences and sums are fp64.  The drawn token is -1 where the row has no positive probability (NaN counts as none).  A
+ * drafted token outside the vocabulary is not accepted.  token_bytes: 4 or 8.  Strides in elements.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_HIP. */
+sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, int64_t target_row_stride, const float* draft_dev,
+                            int64_t draft_seq_stride, int64_t draft_row_stride, const void* tokens_dev, int32_t token_bytes,
+                            const float* uniforms_dev, const int32_t* n_draft_dev, int32_t n_seqs, int32_t n_steps, int32_t vocab,
+                            int32_t* out_dev, int32_t* accepted_dev, void* hip_stream);
+
 const char* sna_last_error(void);
 
 #ifdef __cplusplus

@@ -13,7 +13,7 @@ __all__ = ["ArchDesc", "SubnetCfgC", "Supernet", "lib", "library_path", "arch_de
            "supernet_load", "subnet_forward", "SnaError"]
 
 # Autoregressive serving: needs torch, which the rest of the package's import does not
-_SERVING = ("PagedCache", "PagedBatch", "kv_append", "paged_attention")
+_SERVING = ("PagedCache", "PagedBatch", "kv_append", "paged_attention", "verify_draft")
 __all__ += _SERVING
 
 

@@ -120,6 +120,8 @@ def lib():
     L.sna_kv_append.argtypes = [cp, bp, i32, rp, rp, rp, rp, vp, i32, i32, vp, vp, C.c_float, vp]
     L.sna_kv_append.restype = i32
     L.sna_paged_attention.argtypes = [cp, bp, i32, rp, rp, C.c_float, i32, vp]; L.sna_paged_attention.restype = i32
+    L.sna_verify_draft.argtypes = [vp, i64, i64, vp, i64, i64, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp]
+    L.sna_verify_draft.restype = i32
     _lib = L
     return L
 

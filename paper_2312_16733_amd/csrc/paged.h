@@ -116,4 +116,16 @@ struct PagedAttnArgs {
 };
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 
+struct VerifyArgs {
+  const float *target, *draft;                   // [seq][K + 1][V], [seq][K][V] or nullptr
+  long t_seq, t_row, d_seq, d_row;               // elements between sequences / rows
+  const void* tokens;                            // [seq][K]
+  const float* uniforms;                         // [seq][K + 1]
+  const int* counts;                             // [seq] or nullptr
+  int* out;                                      // [seq][K + 1]
+  int* accepted;                                 // [seq]
+  int K, V;
+};
+hipError_t launch_verify(const VerifyArgs& a, int token_bytes, int n_seqs, hipStream_t s);
+
 }  // namespace sna

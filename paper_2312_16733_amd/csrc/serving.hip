@@ -110,4 +110,24 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "paged_attention: %s", hipGetErrorString(e));
 }
 
+
+sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, int64_t target_row_stride, const float* draft_dev,
+                            int64_t draft_seq_stride, int64_t draft_row_stride, const void* tokens_dev, int32_t token_bytes,
+                            const float* uniforms_dev, const int32_t* n_draft_dev, int32_t n_seqs, int32_t n_steps, int32_t vocab,
+                            int32_t* out_dev, int32_t* accepted_dev, void* hip_stream) {
+  if (n_seqs < 0 || n_seqs > (1 << 24) || n_steps < 0 || n_steps > (1 << 16) || vocab < 1 || vocab > (1 << 28))
+    return fail(SNA_E_CFG_RANGE, "verify_draft: %d sequences, %d drafts, vocabulary of %d", n_seqs, n_steps, vocab);
+  if (token_bytes != 4 && token_bytes != 8) return fail(SNA_E_CFG_RANGE, "verify_draft: tokens of %d bytes (4 and 8 are supported)", token_bytes);
+  if (target_seq_stride < 0 || target_row_stride < 0 || draft_seq_stride < 0 || draft_row_stride < 0) return fail(SNA_E_CFG_RANGE, "verify_draft: negative strides");
+  if (n_seqs == 0) return SNA_OK;
+  if (!target_dev || (n_steps && !tokens_dev) || !uniforms_dev || !out_dev || !accepted_dev) return fail(SNA_E_NULL, "verify_draft: a required pointer is NULL");
+  if (((uintptr_t)target_dev | (uintptr_t)draft_dev | (uintptr_t)uniforms_dev | (uintptr_t)n_draft_dev | (uintptr_t)out_dev | (uintptr_t)accepted_dev) & 3 ||
+      (uintptr_t)tokens_dev & (token_bytes - 1))
+    return fail(SNA_E_CFG_ALIGN, "verify_draft: a pointer is not aligned to its elements");
+  const VerifyArgs a = {target_dev, draft_dev, target_seq_stride, target_row_stride, draft_seq_stride, draft_row_stride, tokens_dev, uniforms_dev,
+                        n_draft_dev, out_dev, accepted_dev, n_steps, vocab};
+  const hipError_t e = launch_verify(a, token_bytes, n_seqs, (hipStream_t)hip_stream);
+  return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "verify_draft: %s", hipGetErrorString(e));
+}
+
 }

@@ -4,6 +4,7 @@
     batch = PagedBatch(starts, lens, page_table, max_new, max_len)
     q = kv_append(cache, batch, q, k, v, inv_freq=inv_freq)   # norms, rotation, k and v into their pages
     out = paged_attention(cache, batch, q)
+    tokens, accepted = verify_draft(target, drafted, uniforms)      # speculative decoding: which drafts stand, and the next token
 
 Rows are the new tokens of all sequences of a step, one after the other.  Nothing here reads device memory or waits for it;
 `PagedBatch.validate` does, for a caller in doubt about what its arrays hold.
@@ -148,3 +149,33 @@ def paged_attention(cache, batch, q, scale=None, window=0, out=None, stream=None
         _check(binding.lib().sna_paged_attention(cache.c, batch.c, q.shape[1], qr, outr, cache.head_dim ** -0.5 if scale is None else scale, window,
                                                  torch.cuda.current_stream(cache.device).cuda_stream))
     return out
+
+
+def verify_draft(target, tokens, uniforms, draft_probs=None, n_draft=None, stream=None):
+    """Which drafted tokens stand, and the token after them.  target fp32 [n][K + 1][V]: the target's probabilities at every
+    drafted place and at the one after the last; tokens [n][K] (int32 or int64); uniforms fp32 [n][K + 1] from [0, 1): one for
+    each draft, the last for the draw; draft_probs fp32 [n][K][V] that the drafts were drawn from, or None where they were
+    chosen without chance; n_draft int32 [n]: how many of the K each sequence has (all).  Returns (out int32 [n][K + 1],
+    accepted int32 [n]): the accepted drafts, the drawn token, -1 behind it."""
+    if stream is not None:
+        with _On(target.device, stream):
+            return verify_draft(target, tokens, uniforms, draft_probs, n_draft)
+    _need(target.dim() == 3 and target.dtype == torch.float32 and target.is_cuda and target.stride(2) == 1, "target: fp32 [sequences][drafts + 1][vocabulary], dense rows on a GPU are needed")
+    n, K, V = target.shape
+    K -= 1
+    device = target.device
+    _need(K >= 0 and tokens.shape == (n, K) and tokens.dtype in (torch.int32, torch.int64) and tokens.device == device and tokens.is_contiguous(),
+          f"tokens: dense int32 or int64 [{n}][{K}] on {device} is needed, got {tuple(tokens.shape)} of {tokens.dtype} on {tokens.device}")
+    _need(uniforms.shape == (n, K + 1) and uniforms.dtype == torch.float32 and uniforms.device == device and uniforms.is_contiguous(), f"uniforms: dense fp32 [{n}][{K + 1}] on {device} is needed")
+    _need(draft_probs is None or draft_probs.shape == (n, K, V) and draft_probs.dtype == torch.float32 and draft_probs.device == device and draft_probs.stride(2) == 1,
+          f"draft_probs: fp32 [{n}][{K}][{V}], dense rows on {device} are needed")
+    _need(n_draft is None or n_draft.shape == (n,) and n_draft.dtype == torch.int32 and n_draft.device == device and n_draft.is_contiguous(), f"n_draft: dense int32 [{n}] on {device} is needed")
+    out = torch.empty((n, K + 1), dtype=torch.int32, device=device)
+    accepted = torch.empty(n, dtype=torch.int32, device=device)
+    with torch.cuda.device(device):
+        _check(binding.lib().sna_verify_draft(
+            target.data_ptr(), target.stride(0), target.stride(1), None if draft_probs is None else draft_probs.data_ptr(),
+            0 if draft_probs is None else draft_probs.stride(0), 0 if draft_probs is None else draft_probs.stride(1), tokens.data_ptr(), tokens.element_size(),
+            uniforms.data_ptr(), None if n_draft is None else n_draft.data_ptr(), n, K, V, out.data_ptr(), accepted.data_ptr(),
+            torch.cuda.current_stream(device).cuda_stream))
+    return out, accepted

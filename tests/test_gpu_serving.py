@@ -229,3 +229,104 @@ def test_step_on_another_stream_and_in_a_graph():
         again = sna.paged_attention(cache, batch, q, stream=other)
         torch.cuda.current_stream().wait_stream(other)
         assert torch.equal(again, out)
+
+
+# ---------------------------------------------------------------- verification
+def verified(target, tokens, u, draft=None, counts=None):
+    """The definition, one sequence and token at a time in Python's 64-bit numbers; also whether no comparison was a close call."""
+    n, K1, V = target.shape
+    out, accepted, clear = [], [], True
+    for b in range(n):
+        c = K1 - 1 if counts is None else min(max(int(counts[b]), 0), K1 - 1)
+        a = 0
+        while a < c:
+            x = int(tokens[b, a])
+            if not 0 <= x < V or not float(u[b, a]) * (1.0 if draft is None else float(draft[b, a, x])) < float(target[b, a, x]):
+                break
+            a += 1
+        p = target[b, a].double()
+        w = p.clone()
+        if a < c:
+            if draft is not None:
+                w = p - draft[b, a].double()
+            elif 0 <= int(tokens[b, a]) < V:
+                w[int(tokens[b, a])] = 0
+        w = torch.where(w > 0, w, 0.0)
+        if not w.sum() > 0:
+            w = torch.where(p > 0, p, 0.0)
+        up = w.cumsum(0)
+        if up[-1] > 0:
+            at = float(u[b, K1 - 1]) * float(up[-1])
+            x = int((up <= at).sum())
+            clear = clear and (float((up - at).abs().min()) > 1e-12 * float(up[-1]) or float(u[b, K1 - 1]) == 0)
+        else:
+            x = -1
+        out.append([int(t) for t in tokens[b, :a]] + [x] + [-1] * (K1 - 1 - a))
+        accepted.append(a)
+    return out, accepted, clear
+
+
+def probabilities(n, K, V, seed, draft):
+    g = torch.Generator().manual_seed(seed)
+    logits = torch.randn(n, K + 1, V, generator=g) * 2.5
+    if draft:
+        q = torch.softmax(logits[:, :K] + torch.randn(n, K, V, generator=g), -1)
+        tokens = torch.multinomial(q.reshape(-1, V), 1, generator=g).view(n, K) if K else torch.zeros(n, 0, dtype=torch.long)
+    else:
+        q = None
+        tokens = logits[:, :K].argmax(-1)
+        logits[:, :K].scatter_add_(2, tokens[..., None], torch.full((n, K, 1), 3.0))
+    return torch.softmax(logits, -1), tokens, torch.rand(n, K + 1, generator=g), q
+
+
+@pytest.mark.parametrize("n,K,V", [(1, 1, 1), (3, 2, 2), (5, 4, 7), (40, 8, 63), (9, 5, 64), (7, 3, 65), (33, 4, 1000), (6, 0, 1001), (4, 70, 130), (12, 5, 4097), (5, 3, 50257), (3, 7, 131072)])
+@pytest.mark.parametrize("draft", [True, False])
+def test_verification(n, K, V, draft):
+    p, tokens, u, q = probabilities(n, K, V, 20 + V % 97, draft)
+    counts = torch.randint(-1, K + 2, (n,), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    for c, t in ((None, tokens.int()), (counts, tokens)):
+        want, accepted, clear = verified(p, t, u, q, c)
+        assert clear
+        got, acc = sna.verify_draft(p.cuda(), t.cuda(), u.cuda(), draft_probs=None if q is None else q.cuda(), n_draft=None if c is None else c.cuda())
+        assert acc.tolist() == accepted
+        assert got.tolist() == want
+
+
+def test_verification_at_its_borders():
+    """Zeros before the draw, a difference that is nothing, uniforms of 0 and next to 1, drafts outside the vocabulary, empty and NaN rows, strided rows."""
+    V = 300
+    p = torch.zeros(8, 3, V)
+    p[:, :, 100], p[:, :, 200] = 0.25, 0.75
+    q = p[:, :2].clone()
+    q[:, :, 100], q[:, :, 200] = 0.25, 0.75
+    tokens = torch.full((8, 2), 200, dtype=torch.int32)
+    u = torch.full((8, 3), 0.5)
+    u[0, 2] = 0.0                                                      # all taken, the first token with a weight
+    u[1, 2] = 1 - 2.0 ** -24                                           # the last
+    u[2, 0] = 1.0                                                      # 1 * 0.75 < 0.75 is false; nothing left of p - q: drawn from p
+    tokens[3, 1] = V                                                   # no such token
+    tokens[4, 0] = -1
+    p[5] = 0.0                                                         # nothing to accept or draw
+    p[6, 0, 200] = float("nan")                                        # not accepted; the difference at 100 is 0, so p's 100 is drawn
+    p[7, 0, 100], p[7, 0, 200], q[7, 0, 200] = 0.5, 0.25, 0.75         # refused at 0.5 * 0.75 >= 0.25: drawn from 0.25 at 100
+    want = [[200, 200, 100], [200, 200, 200], [200, -1, -1], [200, 200, -1], [200, -1, -1], [-1, -1, -1], [100, -1, -1], [100, -1, -1]]
+    wide = torch.full((8, 4, V + 5), float("nan"))
+    wide[:, :3, 3: V + 3] = p
+    wide_q = torch.full((8, 5, V + 2), float("nan"))
+    wide_q[:, 2:4, :V] = q
+    assert verified(p, tokens, u, q)[:2] == (want, [2, 2, 0, 1, 0, 0, 0, 0])
+    for a, d in ((p.cuda(), q.cuda()), (wide.cuda()[:, :3, 3: V + 3], wide_q.cuda()[:, 2:4, :V])):
+        got, acc = sna.verify_draft(a, tokens.cuda(), u.cuda(), draft_probs=d)
+        assert got.tolist() == want and acc.tolist() == [2, 2, 0, 1, 0, 0, 0, 0]
+
+
+def test_verification_follows_the_target():
+    """Over many uniforms the tokens that come out are the target's distribution, whatever the draft's: 5 deviations of 20000 draws."""
+    n, V = 20000, 11
+    g = torch.Generator().manual_seed(30)
+    p, q = (torch.softmax(torch.randn(V, generator=g) * 1.5, 0) for _ in range(2))
+    tokens = torch.multinomial(q, n, replacement=True, generator=g).view(n, 1)
+    u = torch.rand(n, 2, generator=g)
+    got, _ = sna.verify_draft(p.expand(n, 2, V).contiguous().cuda(), tokens.cuda(), u.cuda(), draft_probs=q.expand(n, 1, V).contiguous().cuda())
+    share = torch.bincount(got[:, 0].cpu(), minlength=V) / n
+    assert ((share - p).abs() <= 5 * (p * (1 - p) / n).sqrt()).all()

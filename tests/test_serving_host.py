@@ -98,3 +98,21 @@ def test_validate_finds_what_does_not_fit():
             of(**{**good, **bad}).validate(_Cpu, 5)
     with pytest.raises(ValueError):
         of([0, 1], [65], [[1, 2, 3, 4]], max_len=99).validate(_Cpu, 1)
+
+
+def verify(target=AT, draft=None, tokens=AT, token_bytes=4, uniforms=AT, counts=None, n=2, k=3, v=100, out=AT, accepted=AT, stride=400):
+    return sna.lib().sna_verify_draft(target, stride, 100, draft, stride, 100, tokens, token_bytes, uniforms, counts, n, k, v, out, accepted, None)
+
+
+def test_verification_is_refused():
+    for bad in ("target", "tokens", "uniforms", "out", "accepted"):
+        assert verify(**{bad: None}) == NULL, bad
+    for bad in ("target", "draft", "tokens", "uniforms", "counts", "out", "accepted"):
+        assert verify(**{bad: AT + 2}) == ALIGN, bad
+    assert verify(tokens=AT + 4, token_bytes=8) == ALIGN
+    for bad in (dict(n=-1), dict(k=-1), dict(v=0), dict(token_bytes=2), dict(stride=-1)):
+        assert verify(**bad) == RANGE, bad
+    assert verify(n=0) == 0
+    t = torch.ones(2, 3, 10)
+    with pytest.raises(ValueError):
+        sna.verify_draft(t, torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, 3))                # not on a GPU
