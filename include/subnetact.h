@@ -390,9 +390,14 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
  * i / (q_heads / kv_heads).  Statistics and sums are fp32, the probabilities of a product are rounded to
  * the element type, the result once more.  A token that sees no key (its position is negative) gives zeros.
  * Slots that no visible key of the sequence lies in may hold anything.
- * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_HIP. */
+ * The workspace (16-byte aligned) holds parts of sums of sequences whose keys several blocks share; its contents need not
+ * survive or precede a call.  sna_paged_attention_workspace_bytes: how much a call with these sizes wants (0: none), or a
+ * negative sna_status.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_WORKSPACE, SNA_E_HIP. */
+int64_t sna_paged_attention_workspace_bytes(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, int32_t window);
 sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
-                               const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* hip_stream);
+                               const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* workspace_dev,
+                               size_t workspace_bytes, void* hip_stream);
 
 /* Verification of drafted tokens: sequence b drafted tokens[b][0 .. n_draft[b] - 1] (n_draft_dev NULL: all n_steps).
  * target[b][i] (fp32 [vocab], dense) are the target's probabilities of the token at drafted place i, given those before it,

@@ -119,7 +119,8 @@ def lib():
     cp, bp, rp = C.POINTER(PagedCacheC), C.POINTER(PagedBatchC), C.POINTER(RowsC)
     L.sna_kv_append.argtypes = [cp, bp, i32, rp, rp, rp, rp, vp, i32, i32, vp, vp, C.c_float, vp]
     L.sna_kv_append.restype = i32
-    L.sna_paged_attention.argtypes = [cp, bp, i32, rp, rp, C.c_float, i32, vp]; L.sna_paged_attention.restype = i32
+    L.sna_paged_attention.argtypes = [cp, bp, i32, rp, rp, C.c_float, i32, vp, sz, vp]; L.sna_paged_attention.restype = i32
+    L.sna_paged_attention_workspace_bytes.argtypes = [cp, bp, i32, i32]; L.sna_paged_attention_workspace_bytes.restype = i64
     L.sna_verify_draft.argtypes = [vp, i64, i64, vp, i64, i64, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp]
     L.sna_verify_draft.restype = i32
     _lib = L

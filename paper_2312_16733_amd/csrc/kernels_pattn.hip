@@ -6,6 +6,8 @@
 // The scores are formed transposed (keys x rows): a lane then has one row of queries and the softmax statistics are its own
 // but for two exchanges.  The keys of a product's 16 rows are chosen so (row 4 h + c of product a is key 8 h + 4 a + c of 32)
 // that a lane's scores are the eight keys that the second product wants of it, without a trip through LDS.
+#include <algorithm>
+
 #include "paged.h"
 
 namespace sna {
@@ -169,84 +171,257 @@ struct Attend {
   }
 };
 
+// Where a block's rows are: tokens i0 .. i0 + n - 1 of a sequence, all heads of one key / value head
+struct RowTile {
+  int b, row0, n, pos0;            // first row, tokens, position of the first
+  Span keys, clear;                // keys that some row sees, keys that all see
+  int t0, tiles;                   // tiles of keys; at least one, so that rows without keys are written too
+};
+__device__ __forceinline__ RowTile rows_of_sequence(const PagedAttnArgs& a, int b, int i0, int most) {
+  const Seq sq = sequence(a.s, b);
+  RowTile r;
+  r.b = b;
+  r.n = i0 < 0 ? 0 : min(sq.n - i0, most);
+  r.row0 = sq.row0 + i0;
+  r.pos0 = sq.len - sq.n + i0;
+  const int last = min(r.pos0 + r.n - 1, (a.s.width << a.kv.lps) - 1);
+  r.keys = Span{max(a.window <= r.pos0 ? r.pos0 - a.window + 1 : 0, 0), last + 1};
+  r.clear = Span{a.window <= last ? last - a.window + 1 : 0, r.pos0 + 1};
+  r.t0 = r.keys.lo / PA_K;
+  r.tiles = r.n > 0 ? max((max(r.keys.hi, 0) + PA_K - 1) / PA_K - r.t0, 1) : 0;
+  return r;
+}
+
+template <int D, int MB>
+struct JoinLds {
+  __attribute__((aligned(16))) float o[PA_W][16][D + 4];
+  float top[PA_W][MB][16], sum[PA_W][MB][16];
+};
+
+// Keys of tiles t0 .. t1 - 1 for the rows of `r` and head h; the waves' parts are joined and leave as results, or as a part of
+// them (part != nullptr): [rows_cap][D] sums, then [rows_cap][2] maximum and sum.
 template <class T, int D, int MB>
-__global__ __launch_bounds__(64 * PA_W) void paged_rows_kernel(const PagedAttnArgs a) {
-  constexpr int S = D / 32, J = D / 16, LD = D + 4;
-  __shared__ __attribute__((aligned(16))) float so[PA_W][16][LD];
-  __shared__ float sm[PA_W][MB][16], sl[PA_W][MB][16];
+__device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTile& r, int h, int t0, int t1, float* part, int rows_cap, JoinLds<D, MB>& lds) {
+  constexpr int S = D / 32, J = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, hi = lane >> 4;
-  const int h = blockIdx.y, tile = blockIdx.x;
+  const int rows = r.n * a.G;
+  const unsigned inv = 65536u / a.G + 1;                             // row / G for row * G < 65536
+  RowState<D, MB> st;
+  {
+    int lim[MB], low[MB];
+    u32x4 q[MB][S];
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      const int row = min(16 * m + l16, rows - 1), i = (row * inv) >> 16;
+      lim[m] = r.pos0 + i;
+      low[m] = a.window <= lim[m] ? lim[m] - a.window + 1 : 0;
+      const char* x = a.q + (r.row0 + i) * a.q_t + (h * a.G + row - i * a.G) * a.q_h + hi * 16;
+#pragma unroll
+      for (int s = 0; s < S; ++s) q[m][s] = *(const u32x4*)(x + s * 64);
+    }
+    Attend<T, D, MB> at = {a.kv, a.s.table + (long)r.b * a.s.tstride, r.keys.lo >> a.kv.lps, max(r.keys.hi - 1, 0) >> a.kv.lps, h, l16, hi, {}};
+    at.run(t0 + wave, t1, PA_W, r.keys, r.clear, lim, low, q, a.scale2, st);
+  }
+  // o and sum relative to the largest maximum of the waves
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    st.sum[m] = sum_of_4(st.sum[m]);
+    if (hi == 0) { lds.top[wave][m][l16] = st.top[m]; lds.sum[wave][m][l16] = st.sum[m]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    if (16 * m >= rows) break;
+    float top = lds.top[0][m][l16];
+#pragma unroll
+    for (int w = 1; w < PA_W; ++w) top = fmaxf(top, lds.top[w][m][l16]);
+    const float keep = __builtin_amdgcn_exp2f(st.top[m] - (top == -INFINITY ? 0.f : top));
+    if (m) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < J; ++j) *(f32x4*)&lds.o[wave][l16][16 * j + 4 * hi] = st.o[m][j] * keep;
+    __syncthreads();
+    const int r16 = tid / (D / 8), oct = tid % (D / 8), row = 16 * m + r16;
+    if (r16 < 16 && row < rows) {
+      float t = lds.top[0][m][r16], sum = 0.f;
+#pragma unroll
+      for (int w = 1; w < PA_W; ++w) t = fmaxf(t, lds.top[w][m][r16]);
+      f32x8 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < PA_W; ++w) {
+        sum += lds.sum[w][m][r16] * __builtin_amdgcn_exp2f(lds.top[w][m][r16] - (t == -INFINITY ? 0.f : t));
+        const f32x4 y0 = *(const f32x4*)&lds.o[w][r16][oct * 8], y1 = *(const f32x4*)&lds.o[w][r16][oct * 8 + 4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] += y0[e]; x[4 + e] += y1[e]; }
+      }
+      if (part) {
+        *(f32x8*)(part + row * D + oct * 8) = x;
+        if (oct == 0) { part[rows_cap * D + 2 * row] = t; part[rows_cap * D + 2 * row + 1] = sum; }
+      } else {
+        const int i = (row * inv) >> 16;
+        const float f = sum == 0.f ? 0.f : 1.f / sum;                // a row that sees no key is zero
+        *(u32x4*)(a.o + (r.row0 + i) * a.o_t + (h * a.G + row - i * a.G) * a.o_h + oct * 16) = to_16<T>(x * f);
+      }
+    }
+  }
+}
+
+// Two blocks on a CU where the registers allow it: 8 waves with 16 KB and more under way each
+constexpr int blocks_of(int D, int MB) { return MB * D <= 128 ? 2 : 1; }
+
+// A block for each tile of rows and key / value head
+template <class T, int D, int MB>
+__global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_rows_kernel(const PagedAttnArgs a) {
+  __shared__ JoinLds<D, MB> lds;
+  const int tile = blockIdx.x;
   int b = tile, i0 = 0;
   if (a.max_new > a.tpt) {
     const auto tile0 = [&](int i) { return a.by_tpt.div(clamped(a.s.starts[i], 0, a.s.T)) + i; };
     b = last_at_most(a.s.B, tile, tile0);
     i0 = (tile - tile0(b)) * a.tpt;
   }
-  const Seq sq = sequence(a.s, b);
-  const int n = min(sq.n - i0, a.tpt);                               // tokens of this tile
-  if (n <= 0 || i0 < 0) return;
-  const int row0 = sq.row0 + i0, pos0 = sq.len - sq.n + i0, rows = n * a.G;
-  const unsigned inv = 65536u / a.G + 1;                             // r / G for r * G < 65536
-  int lim[MB], low[MB];
-  u32x4 q[MB][S];
-#pragma unroll
-  for (int m = 0; m < MB; ++m) {
-    const int r = min(16 * m + l16, rows - 1), i = (r * inv) >> 16;
-    lim[m] = pos0 + i;
-    low[m] = a.window <= lim[m] ? lim[m] - a.window + 1 : 0;
-    const char* x = a.q + (row0 + i) * a.q_t + (h * a.G + r - i * a.G) * a.q_h + hi * 16;
-#pragma unroll
-    for (int s = 0; s < S; ++s) q[m][s] = *(const u32x4*)(x + s * 64);
-  }
-  const int last = min(pos0 + n - 1, (a.s.width << a.kv.lps) - 1);   // of the keys that some row sees
-  const Span keys = {max(a.window <= pos0 ? pos0 - a.window + 1 : 0, 0), last + 1};
-  const Span clear = {a.window <= last ? last - a.window + 1 : 0, pos0 + 1};
-  RowState<D, MB> st;
-  Attend<T, D, MB> at = {a.kv, a.s.table + (long)b * a.s.tstride, keys.lo >> a.kv.lps, max(last, 0) >> a.kv.lps, h, l16, hi, {}};
-  at.run(keys.lo / PA_K + wave, (keys.hi + PA_K - 1) / PA_K, PA_W, keys, clear, lim, low, q, a.scale2, st);
+  const RowTile r = rows_of_sequence(a, b, i0, a.tpt);
+  if (r.n > 0) attend_rows<T, D, MB>(a, r, blockIdx.y, r.t0, r.t0 + r.tiles, nullptr, 0, lds);
+}
 
-  // join the waves: o and sum relative to the largest maximum
+// The keys of all sequences and heads, laid end to end, in equal shares over the blocks: what a share cuts off of a
+// (sequence, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what a
+// later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
+struct First { int b, h, last, pad; };
+template <class T, int D, int MB>
+__global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
+  __shared__ JoinLds<D, MB> lds;
+  const int p = blockIdx.x, lane = threadIdx.x & 63, heads = a.kv.heads;
+  First* first = (First*)a.workspace;
+  float* parts = (float*)(first + gridDim.x);
+  const long part_size = (long)a.rows_cap * (D + 2);
+  // this share's first sequence: every wave sums the tiles of all, 64 runs of sequences at a time
+  int lo = 0, count = a.s.B;
+  long before = 0, share = 0, x = 0;
+  for (bool top = true;; top = false) {
+    const int per = (count + 63) >> 6, b0 = lo + lane * per, b1 = min(lo + count, b0 + per);
+    long mine = 0;
+    for (int b = b0; b < b1; ++b) mine += rows_of_sequence(a, b, 0, a.tpt).tiles;
+    long up = mine;
 #pragma unroll
-  for (int m = 0; m < MB; ++m) {
-    st.sum[m] = sum_of_4(st.sum[m]);
-    if (hi == 0) { sm[wave][m][l16] = st.top[m]; sl[wave][m][l16] = st.sum[m]; }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int m = 0; m < MB; ++m) {
-    if (16 * m >= rows) break;
-    float top = sm[0][m][l16];
-#pragma unroll
-    for (int w = 1; w < PA_W; ++w) top = fmaxf(top, sm[w][m][l16]);
-    const float keep = st.top[m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.top[m] - top);
-    if (m) __syncthreads();
-#pragma unroll
-    for (int j = 0; j < J; ++j) *(f32x4*)&so[wave][l16][16 * j + 4 * hi] = st.o[m][j] * keep;
-    __syncthreads();
-    const int r16 = tid / (D / 8), oct = tid % (D / 8), r = 16 * m + r16;
-    if (r16 < 16 && r < rows) {
-      float t = sm[0][m][r16], sum = 0.f;
-#pragma unroll
-      for (int w = 1; w < PA_W; ++w) t = fmaxf(t, sm[w][m][r16]);
-      f32x8 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < PA_W; ++w) {
-        const float tw = sm[w][m][r16];
-        sum += tw == -INFINITY ? 0.f : sl[w][m][r16] * __builtin_amdgcn_exp2f(tw - t);
-        const f32x4 y0 = *(const f32x4*)&so[w][r16][oct * 8], y1 = *(const f32x4*)&so[w][r16][oct * 8 + 4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { x[e] += y0[e]; x[4 + e] += y1[e]; }
-      }
-      const float f = sum == 0.f ? 0.f : 1.f / sum;                  // a row that sees no key is zero
-      const int i = (r * inv) >> 16;
-      *(u32x4*)(a.o + (row0 + i) * a.o_t + (h * a.G + r - i * a.G) * a.o_h + oct * 16) = to_16<T>(x * f);
+    for (int m = 1; m < 64; m *= 2) {
+      const long y = __shfl_up(up, m, 64);
+      if (lane >= m) up += y;
     }
+    if (top) {
+      const long all = __shfl(up, 63, 64) * heads;
+      share = max((all + gridDim.x - 1) / gridDim.x, (long)a.least);
+      x = p * share;
+      if (x >= all) {
+        if (threadIdx.x == 0) first[p].b = -1;
+        return;
+      }
+    }
+    const int k = max(__ffsll((long long)__ballot((before + up) * heads > x)) - 1, 0);
+    before += __shfl(up - mine, k, 64);
+    lo += k * per;
+    if (per == 1) break;
+    count = min(per, count - k * per);
+  }
+  int b = __builtin_amdgcn_readfirstlane(lo);
+  RowTile r = rows_of_sequence(a, b, 0, a.tpt);
+  const long rel = x - before * heads;
+  const int tiles = max(r.tiles, 1);
+  int h = __builtin_amdgcn_readfirstlane((int)min(rel / tiles, heads - 1l)), t = __builtin_amdgcn_readfirstlane((int)(rel % tiles));
+  int left = __builtin_amdgcn_readfirstlane((int)min(share, 1l << 30)), at = 0;     // at: tiles done, of this share
+  int begun = -1;
+  while (true) {
+    const int n = min(left, r.tiles - t);
+    const bool whole = n == r.tiles;
+    if (!whole && t == 0) {
+      begun = b;
+      if (threadIdx.x == 0) first[p] = First{b, h, (int)((x + at + r.tiles - 1) / share), 0};
+    }
+    attend_rows<T, D, MB>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
+    left -= n;
+    at += n;
+    t = 0;
+    if (left == 0) break;
+    if (++h == heads) {
+      h = 0;
+      do {
+        if (++b >= a.s.B) break;
+        r = rows_of_sequence(a, b, 0, a.tpt);
+      } while (r.tiles == 0);
+      if (b >= a.s.B) break;
+    }
+    __syncthreads();                                                 // the next part's joining
+  }
+  if (begun < 0 && threadIdx.x == 0) first[p].b = -1;
+}
+
+// Parts joined: a block for each (sequence, head) that was cut, and up to JN_R rows of it
+constexpr int JN_R = 4;
+template <class T, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a, int blocks) {
+  constexpr int W = D / 4, NP = 256 / W;                             // threads of a row; parts at a time
+  __shared__ float weight[1024], red[4];
+  __shared__ __attribute__((aligned(16))) float so[NP][D + 4];
+  __shared__ float ssum[NP];
+  const int p = blockIdx.x, tid = threadIdx.x;
+  const First f = ((const First*)a.workspace)[p];
+  if (f.b < 0) return;
+  const RowTile r = rows_of_sequence(a, f.b, 0, a.tpt);
+  const float* parts = (const float*)((const First*)a.workspace + blocks);
+  const long part_size = (long)a.rows_cap * (D + 2);
+  const int n = min(f.last - p + 1, 1024), rows = r.n * a.G;
+  const auto part = [&](int j) { return parts + (2 * (p + j) + (j == 0)) * part_size; };
+  for (int row = blockIdx.y * JN_R; row < min(rows, (int)blockIdx.y * JN_R + JN_R); ++row) {
+    float top = -INFINITY;
+    for (int j = tid; j < n; j += 256) top = fmaxf(top, weight[j] = part(j)[a.rows_cap * D + 2 * row]);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+    if ((tid & 63) == 0) red[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    if (top == -INFINITY) top = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    const int g = tid / W, d = tid % W * 4;
+    for (int j = g; j < n; j += NP) {
+      const float w = __builtin_amdgcn_exp2f(weight[j] - top);
+      const float* y = part(j);
+      x += *(const f32x4*)(y + row * D + d) * w;
+      sum += y[a.rows_cap * D + 2 * row + 1] * w;
+    }
+    *(f32x4*)&so[g][d] = x;
+    if (tid % W == 0) ssum[g] = sum;
+    __syncthreads();
+    if (tid < W) {
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) { o += *(const f32x4*)&so[i][d]; s += ssum[i]; }
+      o *= s == 0.f ? 0.f : 1.f / s;
+      const int i = row / a.G;
+      typedef __attribute__((ext_vector_type(4))) unsigned short u16x4;
+      *(u16x4*)(a.o + (r.row0 + i) * a.o_t + (f.h * a.G + row - i * a.G) * a.o_h + d * 2) = __builtin_bit_cast(u16x4, __builtin_convertvector(o, typename T::v4));
+    }
+    __syncthreads();
   }
 }
+
+// Blocks of a launch that shares out the keys: what the chip holds at once
+template <int D, int MB>
+constexpr int split_blocks() { return 256 * blocks_of(D, MB); }
+constexpr int kSplitLeast = 4;     // tiles of a share: one for each wave
 
 template <class T, int D, int MB>
 static void rows_grid(PagedAttnArgs a, hipStream_t s) {
   a.tpt = 16 * MB / a.G;
+  if (a.workspace) {
+    a.tpt = a.max_new;
+    const int blocks = split_blocks<D, MB>();
+    a.rows_cap = a.max_new * a.G;
+    a.least = kSplitLeast;
+    hipLaunchKernelGGL((paged_split_kernel<T, D, MB>), dim3(blocks), dim3(64 * PA_W), 0, s, a);
+    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(blocks, (a.rows_cap + JN_R - 1) / JN_R), dim3(256), 0, s, a, blocks);
+    return;
+  }
   a.by_tpt = FastDiv::by(a.tpt);
   const int tiles = a.max_new > a.tpt ? a.s.T / a.tpt + a.s.B : a.s.B;
   hipLaunchKernelGGL((paged_rows_kernel<T, D, MB>), dim3(tiles, a.kv.heads), dim3(64 * PA_W), 0, s, a);
@@ -257,6 +432,14 @@ static void rows_of(const PagedAttnArgs& a, hipStream_t s) {
   if (rows <= 16) rows_grid<T, D, 1>(a, s);
   else if (rows <= 32) rows_grid<T, D, 2>(a, s);
   else rows_grid<T, D, 4>(a, s);
+}
+
+size_t paged_attention_workspace(int n_seqs, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
+  const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
+  if (rows > 64 || keys <= 1024) return 0;
+  const int mb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const size_t blocks = 256 * blocks_of(head_dim, mb);
+  return blocks * (sizeof(First) + 2 * rows * (head_dim + 2) * sizeof(float));
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) {

@@ -12,6 +12,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 // Element types: eight of them are one 16-byte access and one operand of the matrix instructions.
 struct Bf16 {
   typedef __attribute__((ext_vector_type(8))) __bf16 v8;
+  typedef __attribute__((ext_vector_type(4))) __bf16 v4;
   static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {     // 16 x 16 += 16 x 32 by 32 x 16
 #if defined(__HIP_DEVICE_COMPILE__)
     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -21,6 +22,7 @@ struct Bf16 {
 };
 struct Fp16 {
   typedef __attribute__((ext_vector_type(8))) _Float16 v8;
+  typedef __attribute__((ext_vector_type(4))) _Float16 v4;
   static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
 #if defined(__HIP_DEVICE_COMPILE__)
     c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
@@ -111,9 +113,12 @@ struct PagedAttnArgs {
   int window;                                    // keys that a token sees, its own among them; INT_MAX: all
   float scale2;                                  // scale * log2(e)
   int max_new;
+  void* workspace;                               // of paged_attention_workspace() bytes, or nullptr where that is none
   int tpt;                                       // filled by the launcher: tokens of a tile of rows
   FastDiv by_tpt;
+  int rows_cap, least;                           // rows of a part; least tiles of a share
 };
+size_t paged_attention_workspace(int n_seqs, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 
 struct VerifyArgs {

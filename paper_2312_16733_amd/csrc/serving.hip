@@ -89,13 +89,24 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
 }
 
 
-sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
-                               const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* hip_stream) {
+int64_t sna_paged_attention_workspace_bytes(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, int32_t window) {
   sna_status st;
   if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, q_heads)) != SNA_OK) return st;
   if (window < 0) return fail(SNA_E_CFG_RANGE, "window %d", window);
+  if (batch->n_seqs == 0 || batch->n_tokens == 0) return 0;
+  return (int64_t)paged_attention_workspace(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads, batch->max_new, batch->max_len, window, cache->head_dim);
+}
+
+sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
+                               const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* workspace_dev,
+                               size_t workspace_bytes, void* hip_stream) {
+  sna_status st;
+  const int64_t need = sna_paged_attention_workspace_bytes(cache, batch, q_heads, window);
+  if (need < 0) return (sna_status)need;
   if (batch->n_seqs == 0 || batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_rows(out, "out")) != SNA_OK) return st;
+  if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))
+    return fail(SNA_E_WORKSPACE, "paged_attention: a workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
   PagedAttnArgs a = {};
   a.s = seqs_of(batch);
   a.kv = kv_of(cache);
@@ -106,10 +117,10 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   a.window = window ? window : INT32_MAX;
   a.scale2 = scale * 1.44269504088896340736f;
   a.max_new = batch->max_new;
+  a.workspace = need > 0 ? workspace_dev : nullptr;
   const hipError_t e = launch_paged_attention(a, cache->dtype, cache->head_dim, (hipStream_t)hip_stream);
   return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "paged_attention: %s", hipGetErrorString(e));
 }
-
 
 sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, int64_t target_row_stride, const float* draft_dev,
                             int64_t draft_seq_stride, int64_t draft_row_stride, const void* tokens_dev, int32_t token_bytes,

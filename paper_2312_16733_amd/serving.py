@@ -138,16 +138,22 @@ def kv_append(cache, batch, q, k, v, inv_freq=None, interleaved=False, q_norm=No
     return out
 
 
-def paged_attention(cache, batch, q, scale=None, window=0, out=None, stream=None):
+def paged_attention(cache, batch, q, scale=None, window=0, out=None, workspace=None, stream=None):
     """Causal attention of the step's q [tokens][heads][head_dim] over the cached keys and values, these tokens' own among them
-    (after kv_append).  heads is a multiple of kv_heads.  window: keys that a token sees, its own among them; 0: all."""
+    (after kv_append).  heads is a multiple of kv_heads.  window: keys that a token sees, its own among them; 0: all.
+    workspace: a dense uint8 tensor that is used where it is large enough, instead of one from the allocator."""
     if stream is not None:
         with _On(cache.device, stream):
-            return paged_attention(cache, batch, q, scale, window, out)
+            return paged_attention(cache, batch, q, scale, window, out, workspace)
     qr, out, outr = _step(cache, batch, q, out)
+    need = _check(binding.lib().sna_paged_attention_workspace_bytes(cache.c, batch.c, q.shape[1], window))
+    if need and (workspace is None or workspace.numel() < need):
+        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    elif need:
+        _need(workspace.dtype == torch.uint8 and workspace.device == cache.device and workspace.is_contiguous(), f"workspace: dense uint8 on {cache.device} is needed")
     with torch.cuda.device(cache.device):
         _check(binding.lib().sna_paged_attention(cache.c, batch.c, q.shape[1], qr, outr, cache.head_dim ** -0.5 if scale is None else scale, window,
-                                                 torch.cuda.current_stream(cache.device).cuda_stream))
+                                                 workspace.data_ptr() if need else None, need, torch.cuda.current_stream(cache.device).cuda_stream))
     return out
 
 

@@ -330,3 +330,18 @@ def test_verification_follows_the_target():
     got, _ = sna.verify_draft(p.expand(n, 2, V).contiguous().cuda(), tokens.cuda(), u.cuda(), draft_probs=q.expand(n, 1, V).contiguous().cuda())
     share = torch.bincount(got[:, 0].cpu(), minlength=V) / n
     assert ((share - p).abs() <= 5 * (p * (1 - p) / n).sqrt()).all()
+
+
+@pytest.mark.parametrize("heads,page,seqs,window", [
+    ((32, 8, 128), 16, [(1100 + 37 * i % 900, i % 4 != 3) for i in range(100)], 0),                  # shares that begin and end anywhere
+    ((8, 1, 64), 32, [(5000, 1), (1, 1), (0, 0)] + [(64 * i + 1, 2) for i in range(1, 30)], 0),
+    ((16, 2, 64), 16, [(900 + i, i % 2) for i in range(330)] + [(3000, 1)], 0),                       # more sequences than lanes
+    ((4, 4, 128), 64, [(7000, 16), (4000, 3), (6999, 9)], 2000)])
+def test_attention_of_keys_shared_out(heads, page, seqs, window):
+    s = ref.make([(l, int(n)) for l, n in seqs], *heads, page, torch.bfloat16, seed=15)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, window)
+    workspace = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")                      # NaN wherever it is read as fp32
+    a = sna.paged_attention(cache, batch, s["q"], window=window, workspace=workspace)
+    within(a, want, err, "out")
+    assert torch.equal(sna.paged_attention(cache, batch, s["q"], window=window), a)                 # the sums' order is fixed

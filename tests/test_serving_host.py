@@ -26,8 +26,8 @@ def rows(dev=AT, token_stride=512, head_stride=64):
     return RowsC(dev, token_stride, head_stride)
 
 
-def attention(c=None, b=None, heads=4, q=None, out=None, scale=0.1, window=0):
-    return sna.lib().sna_paged_attention(c or cache(), b or batch(), heads, q or rows(), out or rows(), scale, window, None)
+def attention(c=None, b=None, heads=4, q=None, out=None, scale=0.1, window=0, ws=AT, size=1 << 40):
+    return sna.lib().sna_paged_attention(c or cache(), b or batch(), heads, q or rows(), out or rows(), scale, window, ws, size, None)
 
 
 def append(c=None, b=None, heads=4, q=None, k=None, v=None, out=None, inv=AT, rot=64, qn=None, kn=None):
@@ -62,6 +62,17 @@ def test_rows_are_refused():
         assert append(rot=rot) == RANGE
     assert append(inv=None) == NULL
     assert append(qn=AT) == NULL and append(kn=AT) == NULL
+
+
+def test_workspaces_are_refused():
+    long = batch(max_len=100000)
+    need = sna.lib().sna_paged_attention_workspace_bytes(cache(), long, 4, 0)
+    assert need > 0
+    for bad in (dict(ws=None), dict(ws=AT + 8), dict(size=need - 1)):
+        assert attention(b=long, **bad) == -7, bad
+    assert sna.lib().sna_paged_attention_workspace_bytes(cache(), batch(), 4, 0) == 0                # short: no parts
+    assert sna.lib().sna_paged_attention_workspace_bytes(cache(), long, 4, 500) == 0
+    assert sna.lib().sna_paged_attention_workspace_bytes(cache(dtype=0), long, 4, 0) == RANGE
 
 
 def test_a_step_without_tokens_is_no_launch():
