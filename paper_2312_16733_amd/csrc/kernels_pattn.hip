@@ -443,6 +443,7 @@ size_t paged_attention_workspace(int n_seqs, int kv_heads, int group, int max_ne
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) {
+  if ((long)a.max_new * a.G > 64) return launch_paged_chunks(a, dtype, head_dim, s);
   if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? rows_of<Fp16, 64>(a, s) : rows_of<Fp16, 128>(a, s);
   else head_dim == 64 ? rows_of<Bf16, 64>(a, s) : rows_of<Bf16, 128>(a, s);
   return hipGetLastError();

@@ -19,6 +19,12 @@ struct Bf16 {
 #endif
     return c;
   }
+  static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {     // 32 x 32 += 32 x 16 by 16 x 32
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+#endif
+    return c;
+  }
 };
 struct Fp16 {
   typedef __attribute__((ext_vector_type(8))) _Float16 v8;
@@ -26,6 +32,12 @@ struct Fp16 {
   static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
 #if defined(__HIP_DEVICE_COMPILE__)
     c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+#endif
+    return c;
+  }
+  static __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
 #endif
     return c;
   }
@@ -69,21 +81,34 @@ __device__ __forceinline__ int last_at_most(int n, int x, F f) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Over the two lanes that share lane % 32
+__device__ __forceinline__ float max_of_2(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#endif
+  return v;
+}
+__device__ __forceinline__ float sum_of_2(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+#endif
+  return v;
+}
 // Over the four lanes that share lane % 16
 __device__ __forceinline__ float max_of_4(float v) {
+  v = max_of_2(v);
 #if defined(__HIP_DEVICE_COMPILE__)
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 #endif
   return v;
 }
 __device__ __forceinline__ float sum_of_4(float v) {
+  v = sum_of_2(v);
 #if defined(__HIP_DEVICE_COMPILE__)
-  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
 #endif
   return v;
@@ -119,6 +144,7 @@ struct PagedAttnArgs {
   int rows_cap, least;                           // rows of a part; least tiles of a share
 };
 size_t paged_attention_workspace(int n_seqs, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
+hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 
 struct VerifyArgs {

@@ -1,5 +1,7 @@
 // C entries of the autoregressive serving operators: argument checks, then one or two launches.  Nothing here allocates or
 // throws.
+#include <cmath>
+
 #include "host.h"
 #include "paged.h"
 
@@ -103,6 +105,7 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   sna_status st;
   const int64_t need = sna_paged_attention_workspace_bytes(cache, batch, q_heads, window);
   if (need < 0) return (sna_status)need;
+  if (!(scale > 0.f && scale < INFINITY)) return fail(SNA_E_CFG_RANGE, "scale %g (a positive number is needed)", (double)scale);
   if (batch->n_seqs == 0 || batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_rows(out, "out")) != SNA_OK) return st;
   if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))

@@ -58,6 +58,8 @@ def test_rows_are_refused():
         for name in ("q", "k", "v", "out"):
             assert append(**{name: bad}) == status, name
     assert attention(window=-1) == RANGE
+    for scale in (0.0, -0.1, float("inf"), float("nan")):
+        assert attention(scale=scale) == RANGE
     for rot in (-16, 8, 72, 80):
         assert append(rot=rot) == RANGE
     assert append(inv=None) == NULL
