@@ -7,6 +7,7 @@
 // but for two exchanges.  The keys of a product's 16 rows are chosen so (row 4 h + c of product a is key 8 h + 4 a + c of 32)
 // that a lane's scores are the eight keys that the second product wants of it, without a trip through LDS.
 #include <algorithm>
+#include <climits>
 
 #include "paged.h"
 
@@ -14,6 +15,7 @@ namespace sna {
 
 constexpr int PA_W = 4;            // waves of a block: they take tiles of keys in turn and are joined in LDS
 constexpr int PA_K = 64;           // keys of a tile
+constexpr long kFewRows = 256 * 64;   // rows of a step, all heads, up to which this kernel is used for chunks, too
 
 // One wave's statistics of MB x 16 rows: row of queries 16 m + lane % 16, element of o[m][j][c]: dim 16 j + 4 (lane / 16) + c
 template <int D, int MB>
@@ -86,50 +88,36 @@ struct Attend {
     load_v(t0, now, v);
     find(t0 + step);
     for (int t = t0; t < t1; t += step) {
-      f32x4 sc[MB][2][2];
+      const bool more = t + step < t1;
+      u32x4 p[MB][2];
 #pragma unroll
-      for (int m = 0; m < MB; ++m)
+      for (int m = 0; m < MB; ++m) {
+        f32x4 sc[2][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
-            sc[m][u][a] = f32x4{0.f, 0.f, 0.f, 0.f};
+            sc[u][a] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < S; ++s) sc[m][u][a] = T::mma16(k[u][a][s], q[m][s], sc[m][u][a]);
+            for (int s = 0; s < S; ++s) sc[u][a] = T::mma16(k[u][a][s], q[m][s], sc[u][a]);
           }
-      const bool more = t + step < t1;
-      if (more) {
+        if (m == MB - 1 && more) {                                   // the next keys come in under the softmax and the second product
 #pragma unroll
-        for (int i = 0; i < 4; ++i) now[i] = ids[i];
-        load_k(t + step, now, k);
-        find(t + 2 * step);
-      }
-      u32x4 p[MB][2];
-#pragma unroll
-      for (int m = 0; m < MB; ++m) {
-        const int key0 = t * PA_K + 8 * hi;
+          for (int i = 0; i < 4; ++i) now[i] = ids[i];
+          load_k(t + step, now, k);
+          find(t + 2 * step);
+        }
         if (t * PA_K < clear.lo || t * PA_K + PA_K > clear.hi) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int a = 0; a < 2; ++a)
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const int key = key0 + 32 * u + 4 * a + c;
-                sc[m][u][a][c] = key <= lim[m] && key >= low[m] ? sc[m][u][a][c] * scale2 : -INFINITY;
-              }
-        } else {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int a = 0; a < 2; ++a)
-#pragma unroll
-              for (int c = 0; c < 4; ++c) sc[m][u][a][c] *= scale2;
+          for (int i = 0; i < 16; ++i) {
+            const int key = t * PA_K + 8 * hi + 32 * (i >> 3) + (i & 7);
+            sc[i >> 3][(i >> 2) & 1][i & 3] = key <= lim[m] && key >= low[m] ? sc[i >> 3][(i >> 2) & 1][i & 3] : -INFINITY;
+          }
         }
-        float x = sc[m][0][0][0];
+        float x = sc[0][0][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) x = fmaxf(x, sc[m][i >> 3][(i >> 2) & 1][i & 3]);
-        const float top = fmaxf(st.top[m], max_of_4(x));
+        for (int i = 1; i < 16; ++i) x = fmaxf(x, sc[i >> 3][(i >> 2) & 1][i & 3]);
+        const float top = fmaxf(st.top[m], max_of_4(x) * scale2);
         const float ref = top == -INFINITY ? 0.f : top;              // nothing seen so far
         const float keep = __builtin_amdgcn_exp2f(st.top[m] - ref);
         st.top[m] = top;
@@ -141,7 +129,7 @@ struct Attend {
           f32x8 e;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(sc[m][u][i >> 2][i & 3] - ref);
+            e[i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i >> 2][i & 3], scale2, -ref));
             st.sum[m] += e[i];
           }
           p[m][u] = to_16<T>(e);                                     // the operand type: p is at most 1, off by half a step of it
@@ -177,8 +165,7 @@ struct RowTile {
   Span keys, clear;                // keys that some row sees, keys that all see
   int t0, tiles;                   // tiles of keys; at least one, so that rows without keys are written too
 };
-__device__ __forceinline__ RowTile rows_of_sequence(const PagedAttnArgs& a, int b, int i0, int most) {
-  const Seq sq = sequence(a.s, b);
+__device__ __forceinline__ RowTile rows_of_sequence(const PagedAttnArgs& a, const Seq& sq, int b, int i0, int most) {
   RowTile r;
   r.b = b;
   r.n = i0 < 0 ? 0 : min(sq.n - i0, most);
@@ -279,19 +266,27 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_rows_kernel
     b = last_at_most(a.s.B, tile, tile0);
     i0 = (tile - tile0(b)) * a.tpt;
   }
-  const RowTile r = rows_of_sequence(a, b, i0, a.tpt);
+  const RowTile r = rows_of_sequence(a, sequence(a.s, b), b, i0, a.tpt);
   if (r.n > 0) attend_rows<T, D, MB>(a, r, blockIdx.y, r.t0, r.t0 + r.tiles, nullptr, 0, lds);
 }
 
-// The keys of all sequences and heads, laid end to end, in equal shares over the blocks: what a share cuts off of a
-// (sequence, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what a
-// later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
-struct First { int b, h, last, pad; };
+// Tiles of keys of all tiles of a sequence's rows, for one head; none where the sequence has more rows than are taken here
+__device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) {
+  const Seq sq = sequence(a.s, b);
+  if (sq.n > a.most) return 0;
+  int n = 0;
+  for (int i0 = 0; i0 < sq.n; i0 += a.tpt) n += rows_of_sequence(a, sq, b, i0, a.tpt).tiles;
+  return n;
+}
+// The keys of all tiles of rows and heads, laid end to end, in equal shares over the blocks: what a share cuts off of a
+// (tile of rows, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what
+// a later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
+struct First { int b, i0, h, last; };
 template <class T, int D, int MB>
 __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
   __shared__ JoinLds<D, MB> lds;
   const int p = blockIdx.x, lane = threadIdx.x & 63, heads = a.kv.heads;
-  First* first = (First*)a.workspace;
+  First* first = (First*)a.parts;
   float* parts = (float*)(first + gridDim.x);
   const long part_size = (long)a.rows_cap * (D + 2);
   // this share's first sequence: every wave sums the tiles of all, 64 runs of sequences at a time
@@ -300,7 +295,7 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
   for (bool top = true;; top = false) {
     const int per = (count + 63) >> 6, b0 = lo + lane * per, b1 = min(lo + count, b0 + per);
     long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += rows_of_sequence(a, b, 0, a.tpt).tiles;
+    for (int b = b0; b < b1; ++b) mine += tiles_of_sequence(a, b);
     long up = mine;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
@@ -308,7 +303,7 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
       if (lane >= m) up += y;
     }
     if (top) {
-      const long all = __shfl(up, 63, 64) * heads;
+      const long all = uniform(__shfl(up, 63, 64)) * heads;
       share = max((all + gridDim.x - 1) / gridDim.x, (long)a.least);
       x = p * share;
       if (x >= all) {
@@ -317,24 +312,30 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
       }
     }
     const int k = max(__ffsll((long long)__ballot((before + up) * heads > x)) - 1, 0);
-    before += __shfl(up - mine, k, 64);
+    before += uniform(__shfl(up - mine, k, 64));
     lo += k * per;
     if (per == 1) break;
     count = min(per, count - k * per);
   }
-  int b = __builtin_amdgcn_readfirstlane(lo);
-  RowTile r = rows_of_sequence(a, b, 0, a.tpt);
-  const long rel = x - before * heads;
-  const int tiles = max(r.tiles, 1);
-  int h = __builtin_amdgcn_readfirstlane((int)min(rel / tiles, heads - 1l)), t = __builtin_amdgcn_readfirstlane((int)(rel % tiles));
-  int left = __builtin_amdgcn_readfirstlane((int)min(share, 1l << 30)), at = 0;     // at: tiles done, of this share
-  int begun = -1;
+  // its first tile of rows, head and tile of keys
+  int b = uniform(lo), i0 = 0;
+  Seq sq = uniform(sequence(a.s, b));
+  RowTile r = rows_of_sequence(a, sq, b, 0, a.tpt);
+  long rel = x - before * heads;
+  while (rel >= (long)r.tiles * heads && i0 + a.tpt < sq.n) {
+    rel -= (long)r.tiles * heads;
+    i0 += a.tpt;
+    r = rows_of_sequence(a, sq, b, i0, a.tpt);
+  }
+  int h = uniform((int)min(rel / max(r.tiles, 1), heads - 1l)), t = uniform((int)(rel % max(r.tiles, 1)));
+  int left = (int)min(share, 1l << 30), at = 0;     // at: tiles done, of this share
+  bool begun = false;
   while (true) {
     const int n = min(left, r.tiles - t);
     const bool whole = n == r.tiles;
     if (!whole && t == 0) {
-      begun = b;
-      if (threadIdx.x == 0) first[p] = First{b, h, (int)((x + at + r.tiles - 1) / share), 0};
+      begun = true;
+      if (threadIdx.x == 0) first[p] = First{b, i0, h, (int)((x + at + r.tiles - 1) / share)};
     }
     attend_rows<T, D, MB>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
     left -= n;
@@ -343,15 +344,20 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
     if (left == 0) break;
     if (++h == heads) {
       h = 0;
-      do {
-        if (++b >= a.s.B) break;
-        r = rows_of_sequence(a, b, 0, a.tpt);
-      } while (r.tiles == 0);
-      if (b >= a.s.B) break;
+      i0 += a.tpt;
+      if (i0 >= sq.n) {
+        i0 = 0;
+        do {
+          if (++b >= a.s.B) break;
+          sq = uniform(sequence(a.s, b));
+        } while (sq.n <= 0 || sq.n > a.most);
+        if (b >= a.s.B) break;
+      }
+      r = rows_of_sequence(a, sq, b, i0, a.tpt);
     }
     __syncthreads();                                                 // the next part's joining
   }
-  if (begun < 0 && threadIdx.x == 0) first[p].b = -1;
+  if (!begun && threadIdx.x == 0) first[p].b = -1;
 }
 
 // Parts joined: a block for each (sequence, head) that was cut, and up to JN_R rows of it
@@ -363,10 +369,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a, 
   __shared__ __attribute__((aligned(16))) float so[NP][D + 4];
   __shared__ float ssum[NP];
   const int p = blockIdx.x, tid = threadIdx.x;
-  const First f = ((const First*)a.workspace)[p];
+  const First f = ((const First*)a.parts)[p];
   if (f.b < 0) return;
-  const RowTile r = rows_of_sequence(a, f.b, 0, a.tpt);
-  const float* parts = (const float*)((const First*)a.workspace + blocks);
+  const RowTile r = rows_of_sequence(a, sequence(a.s, f.b), f.b, f.i0, a.tpt);
+  const float* parts = (const float*)((const First*)a.parts + blocks);
   const long part_size = (long)a.rows_cap * (D + 2);
   const int n = min(f.last - p + 1, 1024), rows = r.n * a.G;
   const auto part = [&](int j) { return parts + (2 * (p + j) + (j == 0)) * part_size; };
@@ -405,18 +411,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a, 
   }
 }
 
-// Blocks of a launch that shares out the keys: what the chip holds at once
-template <int D, int MB>
-constexpr int split_blocks() { return 256 * blocks_of(D, MB); }
 constexpr int kSplitLeast = 4;     // tiles of a share: one for each wave
 
 template <class T, int D, int MB>
 static void rows_grid(PagedAttnArgs a, hipStream_t s) {
   a.tpt = 16 * MB / a.G;
-  if (a.workspace) {
-    a.tpt = a.max_new;
-    const int blocks = split_blocks<D, MB>();
-    a.rows_cap = a.max_new * a.G;
+  if (a.parts) {
+    const int blocks = 256 * blocks_of(D, MB);                       // what the chip holds at once
+    if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
+    a.rows_cap = a.tpt * a.G;
     a.least = kSplitLeast;
     hipLaunchKernelGGL((paged_split_kernel<T, D, MB>), dim3(blocks), dim3(64 * PA_W), 0, s, a);
     hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(blocks, (a.rows_cap + JN_R - 1) / JN_R), dim3(256), 0, s, a, blocks);
@@ -427,26 +430,63 @@ static void rows_grid(PagedAttnArgs a, hipStream_t s) {
   hipLaunchKernelGGL((paged_rows_kernel<T, D, MB>), dim3(tiles, a.kv.heads), dim3(64 * PA_W), 0, s, a);
 }
 template <class T, int D>
-static void rows_of(const PagedAttnArgs& a, hipStream_t s) {
-  const long rows = (long)a.max_new * a.G;
-  if (rows <= 16) rows_grid<T, D, 1>(a, s);
-  else if (rows <= 32) rows_grid<T, D, 2>(a, s);
+static void rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
+  if (mb == 1) rows_grid<T, D, 1>(a, s);
+  else if (mb == 2) rows_grid<T, D, 2>(a, s);
   else rows_grid<T, D, 4>(a, s);
 }
-
-size_t paged_attention_workspace(int n_seqs, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
-  const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
-  if (rows > 64 || keys <= 1024) return 0;
-  const int mb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  const size_t blocks = 256 * blocks_of(head_dim, mb);
-  return blocks * (sizeof(First) + 2 * rows * (head_dim + 2) * sizeof(float));
+static size_t parts_bytes(int head_dim, int mb, long rows_cap) {
+  return 256 * blocks_of(head_dim, mb) * (sizeof(First) + 2 * rows_cap * (head_dim + 2) * sizeof(float));
 }
 
-hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) {
-  if ((long)a.max_new * a.G > 64) return launch_paged_chunks(a, dtype, head_dim, s);
-  if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? rows_of<Fp16, 64>(a, s) : rows_of<Fp16, 128>(a, s);
-  else head_dim == 64 ? rows_of<Bf16, 64>(a, s) : rows_of<Bf16, 128>(a, s);
-  return hipGetLastError();
+// How a step is launched, from what the host knows of it.
+struct AttnPlan {
+  int mb;                          // 16 rows of a block of the few-rows kernel, of which there are 1, 2 or 4; 0: not launched
+  bool split;                      // its keys shared out over the blocks
+  int most;                        // tokens of a sequence up to which it takes it
+  bool chunks;                     // the many-rows kernel takes the other sequences
+  int splits;                      // shares of their keys
+  size_t parts, chunk_parts;       // bytes of the workspace, for either
+};
+static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
+  const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
+  AttnPlan p = {};
+  if (rows <= 64 || (long)n_tokens * group * kv_heads <= kFewRows) {
+    p.mb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.split = keys > 1024;
+    p.most = max_new;
+  } else {
+    p.chunks = true;
+    p.splits = paged_chunk_splits(n_tokens, kv_heads, group, max_new, keys);
+    if (p.splits > 1) p.chunk_parts = (size_t)p.splits * n_tokens * kv_heads * group * (head_dim + 2) * sizeof(float);
+    if (n_seqs > 1 && (long)n_seqs * max_new != n_tokens && group <= 16) {    // there may be sequences of few rows
+      p.mb = 1;
+      p.split = true;
+      p.most = 16 / group;
+    }
+  }
+  if (p.mb && p.split) p.parts = (parts_bytes(head_dim, p.mb, (long)std::min(16 * p.mb / group, max_new) * group) + 255) & ~(size_t)255;
+  return p;
+}
+
+size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
+  const AttnPlan p = plan_of(n_seqs, n_tokens, kv_heads, group, max_new, max_len, window, head_dim);
+  return p.parts + p.chunk_parts;
+}
+
+hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s) {
+  const AttnPlan p = plan_of(a.s.B, a.s.T, a.kv.heads, a.G, a.max_new, max_len, a.window == INT_MAX ? 0 : a.window, head_dim);
+  a.most = p.most;
+  if (p.mb) {
+    PagedAttnArgs r = a;
+    r.parts = p.split ? workspace : nullptr;
+    if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? rows_of<Fp16, 64>(r, p.mb, s) : rows_of<Fp16, 128>(r, p.mb, s);
+    else head_dim == 64 ? rows_of<Bf16, 64>(r, p.mb, s) : rows_of<Bf16, 128>(r, p.mb, s);
+  }
+  if (!p.chunks) return hipGetLastError();
+  a.splits = p.splits;
+  a.parts = (char*)workspace + p.parts;
+  return launch_paged_chunks(a, dtype, head_dim, s);
 }
 
 }  // namespace sna

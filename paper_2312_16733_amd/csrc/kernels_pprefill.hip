@@ -39,19 +39,25 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hi = lane >> 5;
   // heads change fastest: where there are 8 of them, each XCD reads one and keeps it in its L2; the last tiles of rows, which
   // see the most keys, first
-  const int h = blockIdx.x % a.kv.heads, tile = gridDim.x / a.kv.heads - 1 - blockIdx.x / a.kv.heads;
+  const int h = blockIdx.x % a.kv.heads, rest = blockIdx.x / a.kv.heads, part = rest % a.splits, tile = gridDim.x / (a.kv.heads * a.splits) - 1 - rest / a.splits;
   const auto tile0 = [&](int i) { return a.by_tpt.div(clamped(a.s.starts[i], 0, a.s.T)) + i; };
   const int b = last_at_most(a.s.B, tile, tile0);
   const Seq sq = sequence(a.s, b);
   const int i0 = (tile - tile0(b)) * a.tpt, n = i0 < 0 ? 0 : min(sq.n - i0, a.tpt);
-  if (n <= 0) return;
+  if (n <= 0 || sq.n <= a.most) return;                              // few rows: not taken here
   const int row0 = sq.row0 + i0, pos0 = sq.len - sq.n + i0, rows = n * a.G;
   const int last = min(pos0 + n - 1, (a.s.width << a.kv.lps) - 1);
   const int first = max(a.window <= pos0 ? pos0 - a.window + 1 : 0, 0);
   int t0 = first / PF_K, t1 = last < 0 ? t0 : last / PF_K + 1;
+  if (a.splits > 1) {                                                // this block's share of the keys
+    const int per = (t1 - t0 + a.splits - 1) / a.splits;
+    t0 = min(t0 + part * per, t1);
+    t1 = min(t0 + per, t1);
+  }
   const int* table = a.s.table + (long)b * a.s.tstride;
   const int c_lo = first >> a.kv.lps, c_hi = max(last, 0) >> a.kv.lps, ps = 1 << a.kv.lps;
-  const auto page = [&](int key) { return clamped(table[clamped(key >> a.kv.lps, c_lo, c_hi)], 0, a.kv.n_pages - 1); };
+  const auto page = [&](int key) { return table[clamped(key >> a.kv.lps, c_lo, c_hi)]; };
+  const auto in_pool = [&](int id) { return clamped(id, 0, a.kv.n_pages - 1); };   // where the page is used: a look at it any earlier would wait for the fetches, too
 
   // this lane's row of queries
   const unsigned inv = 65536u / a.G + 1;
@@ -70,23 +76,31 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
   // fetches: K tile rows of 16 D / 8 bytes, 1 KB an instruction; V tile rows of 128 bytes
   constexpr int KR = 1024 / (D * 2);                                 // keys of a fetch
   const int k_row = lane / (D / 8), k_pos = lane % (D / 8), v_row = lane >> 3, v_pos = lane & 7;
-  int kid, vid[VI > 1 ? 2 : 1];
+  int kid, vid[VI > 1 && W < 8 ? 2 : 1];
   const auto find = [&](int t) {
     kid = page(t * PF_K + KI * KR * wave);                           // KI * KR keys of a wave: within 16 aligned ones
 #pragma unroll
     for (int i = 0; i < (VI > 1 && W < 8 ? 2 : 1); ++i) vid[i] = page(t * PF_K + 8 * (v_pos ^ v_row ^ ((wave + W * i) & 7)));
   };
-  const auto fetch = [&](int t, int buf) {
-    const char* kp = a.kv.k + kid * a.kv.kstride + (long)h * ps * (D * 2);
+  int k_off[KI];                                                     // within the tile's keys, and of their octets
 #pragma unroll
-    for (int i = 0; i < KI; ++i) {
-      const int r = (wave * KI + i) * KR + k_row, slot = (t * PF_K + r) & (ps - 1);
-      fetch16(kp + slot * (D * 2) + (k_pos ^ k_swizzle<D>(r)) * 16, (lds_char*)lds.k[buf] + (wave * KI + i) * 1024);
-    }
+  for (int i = 0; i < KI; ++i) {
+    const int r = (wave * KI + i) * KR + k_row;
+    k_off[i] = (r & (ps - 1)) * (D * 2) + (k_pos ^ k_swizzle<D>(r)) * 16;
+  }
+  const auto fetch = [&](int t, int buf) {
+    const int slot = (t * PF_K) & (ps - 1);
+    const char* kp = a.kv.k + in_pool(__builtin_amdgcn_readfirstlane(kid)) * a.kv.kstride + ((long)h * ps + slot) * (D * 2);
+#pragma unroll
+    for (int i = 0; i < KI; ++i) fetch16(kp + k_off[i], (lds_char*)lds.k[buf] + (wave * KI + i) * 1024);
+    const char* vp[VI > 1 && W < 8 ? 2 : 1];
+#pragma unroll
+    for (int i = 0; i < (VI > 1 && W < 8 ? 2 : 1); ++i)
+      vp[i] = a.kv.v + in_pool(vid[i]) * a.kv.vstride + (((long)h * D + (wave + W * i) * 8 + v_row) * ps + ((t * PF_K + 8 * (v_pos ^ v_row ^ ((wave + W * i) & 7))) & (ps - 1))) * 2;
 #pragma unroll
     for (int i = 0; i < VI; ++i) {
-      const int f = wave + W * i, d = f * 8 + v_row, o = v_pos ^ v_row ^ (f & 7), slot = (t * PF_K + 8 * o) & (ps - 1);
-      fetch16(a.kv.v + vid[W < 8 ? i & 1 : 0] * a.kv.vstride + (((long)h * D + d) * ps + slot) * 2, (lds_char*)lds.v[buf] + f * 1024);
+      if (W == 8) fetch16(vp[0] + i * (W * 16) * ps, (lds_char*)lds.v[buf] + (wave + W * i) * 1024);
+      else fetch16(vp[i & 1] + (i >> 1) * (2 * W * 16) * ps, (lds_char*)lds.v[buf] + (wave + W * i) * 1024);
     }
   };
 
@@ -97,7 +111,11 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
     for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
   float top = -INFINITY, sum = 0.f;                                  // top: of the scores before the scale
   const int key_of = (l32 & 19) | (l32 & 4) << 1 | (l32 & 8) >> 1;   // of the product's row l32
-  const int k_at = key_of * (D * 2), k_sw = k_swizzle<D>(key_of), v_at = l32 * 128;
+  int k_at[S], v_at[4];                                              // octets of the lane's rows; dims 32 and more further on differ by constants
+#pragma unroll
+  for (int s = 0; s < S; ++s) k_at[s] = key_of * (D * 2) + ((2 * s + hi) ^ k_swizzle<D>(key_of)) * 16;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) v_at[s] = l32 * 128 + ((2 * s + hi) ^ v_swizzle(l32)) * 16;
 
   if (t0 < t1) {
     find(t0);
@@ -107,24 +125,36 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
   for (int t = t0, buf = 0; t < t1; ++t, buf ^= 1) {
     __builtin_amdgcn_s_waitcnt(0x0F70);                              // vmcnt(0): this wave's part of the tile has arrived
     __syncthreads();
+    const int key0 = t * PF_K;
+    if (key0 < first || key0 + PF_K > last + 1) {                    // slots of keys that no row sees may hold anything: 0 * NaN is not 0
+      for (int i = tid; i < D * 8; i += 64 * W) {
+        u32x4* x = (u32x4*)lds.v[buf] + i;
+        const int key = key0 + 8 * ((i & 7) ^ v_swizzle(i >> 3));
+        u32x4 y = *x;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          y[w] &= (key + 2 * w >= first && key + 2 * w <= last ? 0xffffu : 0u) | (key + 2 * w + 1 >= first && key + 2 * w + 1 <= last ? 0xffff0000u : 0u);
+        *x = y;
+      }
+      __syncthreads();
+    }
     if (t + 1 < t1) {
       fetch(t + 1, buf ^ 1);
       find(t + 2);
     }
-    const int key0 = t * PF_K;
     if (key0 > w_last || key0 + PF_K <= w_low) continue;             // no row of the wave sees any of it
+    const char *kt = lds.k[buf], *vt = lds.v[buf];
     f32x16 sc[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
 #pragma unroll
-      for (int s = 0; s < S; ++s)
-        sc[u] = T::mma32(*(const u32x4*)(lds.k[buf] + u * (32 * D * 2) + k_at + ((2 * s + hi) ^ k_sw) * 16), q[s], sc[u]);
-    }
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) sc[u] = T::mma32(*(const u32x4*)(kt + u * (32 * D * 2) + k_at[s]), q[s], sc[u]);
     // sc[u][4 (2 s + a) + c]: key 32 u + 16 s + 8 hi + 4 a + c of the tile
-    const bool edge = key0 + PF_K - 1 > w_all || key0 < w_first;
-    if (edge) {
+    if (key0 + PF_K - 1 > w_all || key0 < w_first) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -160,25 +190,24 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
       }
       p[s] = to_16<T>(e);                                            // off by half a step of the operand type
     }
-    const bool partial = key0 < first || key0 + PF_K > last + 1;     // slots that hold no key may hold anything: 0 * NaN is not 0
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int d = 32 * j + l32;
-        u32x4 v = *(const u32x4*)(lds.v[buf] + j * (32 * 128) + v_at + ((2 * s + hi) ^ v_swizzle(d)) * 16);
-        if (partial) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int key = key0 + 16 * s + 8 * hi + 2 * w;
-            v[w] &= (key >= first && key <= last ? 0xffffu : 0u) | (key + 1 >= first && key + 1 <= last ? 0xffff0000u : 0u);
-          }
-        }
-        o[j] = T::mma32(v, p[s], o[j]);
-      }
+      for (int j = 0; j < J; ++j) o[j] = T::mma32(*(const u32x4*)(vt + j * (32 * 128) + v_at[s ^ 2 * (j & 1)]), p[s], o[j]);
   }
   sum = sum_of_2(sum);
   if (!mine) return;
+  if (a.splits > 1) {                                                // a part: sums, then maximum and sum
+    const long r = ((long)part * a.s.T + qi) * (a.kv.heads * a.G) + qh;
+    float* out = (float*)a.parts + r * D + hi * 4;
+    if (sum != 0.f)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *(f32x4*)(out + 32 * j + 8 * i) = f32x4{o[j][4 * i], o[j][4 * i + 1], o[j][4 * i + 2], o[j][4 * i + 3]};
+    if (hi == 0) ((float2*)((float*)a.parts + (long)a.splits * a.s.T * a.kv.heads * a.G * D))[r] = make_float2(top * a.scale2, sum);
+    return;
+  }
   const float f = sum == 0.f ? 0.f : 1.f / sum;                      // a row that sees no key is zero
   char* out = a.o + qi * a.o_t + qh * a.o_h + hi * 8;
 #pragma unroll
@@ -190,17 +219,70 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
     }
 }
 
+// The parts of a token's rows joined: a block for each token, four dims a thread
 template <class T, int D>
+__global__ __launch_bounds__(256) void paged_chunk_join_kernel(const PagedAttnArgs a) {
+  const int t = blockIdx.x, b = last_at_most(a.s.B, t, [&](int i) { return clamped(a.s.starts[i], 0, a.s.T); });
+  const Seq sq = sequence(a.s, b);
+  if (t >= sq.row0 + sq.n || sq.n <= a.most) return;                 // nobody's row, or one that the other kernel has written
+  const int heads = a.kv.heads * a.G;
+  const long step = (long)a.s.T * heads;
+  const float* parts = (const float*)a.parts;
+  const float2* stats = (const float2*)(parts + a.splits * step * D);
+  for (int i = threadIdx.x; i < heads * (D / 4); i += 256) {
+    const int h = i / (D / 4), d = i % (D / 4) * 4;
+    const long r = (long)t * heads + h;
+    float top = -INFINITY;
+    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, stats[p * step + r].x);
+    if (top == -INFINITY) top = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int p = 0; p < a.splits; ++p) {
+      const float2 st = stats[p * step + r];
+      if (st.y == 0.f) continue;                                     // no key of it is seen, and its sums are not written
+      const float w = __builtin_amdgcn_exp2f(st.x - top);
+      x += *(const f32x4*)(parts + (p * step + r) * D + d) * w;
+      sum += st.y * w;
+    }
+    x *= sum == 0.f ? 0.f : 1.f / sum;
+    *(uint2*)(a.o + t * a.o_t + h * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
+  }
+}
+
+// Rows of a block: 32 a wave, 8 waves, or 4 where no sequence has more of them
+static int chunk_waves(int max_new, int group) { return (long)max_new * group <= 128 ? 4 : 8; }
+
+// Shares of the keys.  A step of fewer blocks than the chip holds leaves CUs idle; with S shares it takes ceil(blocks S /
+// capacity) rounds of 1 / S of the time each, and writing and joining the parts costs some percent for each share.  A share
+// has 8 tiles of keys or more.
+int paged_chunk_splits(int n_tokens, int kv_heads, int group, int max_new, long keys) {
+  const int waves = chunk_waves(max_new, group);
+  const long tpt = 32 * waves / group, blocks = (n_tokens + tpt - 1) / tpt * kv_heads, room = 256 * (8 / waves);
+  if (blocks >= room) return 1;
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= 8 && (s == 1 || keys >= 8l * PF_K * s); ++s) {
+    const double cost = (double)((blocks * s + room - 1) / room) / s + 0.03 * (s - 1);
+    if (cost < least) { least = cost; best = s; }
+  }
+  return best;
+}
+
+template <class T, int D, int W>
 static void chunk_grid(PagedAttnArgs a, hipStream_t s) {
-  constexpr int W = 8;
   a.tpt = 32 * W / a.G;
   a.by_tpt = FastDiv::by(a.tpt);
-  hipLaunchKernelGGL((paged_chunk_kernel<T, D, W>), dim3((a.s.T / a.tpt + a.s.B) * a.kv.heads), dim3(64 * W), 0, s, a);
+  hipLaunchKernelGGL((paged_chunk_kernel<T, D, W>), dim3((a.s.T / a.tpt + a.s.B) * a.kv.heads * a.splits), dim3(64 * W), 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((paged_chunk_join_kernel<T, D>), dim3(a.s.T), dim3(256), 0, s, a);
+}
+template <class T, int D>
+static void chunk_of(const PagedAttnArgs& a, hipStream_t s) {
+  chunk_waves(a.max_new, a.G) == 4 ? chunk_grid<T, D, 4>(a, s) : chunk_grid<T, D, 8>(a, s);
 }
 
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) {
-  if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? chunk_grid<Fp16, 64>(a, s) : chunk_grid<Fp16, 128>(a, s);
-  else head_dim == 64 ? chunk_grid<Bf16, 64>(a, s) : chunk_grid<Bf16, 128>(a, s);
+  if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? chunk_of<Fp16, 64>(a, s) : chunk_of<Fp16, 128>(a, s);
+  else head_dim == 64 ? chunk_of<Bf16, 64>(a, s) : chunk_of<Bf16, 128>(a, s);
   return hipGetLastError();
 }
 

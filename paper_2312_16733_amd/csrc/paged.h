@@ -61,11 +61,16 @@ struct PagedKV {
 };
 struct Seq { int row0, n, len; };    // first row, new tokens, cached tokens with them
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }      // in scalar registers
+__device__ __forceinline__ long uniform(long x) {
+  return (long)((unsigned long)(unsigned)uniform((int)(x >> 32)) << 32 | (unsigned)uniform((int)x));
+}
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
 __device__ __forceinline__ Seq sequence(const PagedSeqs& s, int b) {
   const int r0 = clamped(s.starts[b], 0, s.T), r1 = clamped(s.starts[b + 1], 0, s.T);
   return Seq{r0, max(r1 - r0, 0), clamped(s.lens[b], 0, 1 << 30)};
 }
+__device__ __forceinline__ Seq uniform(const Seq& q) { return Seq{uniform(q.row0), uniform(q.n), uniform(q.len)}; }
 // The largest i of [0, n) with f(i) <= x, for a rising f with f(0) <= x: 64 places at a time, one of them a lane, so that
 // up to 64 sequences cost one round trip to memory and up to 4096 two.
 template <class F>
@@ -78,7 +83,7 @@ __device__ __forceinline__ int last_at_most(int n, int x, F f) {
     lo += (__popcll(__ballot(in)) - 1) * step;
     hi = min(hi, lo + step);
   }
-  return __builtin_amdgcn_readfirstlane(lo);
+  return uniform(lo);
 }
 
 // Over the two lanes that share lane % 32
@@ -138,14 +143,18 @@ struct PagedAttnArgs {
   int window;                                    // keys that a token sees, its own among them; INT_MAX: all
   float scale2;                                  // scale * log2(e)
   int max_new;
-  void* workspace;                               // of paged_attention_workspace() bytes, or nullptr where that is none
-  int tpt;                                       // filled by the launcher: tokens of a tile of rows
+  // filled by the launchers
+  int most;                                      // tokens of a sequence up to which the few-rows kernel takes it, not the other
+  void* parts;                                   // parts of sums, where the keys are shared out over blocks
+  int tpt;                                       // tokens of a tile of rows
   FastDiv by_tpt;
   int rows_cap, least;                           // rows of a part; least tiles of a share
+  int splits;                                    // many rows: shares of the keys
 };
-size_t paged_attention_workspace(int n_seqs, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
+size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
+int paged_chunk_splits(int n_tokens, int kv_heads, int group, int max_new, long keys);
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
-hipError_t launch_paged_attention(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
 
 struct VerifyArgs {
   const float *target, *draft;                   // [seq][K + 1][V], [seq][K][V] or nullptr

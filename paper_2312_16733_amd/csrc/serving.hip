@@ -96,7 +96,7 @@ int64_t sna_paged_attention_workspace_bytes(const sna_paged_cache* cache, const 
   if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, q_heads)) != SNA_OK) return st;
   if (window < 0) return fail(SNA_E_CFG_RANGE, "window %d", window);
   if (batch->n_seqs == 0 || batch->n_tokens == 0) return 0;
-  return (int64_t)paged_attention_workspace(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads, batch->max_new, batch->max_len, window, cache->head_dim);
+  return (int64_t)paged_attention_workspace(batch->n_seqs, batch->n_tokens, cache->kv_heads, q_heads / cache->kv_heads, batch->max_new, batch->max_len, window, cache->head_dim);
 }
 
 sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
@@ -120,8 +120,7 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   a.window = window ? window : INT32_MAX;
   a.scale2 = scale * 1.44269504088896340736f;
   a.max_new = batch->max_new;
-  a.workspace = need > 0 ? workspace_dev : nullptr;
-  const hipError_t e = launch_paged_attention(a, cache->dtype, cache->head_dim, (hipStream_t)hip_stream);
+  const hipError_t e = launch_paged_attention(a, cache->dtype, cache->head_dim, batch->max_len, workspace_dev, (hipStream_t)hip_stream);
   return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "paged_attention: %s", hipGetErrorString(e));
 }
 

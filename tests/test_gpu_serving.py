@@ -345,3 +345,19 @@ def test_attention_of_keys_shared_out(heads, page, seqs, window):
     a = sna.paged_attention(cache, batch, s["q"], window=window, workspace=workspace)
     within(a, want, err, "out")
     assert torch.equal(sna.paged_attention(cache, batch, s["q"], window=window), a)                 # the sums' order is fixed
+
+
+@pytest.mark.parametrize("heads,page,seqs,window", [
+    ((32, 8, 128), 16, [(3000, 600), (2500, 1), (1400, 4), (900, 5), (700, 0), (1300, 130)], 0),     # beside the chunks: single tokens, drafts, idle ones
+    ((8, 1, 64), 32, [(5000, 2500)], 0), ((8, 2, 128), 64, [(6000, 3000), (4100, 1)], 0),            # keys of chunks in shares
+    ((32, 8, 64), 16, [(200 + 5 * i, 20 + i % 10) for i in range(40)], 0),                           # many short chunks
+    ((40, 8, 128), 128, [(1000, 450), (2000, 10)], 700), ((64, 2, 64), 16, [(700, 300), (1200, 2), (60, 60)], 0)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_attention_of_mixed_steps(dtype, heads, page, seqs, window):
+    s = ref.make(seqs, *heads, page, ref.DT[dtype], seed=16)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, window)
+    workspace = torch.full((256 << 20,), 255, dtype=torch.uint8, device="cuda")
+    a = sna.paged_attention(cache, batch, s["q"], window=window, workspace=workspace)
+    within(a, want, err, "out")
+    assert torch.equal(sna.paged_attention(cache, batch, s["q"], window=window), a)
