@@ -1,4 +1,4 @@
-"""Builds libsubnetact.so (HIP kernels + C ABI) for gfx950 with hipcc, in tree."""
+"""Builds libsubnetact.so (HIP kernels + C ABI) for gfx950 with hipcc, and the serving binding, in tree."""
 import concurrent.futures as cf
 import os
 import subprocess
@@ -8,6 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsubnetact.so")
+SERVING = os.path.join(HERE, "_serving.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -39,9 +40,28 @@ def build_library(verbose: bool = True) -> str:
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
+    _serving_binding()
     if verbose:
         print(f"built {LIB}")
     return LIB
+
+
+def _serving_binding():
+    """The serving operators' Python binding (host code only) against the installed torch."""
+    import sysconfig
+
+    from torch.utils.cpp_extension import include_paths, library_paths
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    inc = [*include_paths(), os.path.join(rocm, "include"), sysconfig.get_paths()["include"]]
+    lib = [d for p in (*library_paths(), os.path.join(rocm, "lib")) for d in ("-L" + p, "-Wl,-rpath," + p)]
+    r = subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+                        *[x for p in inc for x in ("-isystem", p)], os.path.join(CSRC, "serving_py.cpp"), "-o", SERVING,
+                        "-L" + HERE, "-l:libsubnetact.so", "-Wl,-rpath,$ORIGIN", *lib, "-lc10", "-lc10_hip", "-ltorch", "-ltorch_cpu", "-ltorch_python", "-lamdhip64"],
+                       capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("serving binding failed:\n" + r.stderr)
+    if r.stderr.strip():
+        sys.stderr.write(r.stderr)
 
 
 if __name__ == "__main__":

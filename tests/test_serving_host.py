@@ -92,25 +92,34 @@ def test_tensors_are_refused():
         sna.PagedBatch(n, n[:2], torch.zeros(2, 4, dtype=torch.int32), 1, 1)                        # not on a GPU
 
 
-class _Cpu:                                                            # what validate() looks at
-    page_size, n_pages = 16, 9
-
-
 def test_validate_finds_what_does_not_fit():
-    def of(starts, lens, table, max_new=4, max_len=64):
-        b = serving.PagedBatch.__new__(serving.PagedBatch)
-        b.starts, b.lens, b.page_table = (torch.tensor(x, dtype=torch.int32) for x in (starts, lens, table))
-        b.max_new, b.max_len = max_new, max_len
-        return b
+    def of(starts, lens, table, n_tokens=5, max_new=4, max_len=64):
+        serving._validate(*(torch.tensor(x, dtype=torch.int32) for x in (starts, lens, table)), max_new, max_len, 16, 9, n_tokens)
 
     good = dict(starts=[0, 1, 1, 5], lens=[17, 0, 33], table=[[0, 8, -1, -1], [-1] * 4, [3, 4, 5, 99]])
-    of(**good).validate(_Cpu, 5)
+    of(**good)
     for bad in (dict(starts=[1, 1, 1, 5]), dict(starts=[0, 2, 1, 5]), dict(starts=[0, 1, 1, 4]), dict(lens=[17, 0, 65]), dict(lens=[17, 0, 3]), dict(lens=[17, 16, 33]),
                 dict(table=[[0, 9, -1, -1], [-1] * 4, [3, 4, 5, 99]]), dict(max_new=3), dict(max_len=32), dict(lens=[17, 0, 49])):
         with pytest.raises(ValueError):
-            of(**{**good, **bad}).validate(_Cpu, 5)
+            of(**{**good, **bad})
     with pytest.raises(ValueError):
-        of([0, 1], [65], [[1, 2, 3, 4]], max_len=99).validate(_Cpu, 1)
+        of([0, 1], [65], [[1, 2, 3, 4]], n_tokens=1, max_len=99)
+
+
+def test_calls_are_refused():
+    for call, args in ((sna.kv_append, 5), (sna.paged_attention, 3), (sna.verify_draft, 3)):
+        with pytest.raises(TypeError):
+            call(*[None] * (args - 1))
+        with pytest.raises(TypeError):
+            call(*[None] * args, nonsense=1)
+        with pytest.raises(TypeError):
+            call(*[None] * 13)
+    with pytest.raises(TypeError):
+        sna.kv_append(None, None, None, None, None)
+    with pytest.raises(TypeError):
+        sna.paged_attention(1, 2, 3, cache=1)
+    with pytest.raises(ValueError):
+        sna.verify_draft(None, None, None)
 
 
 def verify(target=AT, draft=None, tokens=AT, token_bytes=4, uniforms=AT, counts=None, n=2, k=3, v=100, out=AT, accepted=AT, stride=400):
