@@ -282,13 +282,14 @@ __device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) 
 // (tile of rows, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what
 // a later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
 struct First { int b, i0, h, last; };
+__host__ __device__ constexpr long part_floats(long rows, int D) { return (rows * (D + 2) + 3) & ~3l; }    // 16-byte aligned
 template <class T, int D, int MB>
 __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
   __shared__ JoinLds<D, MB> lds;
   const int p = blockIdx.x, lane = threadIdx.x & 63, heads = a.kv.heads;
   First* first = (First*)a.parts;
   float* parts = (float*)(first + gridDim.x);
-  const long part_size = (long)a.rows_cap * (D + 2);
+  const long part_size = part_floats(a.rows_cap, D);
   // this share's first sequence: every wave sums the tiles of all, 64 runs of sequences at a time
   int lo = 0, count = a.s.B;
   long before = 0, share = 0, x = 0;
@@ -360,54 +361,68 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
   if (!begun && threadIdx.x == 0) first[p].b = -1;
 }
 
-// Parts joined: a block for each (sequence, head) that was cut, and up to JN_R rows of it
-constexpr int JN_R = 4;
+// Parts joined: JN_Y blocks for each (tile of rows, head) that was cut.  A thread has four dims of a row; the 256 / (D / 4)
+// groups of a row's threads take that many rows at a time where the parts are few, or share a row's parts where they are many.
+// Sums, maximum and statistics of a part are asked for together: with the statistics first, a row of 64 parts took 5 us.
+constexpr int JN_Y = 8;
 template <class T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a, int blocks) {
-  constexpr int W = D / 4, NP = 256 / W;                             // threads of a row; parts at a time
-  __shared__ float weight[1024], red[4];
-  __shared__ __attribute__((aligned(16))) float so[NP][D + 4];
-  __shared__ float ssum[NP];
-  const int p = blockIdx.x, tid = threadIdx.x;
+  constexpr int W = D / 4, N = 256 / W, U = 4;                       // threads of a row; groups; parts under way
+  __shared__ __attribute__((aligned(16))) float so[N][D];
+  __shared__ float2 ss[N];
+  const int p = blockIdx.x, g = threadIdx.x / W, d = threadIdx.x % W * 4;
   const First f = ((const First*)a.parts)[p];
   if (f.b < 0) return;
   const RowTile r = rows_of_sequence(a, sequence(a.s, f.b), f.b, f.i0, a.tpt);
-  const float* parts = (const float*)((const First*)a.parts + blocks);
-  const long part_size = (long)a.rows_cap * (D + 2);
-  const int n = min(f.last - p + 1, 1024), rows = r.n * a.G;
-  const auto part = [&](int j) { return parts + (2 * (p + j) + (j == 0)) * part_size; };
-  for (int row = blockIdx.y * JN_R; row < min(rows, (int)blockIdx.y * JN_R + JN_R); ++row) {
-    float top = -INFINITY;
-    for (int j = tid; j < n; j += 256) top = fmaxf(top, weight[j] = part(j)[a.rows_cap * D + 2 * row]);
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-    if ((tid & 63) == 0) red[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    if (top == -INFINITY) top = 0.f;
+  const int n = f.last - p + 1, rows = r.n * a.G;
+  int share = 1;                                                     // groups that share a row
+  while (share < N && n > U * share) share *= 2;
+  const int at_once = N / share;
+  const long part_size = part_floats(a.rows_cap, D);
+  const float* parts = (const float*)((const First*)a.parts + blocks) + (2 * p + 1) * part_size;       // part 0; part j > 0 lies 2 j - 1 further on
+  for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {       // the same turns for the block
+    const int row = row0 + g / share, row_in = min(row, rows - 1);
+    float top = -INFINITY, sum = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    const int g = tid / W, d = tid % W * 4;
-    for (int j = g; j < n; j += NP) {
-      const float w = __builtin_amdgcn_exp2f(weight[j] - top);
-      const float* y = part(j);
-      x += *(const f32x4*)(y + row * D + d) * w;
-      sum += y[a.rows_cap * D + 2 * row + 1] * w;
-    }
-    *(f32x4*)&so[g][d] = x;
-    if (tid % W == 0) ssum[g] = sum;
-    __syncthreads();
-    if (tid < W) {
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      float s = 0.f;
+    for (int j0 = g % share; j0 < n; j0 += share * U) {
+      f32x4 y[U];
+      float2 st[U];
 #pragma unroll
-      for (int i = 0; i < NP; ++i) { o += *(const f32x4*)&so[i][d]; s += ssum[i]; }
-      o *= s == 0.f ? 0.f : 1.f / s;
-      const int i = row / a.G;
-      typedef __attribute__((ext_vector_type(4))) unsigned short u16x4;
-      *(u16x4*)(a.o + (r.row0 + i) * a.o_t + (f.h * a.G + row - i * a.G) * a.o_h + d * 2) = __builtin_bit_cast(u16x4, __builtin_convertvector(o, typename T::v4));
+      for (int u = 0; u < U; ++u) {
+        const int j = min(j0 + u * share, n - 1);
+        const float* q = parts + max(2 * j - 1, 0) * part_size;
+        y[u] = *(const f32x4*)(q + row_in * D + d);
+        st[u] = *(const float2*)(q + a.rows_cap * D + 2 * row_in);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (j0 + u * share < n) {
+          const float now = fmaxf(top, st[u].x), ref = now == -INFINITY ? 0.f : now;
+          const float keep = __builtin_amdgcn_exp2f(top - ref), w = __builtin_amdgcn_exp2f(st[u].x - ref);
+          x = x * keep + y[u] * w;
+          sum = sum * keep + st[u].y * w;
+          top = now;
+        }
     }
-    __syncthreads();
+    if (share > 1) {                                                 // the same for the block
+      __syncthreads();
+      *(f32x4*)&so[g][d] = x;
+      if (d == 0) ss[g] = make_float2(top, sum);
+      __syncthreads();
+      if (g % share) continue;
+      for (int i = 1; i < share; ++i) {
+        const float2 st = ss[g + i];
+        const float now = fmaxf(top, st.x), ref = now == -INFINITY ? 0.f : now;
+        const float keep = __builtin_amdgcn_exp2f(top - ref), w = __builtin_amdgcn_exp2f(st.x - ref);
+        x = x * keep + *(const f32x4*)&so[g + i][d] * w;
+        sum = sum * keep + st.y * w;
+        top = now;
+      }
+    }
+    if (row >= rows) continue;
+    x *= sum == 0.f ? 0.f : 1.f / sum;
+    const int i = row / a.G;
+    *(uint2*)(a.o + (r.row0 + i) * a.o_t + (f.h * a.G + row - i * a.G) * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
   }
 }
 
@@ -422,7 +437,7 @@ static void rows_grid(PagedAttnArgs a, hipStream_t s) {
     a.rows_cap = a.tpt * a.G;
     a.least = kSplitLeast;
     hipLaunchKernelGGL((paged_split_kernel<T, D, MB>), dim3(blocks), dim3(64 * PA_W), 0, s, a);
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(blocks, (a.rows_cap + JN_R - 1) / JN_R), dim3(256), 0, s, a, blocks);
+    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a, blocks);
     return;
   }
   a.by_tpt = FastDiv::by(a.tpt);
@@ -436,8 +451,13 @@ static void rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
   else rows_grid<T, D, 4>(a, s);
 }
 static size_t parts_bytes(int head_dim, int mb, long rows_cap) {
-  return 256 * blocks_of(head_dim, mb) * (sizeof(First) + 2 * rows_cap * (head_dim + 2) * sizeof(float));
+  return 256 * blocks_of(head_dim, mb) * (sizeof(First) + 2 * part_floats(rows_cap, head_dim) * sizeof(float));
 }
+
+// Blocks of whole (tile of rows, head)s walk the longest sequence in turns of a tile for each wave, as many times over as the chip
+// has to be filled; shared out, the keys take the mean instead, but their parts are written and joined in a second launch.
+// Sequences are taken to be 0.6 of the longest on average.
+constexpr long kSplitGain = 6;     // turns that sharing has to save
 
 // How a step is launched, from what the host knows of it.
 struct AttnPlan {
@@ -453,8 +473,9 @@ static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
   AttnPlan p = {};
   if (rows <= 64 || (long)n_tokens * group * kv_heads <= kFewRows) {
     p.mb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.split = keys > 1024;
     p.most = max_new;
+    const long units = (n_tokens / std::max(16 * p.mb / group, 1) + n_seqs) * (long)kv_heads, room = 256 * blocks_of(head_dim, p.mb), turns = (keys + PA_W * PA_K - 1) / (PA_W * PA_K);
+    p.split = (units + room - 1) / room * turns - units * turns * 6 / (10 * room) > kSplitGain;
   } else {
     p.chunks = true;
     p.splits = paged_chunk_splits(n_tokens, kv_heads, group, max_new, keys);

@@ -12,6 +12,7 @@
 namespace sna {
 
 constexpr int VD_W = 16;           // waves of a block
+constexpr int VD_S = 8;            // values of a lane, where one wave looks for the draw
 
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
@@ -28,49 +29,166 @@ __device__ __forceinline__ double wave_scan(double v) {              // inclusiv
   return v;
 }
 
-struct Weights {                   // of one sequence's draw
-  const float* p; const float* q;  // q: nullptr where the draft's token alone is taken out, or nothing
-  int out;                         // that token, or -1
-  __device__ __forceinline__ double of(int x, float px, float qx) const {
-    double w = q ? (double)px - (double)qx : (double)px;
-    if (x == out) w = 0.0;
-    return w > 0.0 ? w : 0.0;                                        // NaN counts as nothing
-  }
-};
 typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4u;  // rows of odd vocabularies start anywhere
 
-// Sum over [x0, x1) by one wave
+// The weights of one sequence's draw: a row of the target, less a row of the draft, or less one token, or all of it
+enum Less { LESS_NOTHING, LESS_ROW, LESS_TOKEN };
+struct Weights {
+  const float* p; const float* q;
+  int out;                         // the token taken out
+};
+template <Less L>
+__device__ __forceinline__ double weight(const Weights& w, int x, float p, float q) {
+  if (L == LESS_ROW) return fmax((double)p - (double)q, 0.0);        // NaN counts as nothing
+  return L == LESS_TOKEN && x == w.out ? 0.0 : fmax((double)p, 0.0);
+}
+
+// Sum over [x0, x1) by one wave.  A wave asks for VD_U kilobytes of either row before it waits: with one at a time it waited
+// out a round trip to memory for each.
+constexpr int VD_U = 4;
+template <Less L>
 __device__ __forceinline__ double run_sum(const Weights& w, int x0, int x1) {
   const int lane = threadIdx.x & 63;
-  double s = 0.0;
+  double s[VD_U] = {};
   int x = x0 + 4 * lane;
-  for (; x + 3 < x1; x += 256) {
-    const f32x4u p = *(const f32x4u*)(w.p + x), q = w.q ? *(const f32x4u*)(w.q + x) : f32x4u{0.f, 0.f, 0.f, 0.f};
+  for (; x + 256 * (VD_U - 1) + 3 < x1; x += 256 * VD_U) {
+    f32x4u p[VD_U], q[VD_U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s += w.of(x + e, p[e], q[e]);
+    for (int i = 0; i < VD_U; ++i) {
+      p[i] = *(const f32x4u*)(w.p + x + 256 * i);
+      if (L == LESS_ROW) q[i] = *(const f32x4u*)(w.q + x + 256 * i);
+    }
+#pragma unroll
+    for (int i = 0; i < VD_U; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i] += weight<L>(w, x + 256 * i + e, p[i][e], L == LESS_ROW ? q[i][e] : 0.f);
   }
-  for (; x < x1; ++x) s += w.of(x, w.p[x], w.q ? w.q[x] : 0.f);       // one lane's, up to three
-  return wave_sum(s);
+  // what is left: less than VD_U fours a lane, the last of one lane partial
+  f32x4u p[VD_U], q[VD_U];
+#pragma unroll
+  for (int i = 0; i < VD_U; ++i)
+    if (x + 256 * i + 3 < x1) {
+      p[i] = *(const f32x4u*)(w.p + x + 256 * i);
+      if (L == LESS_ROW) q[i] = *(const f32x4u*)(w.q + x + 256 * i);
+    }
+#pragma unroll
+  for (int i = 0; i < VD_U; ++i) {
+    const int y = x + 256 * i;
+    if (y + 3 < x1) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i] += weight<L>(w, y + e, p[i][e], L == LESS_ROW ? q[i][e] : 0.f);
+    } else {
+      for (int z = y; z < x1; ++z) s[i] += weight<L>(w, z, w.p[z], L == LESS_ROW ? w.q[z] : 0.f);
+    }
+  }
+  double t = 0.0;
+#pragma unroll
+  for (int i = 0; i < VD_U; ++i) t += s[i];
+  return wave_sum(t);
+}
+
+// The run that a draw of `at` falls into, of VD_W with the given sums, `up` before the first of them: the first whose end lies
+// beyond it, or the last with any weight where rounding leaves none.  `up` becomes what lies before that run.
+__device__ __forceinline__ int run_of(const double* sums, double at, double& up) {
+  int r = 0;
+  bool found = false;
+  double end = up;
+#pragma unroll
+  for (int i = 0; i < VD_W; ++i) {
+    const double v = sums[i];
+    if (!found && v > 0.0) { r = i; up = end; }
+    end += v;
+    found = found || end > at;
+  }
+  return uniform(r);
+}
+
+// The token that a draw with u falls on; -1 in `token` and a total of zero where there is nothing to draw from.  All waves.
+template <Less L>
+__device__ __forceinline__ double draw(const Weights& w, int V, double u, double* sums, int& token) {
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+  const int len1 = (((V + VD_W - 1) / VD_W) + 3) & ~3;               // values of a wave's run
+  {
+    const int x0 = min(V, wave * len1);
+    const double s = run_sum<L>(w, x0, min(V, x0 + len1));
+    if (lane == 0) sums[wave] = s;
+  }
+  __syncthreads();
+  double total = 0.0, before = 0.0;
+#pragma unroll
+  for (int i = 0; i < VD_W; ++i) total += sums[i];
+  if (!(total > 0.0)) return 0.0;
+  const double at = u * total;
+  int r = run_of(sums, at, before), s0 = min(V, r * len1), s1 = min(V, s0 + len1);
+  if (len1 > 64 * VD_S) {                                            // too long for one wave's registers
+    const int len2 = (((s1 - s0 + VD_W - 1) / VD_W) + 3) & ~3, x0 = min(s1, s0 + wave * len2);
+    const double s = run_sum<L>(w, x0, min(s1, x0 + len2));
+    if (lane == 0) sums[VD_W + wave] = s;
+    __syncthreads();
+    r = run_of(sums + VD_W, at, before);
+    s0 = min(s1, s0 + r * len2);
+    s1 = min(s1, s0 + len2);
+  }
+  if (wave != 0) return total;
+  // VD_S values a lane at a time, in order (two turns and more for vocabularies of 131072 and more)
+  for (int base = s0; base < s1; base += 64 * VD_S) {
+    double v[VD_S], mine = 0.0;
+    const int z0 = base + lane * VD_S;
+    float p[VD_S], q[VD_S];
+#pragma unroll
+    for (int i = 0; i < VD_S; ++i)
+      if (z0 + i < s1) {
+        p[i] = w.p[z0 + i];
+        if (L == LESS_ROW) q[i] = w.q[z0 + i];
+      }
+#pragma unroll
+    for (int i = 0; i < VD_S; ++i) {
+      v[i] = z0 + i < s1 ? weight<L>(w, z0 + i, p[i], L == LESS_ROW ? q[i] : 0.f) : 0.0;
+      mine += v[i];
+    }
+    const double up = wave_scan(mine);
+    double c = before + up - mine;
+    int hit = -1, any = -1;
+#pragma unroll
+    for (int i = 0; i < VD_S; ++i) {
+      c += v[i];
+      if (v[i] > 0.0) {
+        any = z0 + i;
+        if (hit < 0 && c > at) hit = z0 + i;
+      }
+    }
+    const unsigned long long hits = __ballot(hit >= 0), anys = __ballot(any >= 0);
+    if (hits) {
+      token = __shfl(hit, __ffsll((long long)hits) - 1, 64);
+      break;
+    }
+    if (anys) token = __shfl(any, 63 - __clzll((long long)anys), 64);
+    before += __shfl(up, 63, 64);
+  }
+  return total;
 }
 
 template <class Tok>
 __global__ __launch_bounds__(64 * VD_W) void verify_kernel(const VerifyArgs a) {
-  __shared__ double sums[VD_W];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), K = a.K, V = a.V;
+  __shared__ double sums[2 * VD_W];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), K = a.K, V = a.V;
   const Tok* tokens = (const Tok*)a.tokens + (long)b * K;
   const float* u = a.uniforms + (long)b * (K + 1);
+  const double u_draw = fmin(fmax((double)u[K], 0.0), 1.0);
+  // the first draft that is not taken: every wave finds it for itself, 64 at a time; a place beyond the sequence's drafts is
+  // looked at, too, so that its loads need not wait for their number
   const int count = a.counts ? clamped(a.counts[b], 0, K) : K;
-  // the first draft that is not taken: every wave finds it for itself, 64 at a time
   int acc = 0;
-  for (int i0 = 0; i0 < count; i0 += 64) {
+  for (int i0 = 0; i0 < K; i0 += 64) {
     const int i = i0 + lane;
     bool taken = false;
-    if (i < count) {
+    if (i < K) {
+      const float ui = u[i];
       const long x = (long)tokens[i];
       if (x >= 0 && x < V) {
         const double p = a.target[b * a.t_seq + i * a.t_row + x];
         const double q = a.draft ? a.draft[b * a.d_seq + i * a.d_row + x] : 1.f;
-        taken = (double)u[i] * q < p;
+        taken = (double)ui * q < p;
       }
     }
     const unsigned long long no = ~__ballot(taken);
@@ -78,83 +196,22 @@ __global__ __launch_bounds__(64 * VD_W) void verify_kernel(const VerifyArgs a) {
     acc = i0 + run;
     if (run < 64) break;
   }
-  acc = __builtin_amdgcn_readfirstlane(min(acc, count));
+  acc = uniform(min(acc, count));
   Weights w = {a.target + b * a.t_seq + acc * a.t_row, nullptr, -1};
+  int token = -1;
+  double total = 0.0;
   if (acc < count) {
-    if (a.draft) w.q = a.draft + b * a.d_seq + acc * a.d_row;
-    else {
+    if (a.draft) {
+      w.q = a.draft + b * a.d_seq + acc * a.d_row;
+      total = draw<LESS_ROW>(w, V, u_draw, sums, token);
+    } else {
       const long x = (long)tokens[acc];
       w.out = x >= 0 && x < V ? (int)x : -1;
+      total = draw<LESS_TOKEN>(w, V, u_draw, sums, token);
     }
-  }
-  double total = 0.0, before = 0.0, run0[VD_W];
-  const int len1 = (((V + VD_W - 1) / VD_W) + 3) & ~3;               // values of a wave's run
-  for (int turn = 0; turn < 2; ++turn) {
-    const int x0 = min(V, wave * len1), x1 = min(V, x0 + len1);
-    const double s = run_sum(w, x0, x1);
-    if (turn) __syncthreads();
-    if (lane == 0) sums[wave] = s;
     __syncthreads();
-    total = 0.0;
-#pragma unroll
-    for (int i = 0; i < VD_W; ++i) {
-      run0[i] = sums[i];
-      total += run0[i];
-    }
-    if (total > 0.0 || (!w.q && w.out < 0)) break;
-    w.q = nullptr;                                                   // nothing left of the difference: the target's row itself
-    w.out = -1;
   }
-  int token = -1;
-  if (total > 0.0) {
-    const double at = fmin(fmax((double)u[K], 0.0), 1.0) * total;
-    // the first run whose end lies beyond the draw; the last with any weight where rounding leaves none
-    int r1 = 0;
-    bool found = false;
-    double up = 0.0;
-#pragma unroll
-    for (int i = 0; i < VD_W; ++i) {
-      if (!found && run0[i] > 0.0) { r1 = i; before = up; }
-      up += run0[i];
-      found = found || up > at;
-    }
-    const int s0 = min(V, r1 * len1), s1 = min(V, s0 + len1), len2 = (((s1 - s0 + VD_W - 1) / VD_W) + 3) & ~3;
-    const int x0 = min(s1, s0 + wave * len2), x1 = min(s1, x0 + len2);
-    const double s = run_sum(w, x0, x1);
-    __syncthreads();
-    if (lane == 0) sums[wave] = s;
-    __syncthreads();
-    if (wave == 0) {
-      int r2 = 0;
-      found = false;
-      up = before;
-#pragma unroll
-      for (int i = 0; i < VD_W; ++i) {
-        const double v = sums[i];
-        if (!found && v > 0.0) { r2 = i; before = up; }
-        up += v;
-        found = found || up > at;
-      }
-      // that run: a stretch of it a lane
-      const int y0 = min(s1, s0 + r2 * len2), y1 = min(s1, y0 + len2), len3 = (y1 - y0 + 63) / 64;
-      const int z0 = min(y1, y0 + lane * len3), z1 = min(y1, z0 + len3);
-      double mine = 0.0;
-      for (int x = z0; x < z1; ++x) mine += w.of(x, w.p[x], w.q ? w.q[x] : 0.f);
-      double c = before + wave_scan(mine) - mine;
-      int hit = -1, any = -1;
-      for (int x = z0; x < z1; ++x) {
-        const double v = w.of(x, w.p[x], w.q ? w.q[x] : 0.f);
-        c += v;
-        if (v > 0.0) {
-          any = x;
-          if (hit < 0 && c > at) hit = x;
-        }
-      }
-      const unsigned long long hits = __ballot(hit >= 0), anys = __ballot(any >= 0);
-      if (hits) token = __shfl(hit, __ffsll((long long)hits) - 1, 64);
-      else if (anys) token = __shfl(any, 63 - __clzll((long long)anys), 64);
-    }
-  }
+  if (!(total > 0.0)) draw<LESS_NOTHING>(w, V, u_draw, sums, token);  // all taken, or nothing left: the target's row itself
   if (wave == 0) {
     for (int i = lane; i <= K; i += 64) a.out[(long)b * (K + 1) + i] = i < acc ? (int)tokens[i] : i == acc ? token : -1;
     if (lane == 0) a.accepted[b] = acc;
