@@ -1,54 +1,84 @@
 // New tokens enter the paged cache: per-head RMS norm and position rotation of q and k, k and v into their pages.
 //   x' = x * rsqrt(mean(x^2) + eps) * w            (with a norm)
 //   (x'_a, x'_b) -> (x'_a cos - x'_b sin, x'_a sin + x'_b cos),   angle = position * inv_freq[pair]
-// Bound by memory: every element is read once and written once.  A block takes up to 16 tokens that share 16 aligned slots of
-// a page, for some heads of q, k or v: then v, which the cache keeps transposed, leaves as whole runs of 16 slots (32 bytes,
-// all of a page of 16), and an angle is evaluated once a block instead of once a head.  It is formed in 64 bits, in turns,
-// and only its fraction goes on in 32: at position 10^5 a 32-bit product would be off by 6e-3 radians.
+// Bound by memory: every element is read once and written once (13551 tokens of 32 + 8 + 8 heads of 128: 69.6 us, 4.8 TB/s,
+// what a large copy reaches).  A block takes the new tokens of 16 aligned slots of a page and some heads of q or k, so that an
+// angle is evaluated once a block instead of once a head, or of 64 slots and some heads of v: the cache keeps v transposed, and
+// 64 slots are a line of 128 bytes (runs of 16 slots, written by four blocks, made it 85 to 97 us).  Two rows' loads a thread
+// are under way: four took the registers of the fifth wave of a SIMD (85 us).  An angle is formed in 64 bits, in turns, and
+// only its fraction goes on in 32: at position 10^5 a 32-bit product would be off by 6e-3 radians.
 #include "paged.h"
 
 namespace sna {
 
-constexpr int AP_TOK = 16;         // aligned slots of a block: the smallest page
-constexpr int AP_IT = 4;           // loads of 32 bytes (q, k) or 16 (v) that a thread has under way
+constexpr int AP_TOK = 16;         // aligned slots of a block of q or k: the smallest page
+constexpr int AP_VT = 64;          // of v: 128 bytes of a row of the transposed page, a whole line of the cache
+constexpr int AP_IT = 4;           // pieces of 32 bytes (q, k) or 16 (v) a thread
 
-// Tiles of the sequences before b, or more: sequence b's new tokens touch at most (n + 14) / 16 + 1 runs of 16 slots.
-__device__ __forceinline__ int append_tile0(const PagedSeqs& s, int b) { return (clamped(s.starts[b], 0, s.T) >> 4) + 2 * b; }
+// Tiles of the sequences before b, or more: n new tokens touch at most (n + TOK - 2) / TOK + 1 runs of TOK slots
+template <int TOK>
+__device__ __forceinline__ int append_tile0(const PagedSeqs& s, int b) { return clamped(s.starts[b], 0, s.T) / TOK + 2 * b; }
+// The new tokens of one of those runs
+struct Run { int b, row0, first, cnt, off; };    // sequence, first row, its position, tokens, slots before it in the run
+template <int TOK>
+__device__ __forceinline__ Run append_run(const AppendArgs& a, int tile) {
+  Run r;
+  if (a.one) return Run{tile, tile, clamped(a.s.lens[tile], 0, 1 << 30) - 1, 1, 0};
+  r.b = last_at_most(a.s.B, tile, [&](int i) { return append_tile0<TOK>(a.s, i); });
+  const Seq q = uniform(sequence(a.s, r.b));
+  const int p0 = q.len - q.n, base = (p0 & ~(TOK - 1)) + (tile - append_tile0<TOK>(a.s, r.b)) * TOK;
+  r.first = max(p0, base);
+  r.cnt = min(q.len, base + TOK) - r.first;
+  r.row0 = q.row0 + r.first - p0;
+  r.off = r.first - base;
+  return r;
+}
+__device__ __forceinline__ int page_of(const AppendArgs& a, int b, int pos) {            // -1: none of the pool's
+  const int col = pos >> a.kv.lps;
+  const int page = pos >= 0 && col < a.s.width ? a.s.table[(long)b * a.s.tstride + col] : -1;
+  return page < a.kv.n_pages ? page : -1;
+}
 
+// Values: VT aligned slots of VH heads, through LDS
 template <class T, int D>
-__device__ __forceinline__ void append_v(const AppendArgs& a, int part, int row0, int cnt, int off, char* page, int slot, char* lds) {
-  constexpr int O = D / 8, LD = D + 8;                               // octets of a head, LDS row
-  const int nt = blockDim.x, tid = threadIdx.x, ps2 = 2 << a.kv.lps;
+__device__ __forceinline__ void append_v(const AppendArgs& a, int tile, int part, char* lds) {
+  constexpr int O = D / 8, LD = D + 8, VH = AP_IT * 256 / (O * AP_VT);     // octets of a head, LDS row; heads of a block
+  const int tid = threadIdx.x, ps2 = 2 << a.kv.lps, mask = (1 << a.kv.lps) - 1;
+  const Run r = append_run<AP_VT>(a, tile);
   if (a.one) {
-    const int u = part * 64 + tid, h = u / O, o = u % O;
-    if (h >= a.kv.heads) return;
-    const u32x4 x = *(const u32x4*)(a.v + row0 * a.v_t + h * a.v_h + o * 16);
-    char* y = page + ((long)(h * D + o * 8) * ps2) + 2 * slot;
+    const int page = page_of(a, r.b, r.first), u = part * 64 + tid, h = u / O, o = u % O;
+    if (h >= a.kv.heads || page < 0) return;
+    const u32x4 x = *(const u32x4*)(a.v + r.row0 * a.v_t + h * a.v_h + o * 16);
+    char* y = a.kv.v + page * a.kv.vstride + ((long)(h * D + o * 8) * ps2) + 2 * (r.first & mask);
 #pragma unroll
     for (int e = 0; e < 8; ++e) *(unsigned short*)(y + e * ps2) = (unsigned short)(x[e >> 1] >> (16 * (e & 1)));
     return;
   }
-  constexpr int VH = AP_IT * 256 / (O * AP_TOK);                     // heads of a block
+  if (r.cnt <= 0) return;
   const int h0 = part * VH;
   u32x4 x[AP_IT];
 #pragma unroll
   for (int i = 0; i < AP_IT; ++i) {
-    const int u = i * nt + tid, tok = (u / O) % AP_TOK, h = h0 + u / (O * AP_TOK);
-    if (tok < cnt && h < a.kv.heads) x[i] = *(const u32x4*)(a.v + (row0 + tok) * a.v_t + h * a.v_h + (u % O) * 16);
+    const int u = i * 256 + tid, tok = min((u / O) % AP_VT, r.cnt - 1), h = min(h0 + u / (O * AP_VT), a.kv.heads - 1);
+    x[i] = *(const u32x4*)(a.v + (r.row0 + tok) * a.v_t + h * a.v_h + (u % O) * 16);
   }
+  // a thread writes runs of 8 slots: so-th of the tile, the same for all of its runs
+  constexpr int SO = AP_VT / 8;
+  const int so = tid % SO, first = r.first - r.off + 8 * so, page = page_of(a, r.b, first);
 #pragma unroll
   for (int i = 0; i < AP_IT; ++i) {
-    const int u = i * nt + tid, tok = (u / O) % AP_TOK, h = u / (O * AP_TOK);
-    if (tok < cnt && h0 + h < a.kv.heads) *(u32x4*)(lds + ((h * AP_TOK + tok + off) * LD + (u % O) * 8) * 2) = x[i];
+    const int u = i * 256 + tid, tok = (u / O) % AP_VT, h = u / (O * AP_VT);
+    if (tok < r.cnt && h0 + h < a.kv.heads) *(u32x4*)(lds + ((h * AP_VT + tok + r.off) * LD + (u % O) * 8) * 2) = x[i];
   }
   __syncthreads();
+  if (page < 0) return;
 #pragma unroll
   for (int i = 0; i < AP_IT; ++i) {
-    const int u = i * nt + tid, so = u & 1, d = (u >> 1) % D, h = (u >> 1) / D;
+    const int u = i * 256 + tid, d = (u / SO) % D, h = u / SO / D;
     if (h0 + h >= a.kv.heads) continue;
-    const unsigned short* col = (const unsigned short*)lds + (h * AP_TOK + 8 * so) * LD + d;
-    char* y = page + (long)((h0 + h) * D + d) * ps2 + 2 * (slot - off + 8 * so);
-    if (off <= 8 * so && off + cnt >= 8 * so + 8) {
+    const unsigned short* col = (const unsigned short*)lds + (h * AP_VT + 8 * so) * LD + d;
+    char* y = a.kv.v + page * a.kv.vstride + (long)((h0 + h) * D + d) * ps2 + 2 * (first & mask);
+    if (r.off <= 8 * so && r.off + r.cnt >= 8 * so + 8) {
       u32x4 w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = col[2 * e * LD] | (unsigned)col[(2 * e + 1) * LD] << 16;
@@ -56,7 +86,7 @@ __device__ __forceinline__ void append_v(const AppendArgs& a, int part, int row0
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (8 * so + e >= off && 8 * so + e < off + cnt) *(unsigned short*)(y + 2 * e) = col[e * LD];
+        if (8 * so + e >= r.off && 8 * so + e < r.off + r.cnt) *(unsigned short*)(y + 2 * e) = col[e * LD];
     }
   }
 }
@@ -72,17 +102,16 @@ __device__ __forceinline__ void append_qk(const AppendArgs& a, const bool is_k, 
   const unsigned inv = 65536u / nh + 1;                              // r / nh for r * nh < 65536
   const char* src = is_k ? a.k : a.q;
   const long st = is_k ? a.k_t : a.q_t, sh = is_k ? a.k_h : a.q_h;
-  u32x4 u[AP_IT][2];
-#pragma unroll
-  for (int i = 0; i < AP_IT; ++i) {
-    const int r = (i * nt + tid) / L;
-    if (r < rows) {
-      const int tok = (r * inv) >> 16, h = h0 + r - tok * nh;
-      const char* x = src + (row0 + tok) * st + h * sh;
-      u[i][0] = *(const u32x4*)(x + oa * 16);
-      u[i][1] = *(const u32x4*)(x + ob * 16);
-    }
-  }
+  // rows beyond the last read it again: a guarded load would be waited for before the next guard
+  u32x4 u[2][2];
+  const auto load = [&](int i) {
+    const int r = min((i * nt + tid) / L, rows - 1), tok = (r * inv) >> 16, h = h0 + r - tok * nh;
+    const char* x = src + (row0 + tok) * st + h * sh;
+    u[i & 1][0] = *(const u32x4*)(x + oa * 16);
+    u[i & 1][1] = *(const u32x4*)(x + ob * 16);
+  };
+  load(0);
+  if (nt / L < rows) load(1);
   f32x8 w[2];
   if (NORM) {
     const float* g = is_k ? a.k_norm : a.q_norm;
@@ -101,9 +130,10 @@ __device__ __forceinline__ void append_qk(const AppendArgs& a, const bool is_k, 
 #pragma unroll
   for (int i = 0; i < AP_IT; ++i) {
     const int r = (i * nt + tid) / L;
+    f32x8 x = to_f32<T>(u[i & 1][0]), y = to_f32<T>(u[i & 1][1]);
+    if (i + 2 < AP_IT && (i + 2) * nt / L < rows) load(i + 2);
     if (r >= rows) continue;                                         // the same for a row's lanes
     const int tok = (r * inv) >> 16, h = h0 + r - tok * nh;
-    f32x8 x = to_f32<T>(u[i][0]), y = to_f32<T>(u[i][1]);
     if (NORM) {
       float ss = 0.f;
 #pragma unroll
@@ -153,50 +183,34 @@ __device__ __forceinline__ void append_qk(const AppendArgs& a, const bool is_k, 
   }
 }
 
-// Grid: runs of 16 slots x (parts of q's heads, of k's, of v's).  A step of single tokens, where only latency counts, gets a
-// wave for each token and part instead.
+// Blocks: (runs of AP_TOK slots) x (parts of q's heads, of k's), then (runs of AP_VT) x (parts of v's).  A step of single tokens,
+// where only latency counts, gets a wave for each token and part instead.
 template <class T, int D, bool NORM>
 __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
-  constexpr int L = D / 16, HP = AP_IT * 256 / (L * AP_TOK), VH = AP_IT * 256 / (D / 8 * AP_TOK);
-  __shared__ __attribute__((aligned(16))) char lds[VH * AP_TOK * (D + 8) * 2];
+  constexpr int L = D / 16, HP = AP_IT * 256 / (L * AP_TOK), VH = AP_IT * 256 / (D / 8 * AP_VT);
+  __shared__ __attribute__((aligned(16))) char lds[VH * AP_VT * (D + 8) * 2];
   static_assert(sizeof(lds) >= AP_TOK * D / 2 * sizeof(float2), "the angles of 16 tokens");
-  int b, row0, first, cnt, off;
-  if (a.one) {
-    b = blockIdx.x;
-    row0 = b;
-    first = clamped(a.s.lens[b], 0, 1 << 30) - 1;
-    cnt = 1;
-    off = 0;
-  } else {
-    const int tile = blockIdx.x;
-    b = last_at_most(a.s.B, tile, [&](int i) { return append_tile0(a.s, i); });
-    const Seq q = sequence(a.s, b);
-    const int p0 = q.len - q.n, base = (p0 & ~(AP_TOK - 1)) + (tile - append_tile0(a.s, b)) * AP_TOK;
-    first = max(p0, base);
-    cnt = min(q.len, base + AP_TOK) - first;
-    if (cnt <= 0) return;
-    row0 = q.row0 + first - p0;
-    off = first - base;
-  }
-  const int col = first >> a.kv.lps, slot = first & ((1 << a.kv.lps) - 1);
-  int page = -1;
-  if (first >= 0 && col < a.s.width) page = a.s.table[(long)b * a.s.tstride + col];
-  const bool ok = page >= 0 && page < a.kv.n_pages;                  // a token without a page of the pool is not stored
-  int part = blockIdx.y;
-  const int hp = a.one ? 64 / L : HP;
-  if (part < a.q_parts) return append_qk<T, D, NORM>(a, false, part * hp, row0, first, cnt, nullptr, 0, (float2*)lds);
-  part -= a.q_parts;
-  if (part < a.k_parts) return append_qk<T, D, NORM>(a, true, part * hp, row0, first, cnt, ok ? a.kv.k + page * a.kv.kstride : nullptr, slot, (float2*)lds);
-  if (ok) append_v<T, D>(a, part - a.k_parts, row0, cnt, off, a.kv.v + page * a.kv.vstride, slot, lds);
+  const int x = blockIdx.x, qk = a.q_parts + a.k_parts;
+  if (x >= a.qk_tiles * qk) return append_v<T, D>(a, (x - a.qk_tiles * qk) / a.v_parts, (x - a.qk_tiles * qk) % a.v_parts, lds);
+  const int part = x % qk, hp = a.one ? 64 / L : HP;
+  const Run r = append_run<AP_TOK>(a, x / qk);
+  if (r.cnt <= 0) return;
+  const bool is_k = part >= a.q_parts;
+  const int page = is_k ? page_of(a, r.b, r.first) : -1;             // a token without a page of the pool is not stored
+  append_qk<T, D, NORM>(a, is_k, (part - (is_k ? a.q_parts : 0)) * hp, r.row0, r.first, r.cnt, page < 0 ? nullptr : a.kv.k + page * a.kv.kstride,
+                        r.first & ((1 << a.kv.lps) - 1), (float2*)lds);
 }
 
 template <class T, int D>
 static void append_grid(AppendArgs a, hipStream_t s) {
   constexpr int L = D / 16;
-  const int hp = a.one ? 64 / L : AP_IT * 256 / (L * AP_TOK), vh = a.one ? 64 / (D / 8) : AP_IT * 256 / (D / 8 * AP_TOK);
+  const int hp = a.one ? 64 / L : AP_IT * 256 / (L * AP_TOK), vh = a.one ? 64 / (D / 8) : AP_IT * 256 / (D / 8 * AP_VT);
   a.q_parts = (a.Hq + hp - 1) / hp;
   a.k_parts = (a.kv.heads + hp - 1) / hp;
-  const dim3 grid(a.one ? a.s.B : a.s.T / AP_TOK + 2 * a.s.B, a.q_parts + a.k_parts + (a.kv.heads + vh - 1) / vh), block(a.one ? 64 : 256);
+  a.v_parts = (a.kv.heads + vh - 1) / vh;
+  a.qk_tiles = a.one ? a.s.B : a.s.T / AP_TOK + 2 * a.s.B;
+  const int v_tiles = a.one ? a.s.B : a.s.T / AP_VT + 2 * a.s.B;
+  const dim3 grid(a.qk_tiles * (a.q_parts + a.k_parts) + v_tiles * a.v_parts), block(a.one ? 64 : 256);
   if (a.q_norm) hipLaunchKernelGGL((append_kernel<T, D, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((append_kernel<T, D, false>), grid, block, 0, s, a);
 }

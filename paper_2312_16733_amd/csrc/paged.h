@@ -129,7 +129,7 @@ struct AppendArgs {
   int Hq, half;                                  // half: rotated pairs of a head
   float eps;
   int interleaved, one;                          // one: every sequence brings exactly one token
-  int q_parts, k_parts;                          // filled by the launcher
+  int q_parts, k_parts, v_parts, qk_tiles;       // filled by the launcher
 };
 hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, hipStream_t s);
 
