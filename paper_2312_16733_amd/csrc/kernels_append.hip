@@ -23,7 +23,7 @@ struct Run { int b, row0, first, cnt, off; };    // sequence, first row, its pos
 template <int TOK>
 __device__ __forceinline__ Run append_run(const AppendArgs& a, int tile) {
   Run r;
-  if (a.one) return Run{tile, tile, clamped(a.s.lens[tile], 0, 1 << 30) - 1, 1, 0};
+  if (a.one) return Run{tile, tile, clamped(a.s.lens[tile], 0, a.s.max_len) - 1, 1, 0};
   r.b = last_at_most(a.s.B, tile, [&](int i) { return append_tile0<TOK>(a.s, i); });
   const Seq q = uniform(sequence(a.s, r.b));
   const int p0 = q.len - q.n, base = (p0 & ~(TOK - 1)) + (tile - append_tile0<TOK>(a.s, r.b)) * TOK;

@@ -15,7 +15,9 @@ namespace sna {
 
 constexpr int PA_W = 4;            // waves of a block: they take tiles of keys in turn and are joined in LDS
 constexpr int PA_K = 64;           // keys of a tile
-constexpr long kFewRows = 256 * 64;   // rows of a step, all heads, up to which this kernel is used for chunks, too
+// Scores of a step (rows, all heads, times keys) up to which this kernel is used for chunks, too: 60 tokens over 4096 keys, 32
+// heads (8 M) 27 us here and 46 with the many-rows kernel, 100 over 8192 (26 M) 74 and 65, 16 x 30 over 4096 (63 M) 102 and 78.
+constexpr long kFewScores = 24l << 20;
 
 // One wave's statistics of MB x 16 rows: row of queries 16 m + lane % 16, element of o[m][j][c]: dim 16 j + 4 (lane / 16) + c
 template <int D, int MB>
@@ -33,10 +35,9 @@ struct Attend {
   int c_lo, c_hi, h, l16, hi;
   int ids[4];                      // pages of the next tile: keys of both halves (K), value octets of both halves
 
-  __device__ __forceinline__ int page(int key) const {
-    const int id = table[clamped(key >> kv.lps, c_lo, c_hi)];
-    return clamped(id, 0, kv.n_pages - 1);
-  }
+  __device__ __forceinline__ int page(int key) const { return table[clamped(key >> kv.lps, c_lo, c_hi)]; }
+  // where the page is used: a look at it any earlier would wait for the keys and values that were asked for before it, too
+  __device__ __forceinline__ long in_pool(int id) const { return clamped(id, 0, kv.n_pages - 1); }
   __device__ __forceinline__ void find(int t) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -49,7 +50,7 @@ struct Attend {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int slot = (t * PA_K + 32 * u + 8 * (l16 >> 2) + (l16 & 3)) & (ps - 1);
-      const char* p = kv.k + id[u] * kv.kstride + ((long)h * ps + slot) * (2 * D) + hi * 16;
+      const char* p = kv.k + in_pool(id[u]) * kv.kstride + ((long)h * ps + slot) * (2 * D) + hi * 16;
 #pragma unroll
       for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -61,7 +62,7 @@ struct Attend {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int slot = (t * PA_K + 32 * u + 8 * hi) & (ps - 1);
-      const char* p = kv.v + id[2 + u] * kv.vstride + (((long)h * D + l16) * ps + slot) * 2;
+      const char* p = kv.v + in_pool(id[2 + u]) * kv.vstride + (((long)h * D + l16) * ps + slot) * 2;
 #pragma unroll
       for (int j = 0; j < J; ++j) v[u][j] = *(const u32x4*)(p + (long)j * 32 * ps);
     }
@@ -288,24 +289,24 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
   __shared__ JoinLds<D, MB> lds;
   const int p = blockIdx.x, lane = threadIdx.x & 63, heads = a.kv.heads;
   First* first = (First*)a.parts;
-  float* parts = (float*)(first + gridDim.x);
+  float* parts = (float*)(first + a.blocks);
   const long part_size = part_floats(a.rows_cap, D);
   // this share's first sequence: every wave sums the tiles of all, 64 runs of sequences at a time
-  int lo = 0, count = a.s.B;
-  long before = 0, share = 0, x = 0;
+  // (the host has seen to it that all of them fit 31 bits)
+  int lo = 0, count = a.s.B, before = 0, share = 0, x = 0;
   for (bool top = true;; top = false) {
     const int per = (count + 63) >> 6, b0 = lo + lane * per, b1 = min(lo + count, b0 + per);
-    long mine = 0;
+    int mine = 0;
     for (int b = b0; b < b1; ++b) mine += tiles_of_sequence(a, b);
-    long up = mine;
+    int up = mine;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
-      const long y = __shfl_up(up, m, 64);
+      const int y = __shfl_up(up, m, 64);
       if (lane >= m) up += y;
     }
     if (top) {
-      const long all = uniform(__shfl(up, 63, 64)) * heads;
-      share = max((all + gridDim.x - 1) / gridDim.x, (long)a.least);
+      const int all = uniform(__shfl(up, 63, 64)) * heads;
+      share = max((all + a.blocks - 1) / a.blocks, a.least);          // blocks: a power of two
       x = p * share;
       if (x >= all) {
         if (threadIdx.x == 0) first[p].b = -1;
@@ -314,31 +315,30 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
     }
     const int k = max(__ffsll((long long)__ballot((before + up) * heads > x)) - 1, 0);
     before += uniform(__shfl(up - mine, k, 64));
-    lo += k * per;
+    lo = min(lo + k * per, a.s.B - 1);
     if (per == 1) break;
-    count = min(per, count - k * per);
+    count = clamped(count - k * per, 1, per);
   }
   // its first tile of rows, head and tile of keys
   int b = uniform(lo), i0 = 0;
   Seq sq = uniform(sequence(a.s, b));
   RowTile r = rows_of_sequence(a, sq, b, 0, a.tpt);
-  long rel = x - before * heads;
-  while (rel >= (long)r.tiles * heads && i0 + a.tpt < sq.n) {
-    rel -= (long)r.tiles * heads;
+  int rel = x - before * heads;
+  while (rel >= r.tiles * heads && i0 + a.tpt < sq.n) {
+    rel -= r.tiles * heads;
     i0 += a.tpt;
     r = rows_of_sequence(a, sq, b, i0, a.tpt);
   }
-  int h = uniform((int)min(rel / max(r.tiles, 1), heads - 1l)), t = uniform((int)(rel % max(r.tiles, 1)));
-  int left = (int)min(share, 1l << 30), at = 0;     // at: tiles done, of this share
+  int h = clamped(rel / max(r.tiles, 1), 0, heads - 1), t = clamped(rel - h * r.tiles, 0, max(r.tiles - 1, 0)), left = share, at = 0;     // at: tiles done, of this share
   bool begun = false;
   while (true) {
     const int n = min(left, r.tiles - t);
     const bool whole = n == r.tiles;
     if (!whole && t == 0) {
       begun = true;
-      if (threadIdx.x == 0) first[p] = First{b, i0, h, (int)((x + at + r.tiles - 1) / share)};
+      if (threadIdx.x == 0) first[p] = First{b, i0, h, min((x + at + r.tiles - 1) / share, a.blocks - 1)};
     }
-    attend_rows<T, D, MB>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
+    if (r.n > 0) attend_rows<T, D, MB>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
     left -= n;
     at += n;
     t = 0;
@@ -366,8 +366,8 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
 // Sums, maximum and statistics of a part are asked for together: with the statistics first, a row of 64 parts took 5 us.
 constexpr int JN_Y = 8;
 template <class T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a, int blocks) {
-  constexpr int W = D / 4, N = 256 / W, U = 4;                       // threads of a row; groups; parts under way
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) {
+  constexpr int W = D / 4, N = 256 / W, U = 8;                       // threads of a row; groups; parts under way
   __shared__ __attribute__((aligned(16))) float so[N][D];
   __shared__ float2 ss[N];
   const int p = blockIdx.x, g = threadIdx.x / W, d = threadIdx.x % W * 4;
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a, 
   while (share < N && n > U * share) share *= 2;
   const int at_once = N / share;
   const long part_size = part_floats(a.rows_cap, D);
-  const float* parts = (const float*)((const First*)a.parts + blocks) + (2 * p + 1) * part_size;       // part 0; part j > 0 lies 2 j - 1 further on
+  const float* parts = (const float*)((const First*)a.parts + a.blocks) + (2 * p + 1) * part_size;       // part 0; part j > 0 lies 2 j - 1 further on
   for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {       // the same turns for the block
     const int row = row0 + g / share, row_in = min(row, rows - 1);
     float top = -INFINITY, sum = 0.f;
@@ -436,8 +436,9 @@ static void rows_grid(PagedAttnArgs a, hipStream_t s) {
     if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
     a.rows_cap = a.tpt * a.G;
     a.least = kSplitLeast;
+    a.blocks = blocks;
     hipLaunchKernelGGL((paged_split_kernel<T, D, MB>), dim3(blocks), dim3(64 * PA_W), 0, s, a);
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a, blocks);
+    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
     return;
   }
   a.by_tpt = FastDiv::by(a.tpt);
@@ -471,16 +472,16 @@ struct AttnPlan {
 static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
   const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
   AttnPlan p = {};
-  if (rows <= 64 || (long)n_tokens * group * kv_heads <= kFewRows) {
-    p.mb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  if (rows <= 64 || (long)n_tokens * group * kv_heads * keys <= kFewScores) {
+    p.mb = rows <= 16 ? 1 : group <= 32 ? 2 : 4;
     p.most = max_new;
     const long units = (n_tokens / std::max(16 * p.mb / group, 1) + n_seqs) * (long)kv_heads, room = 256 * blocks_of(head_dim, p.mb), turns = (keys + PA_W * PA_K - 1) / (PA_W * PA_K);
-    p.split = (units + room - 1) / room * turns - units * turns * 6 / (10 * room) > kSplitGain;
+    p.split = (units + room - 1) / room * turns - units * turns * 6 / (10 * room) > kSplitGain && units * ((keys >> 6) + 2) < 1l << 30;
   } else {
     p.chunks = true;
     p.splits = paged_chunk_splits(n_tokens, kv_heads, group, max_new, keys);
     if (p.splits > 1) p.chunk_parts = (size_t)p.splits * n_tokens * kv_heads * group * (head_dim + 2) * sizeof(float);
-    if (n_seqs > 1 && (long)n_seqs * max_new != n_tokens && group <= 16) {    // there may be sequences of few rows
+    if (n_seqs > 1 && (long)n_seqs * max_new != n_tokens && group <= 16 && n_seqs * (long)kv_heads * ((keys >> 6) + 2) < 1l << 30) {    // there may be sequences of few rows
       p.mb = 1;
       p.split = true;
       p.most = 16 / group;

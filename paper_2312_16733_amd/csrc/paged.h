@@ -53,6 +53,7 @@ __device__ __forceinline__ u32x4 to_16(f32x8 x) { return __builtin_bit_cast(u32x
 struct PagedSeqs {
   const int* starts; const int* lens; const int* table;
   int B, T, width, tstride;
+  int max_len;                       // longer ones are taken to be this long
 };
 struct PagedKV {
   char* k; char* v;                  // [page][head][slot][dim], [page][head][dim][slot]
@@ -62,13 +63,10 @@ struct PagedKV {
 struct Seq { int row0, n, len; };    // first row, new tokens, cached tokens with them
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }      // in scalar registers
-__device__ __forceinline__ long uniform(long x) {
-  return (long)((unsigned long)(unsigned)uniform((int)(x >> 32)) << 32 | (unsigned)uniform((int)x));
-}
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return min(max(x, lo), hi); }
 __device__ __forceinline__ Seq sequence(const PagedSeqs& s, int b) {
   const int r0 = clamped(s.starts[b], 0, s.T), r1 = clamped(s.starts[b + 1], 0, s.T);
-  return Seq{r0, max(r1 - r0, 0), clamped(s.lens[b], 0, 1 << 30)};
+  return Seq{r0, max(r1 - r0, 0), clamped(s.lens[b], 0, s.max_len)};
 }
 __device__ __forceinline__ Seq uniform(const Seq& q) { return Seq{uniform(q.row0), uniform(q.n), uniform(q.len)}; }
 // The largest i of [0, n) with f(i) <= x, for a rising f with f(0) <= x: 64 places at a time, one of them a lane, so that
@@ -148,7 +146,7 @@ struct PagedAttnArgs {
   void* parts;                                   // parts of sums, where the keys are shared out over blocks
   int tpt;                                       // tokens of a tile of rows
   FastDiv by_tpt;
-  int rows_cap, least;                           // rows of a part; least tiles of a share
+  int rows_cap, least, blocks;                   // rows of a part; least tiles of a share; blocks that share
   int splits;                                    // many rows: shares of the keys
 };
 size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);

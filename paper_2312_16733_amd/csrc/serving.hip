@@ -49,7 +49,7 @@ static sna_status check_rows(const sna_rows* r, const char* name) {
 }
 
 static PagedSeqs seqs_of(const sna_paged_batch* b) {
-  return PagedSeqs{b->starts_dev, b->lens_dev, b->page_table_dev, b->n_seqs, b->n_tokens, b->table_width < (1 << 20) ? b->table_width : 1 << 20, (int)b->table_stride};   // 2^30 slots
+  return PagedSeqs{b->starts_dev, b->lens_dev, b->page_table_dev, b->n_seqs, b->n_tokens, b->table_width < (1 << 20) ? b->table_width : 1 << 20, (int)b->table_stride, b->max_len};   // 2^30 slots
 }
 static PagedKV kv_of(const sna_paged_cache* c) {
   return PagedKV{(char*)c->k_pages_dev, (char*)c->v_pages_dev, 2 * c->k_page_stride, 2 * c->v_page_stride, c->n_pages, __builtin_ctz(c->page_size), c->kv_heads};
@@ -75,6 +75,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
       (st = check_rows(q_out, "q_out")) != SNA_OK) return st;
   AppendArgs a = {};
   a.s = seqs_of(batch);
+  a.s.max_len = 1 << 30;                                             // a token is stored at its place, or nowhere
   a.kv = kv_of(cache);
   a.q = (const char*)q->dev; a.k = (const char*)k->dev; a.v = (const char*)v->dev; a.qo = (char*)q_out->dev;
   a.inv_freq = inv_freq_dev; a.q_norm = q_norm_dev; a.k_norm = k_norm_dev;
