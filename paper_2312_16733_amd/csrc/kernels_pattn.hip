@@ -13,8 +13,8 @@
 
 namespace sna {
 
-constexpr int PA_W = 4;            // waves of a block: they take tiles of keys in turn and are joined in LDS
-constexpr int PA_K = 64;           // keys of a tile
+// Keys of a wave's tile: 64, or 32 where more rows of sums would leave room in the registers for one block on a CU only
+constexpr int tile_keys(int D, int MB) { return MB * D > 128 ? 32 : 64; }
 // Scores of a step (rows, all heads, times keys) up to which this kernel is used for chunks, too: 60 tokens over 4096 keys, 32
 // heads (8 M) 27 us here and 46 with the many-rows kernel, 100 over 8192 (26 M) 74 and 65, 16 x 30 over 4096 (63 M) 102 and 78.
 constexpr long kFewScores = 24l << 20;
@@ -27,29 +27,31 @@ struct RowState {
 };
 struct Span { int lo, hi; };       // keys lo .. hi - 1
 
+// Queries are in registers, or in LDS where they would take those of a second block on the CU; every wave of a block has the same
+constexpr bool queries_in_lds(int D, int MB) { return MB * D > 128; }
 template <class T, int D, int MB>
 struct Attend {
-  static constexpr int S = D / 32, J = D / 16;
+  static constexpr int S = D / 32, J = D / 16, KT = tile_keys(D, MB), U = KT / 32;
   const PagedKV kv;
   const int* table;                // the sequence's
   int c_lo, c_hi, h, l16, hi;
-  int ids[4];                      // pages of the next tile: keys of both halves (K), value octets of both halves
+  int ids[2 * U];                  // pages of the next tile: keys of each 32, value octets of each 32
 
   __device__ __forceinline__ int page(int key) const { return table[clamped(key >> kv.lps, c_lo, c_hi)]; }
   // where the page is used: a look at it any earlier would wait for the keys and values that were asked for before it, too
   __device__ __forceinline__ long in_pool(int id) const { return clamped(id, 0, kv.n_pages - 1); }
   __device__ __forceinline__ void find(int t) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      ids[u] = page(t * PA_K + 32 * u + 8 * (l16 >> 2));
-      ids[2 + u] = page(t * PA_K + 32 * u + 8 * hi);
+    for (int u = 0; u < U; ++u) {
+      ids[u] = page(t * KT + 32 * u + 8 * (l16 >> 2));
+      ids[U + u] = page(t * KT + 32 * u + 8 * hi);
     }
   }
-  __device__ __forceinline__ void load_k(int t, const int (&id)[4], u32x4 (&k)[2][2][S]) const {
+  __device__ __forceinline__ void load_k(int t, const int (&id)[2 * U], u32x4 (&k)[U][2][S]) const {
     const int ps = 1 << kv.lps;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int slot = (t * PA_K + 32 * u + 8 * (l16 >> 2) + (l16 & 3)) & (ps - 1);
+    for (int u = 0; u < U; ++u) {
+      const int slot = (t * KT + 32 * u + 8 * (l16 >> 2) + (l16 & 3)) & (ps - 1);
       const char* p = kv.k + in_pool(id[u]) * kv.kstride + ((long)h * ps + slot) * (2 * D) + hi * 16;
 #pragma unroll
       for (int a = 0; a < 2; ++a)
@@ -57,12 +59,12 @@ struct Attend {
         for (int s = 0; s < S; ++s) k[u][a][s] = *(const u32x4*)(p + a * (8 * D) + s * 64);
     }
   }
-  __device__ __forceinline__ void load_v(int t, const int (&id)[4], u32x4 (&v)[2][J]) const {
+  __device__ __forceinline__ void load_v(int t, const int (&id)[2 * U], u32x4 (&v)[U][J]) const {
     const int ps = 1 << kv.lps;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int slot = (t * PA_K + 32 * u + 8 * hi) & (ps - 1);
-      const char* p = kv.v + in_pool(id[2 + u]) * kv.vstride + (((long)h * D + l16) * ps + slot) * 2;
+    for (int u = 0; u < U; ++u) {
+      const int slot = (t * KT + 32 * u + 8 * hi) & (ps - 1);
+      const char* p = kv.v + in_pool(id[U + u]) * kv.vstride + (((long)h * D + l16) * ps + slot) * 2;
 #pragma unroll
       for (int j = 0; j < J; ++j) v[u][j] = *(const u32x4*)(p + (long)j * 32 * ps);
     }
@@ -71,7 +73,7 @@ struct Attend {
   // Tiles t0, t0 + step, .. below t1.  lim / low: the last and first key that the lane's row of each m sees; all of them
   // see the keys from `clear.lo` to `clear.hi - 1`, none sees any outside `keys`.
   __device__ __forceinline__ void run(int t0, int t1, int step, Span keys, Span clear, const int (&lim)[MB], const int (&low)[MB],
-                                      const u32x4 (&q)[MB][S], float scale2, RowState<D, MB>& st) {
+                                      const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<D, MB>& st) {
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
       st.top[m] = -INFINITY;
@@ -80,66 +82,74 @@ struct Attend {
       for (int j = 0; j < J; ++j) st.o[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     if (t0 >= t1) return;
-    u32x4 k[2][2][S], v[2][J];
-    int now[4];
+    u32x4 k[U][2][S], v[U][J];
+    int now[2 * U];
     find(t0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) now[i] = ids[i];
+    for (int i = 0; i < 2 * U; ++i) now[i] = ids[i];
     load_k(t0, now, k);
     load_v(t0, now, v);
     find(t0 + step);
     for (int t = t0; t < t1; t += step) {
       const bool more = t + step < t1;
-      u32x4 p[MB][2];
+      u32x4 p[MB][U];
+      int lane = hi * 16 + l16;
+#if defined(__HIP_DEVICE_COMPILE__)
+      if (queries_in_lds(D, MB)) asm volatile("" : "+v"(lane));        // read anew for each tile, not kept in registers
+#endif
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
-        f32x4 sc[2][2];
+        f32x4 sc[U][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int i = 0; i < 2 * U; ++i) sc[i >> 1][i & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            sc[u][a] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < S; ++s) {
+          const u32x4 x = queries_in_lds(D, MB) ? q_lds[m * S + s][lane] : q[m][s];
 #pragma unroll
-            for (int s = 0; s < S; ++s) sc[u][a] = T::mma16(k[u][a][s], q[m][s], sc[u][a]);
-          }
+          for (int i = 0; i < 2 * U; ++i) sc[i >> 1][i & 1] = T::mma16(k[i >> 1][i & 1][s], x, sc[i >> 1][i & 1]);
+        }
         if (m == MB - 1 && more) {                                   // the next keys come in under the softmax and the second product
 #pragma unroll
-          for (int i = 0; i < 4; ++i) now[i] = ids[i];
+          for (int i = 0; i < 2 * U; ++i) now[i] = ids[i];
           load_k(t + step, now, k);
           find(t + 2 * step);
         }
-        if (t * PA_K < clear.lo || t * PA_K + PA_K > clear.hi) {
+        if (t * KT < clear.lo || t * KT + KT > clear.hi) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = t * PA_K + 8 * hi + 32 * (i >> 3) + (i & 7);
+          for (int i = 0; i < 8 * U; ++i) {
+            const int key = t * KT + 8 * hi + 32 * (i >> 3) + (i & 7);
             sc[i >> 3][(i >> 2) & 1][i & 3] = key <= lim[m] && key >= low[m] ? sc[i >> 3][(i >> 2) & 1][i & 3] : -INFINITY;
           }
         }
         float x = sc[0][0][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) x = fmaxf(x, sc[i >> 3][(i >> 2) & 1][i & 3]);
-        const float top = fmaxf(st.top[m], max_of_4(x) * scale2);
-        const float ref = top == -INFINITY ? 0.f : top;              // nothing seen so far
-        const float keep = __builtin_amdgcn_exp2f(st.top[m] - ref);
-        st.top[m] = top;
-        st.sum[m] *= keep;
+        for (int i = 1; i < 8 * U; ++i) x = fmaxf(x, sc[i >> 3][(i >> 2) & 1][i & 3]);
+        // the reference is raised only where a score exceeds it by a factor of 2^8 and more: below that the exponentials, their
+        // sums and the products are exact enough as they are (p up to 2^8 in the operand type, fp32 sums), and o stays untouched
+        x = max_of_4(x) * scale2;
+        if (__any(x - st.top[m] > 8.f)) {
+          const float top = fmaxf(st.top[m], x), keep = __builtin_amdgcn_exp2f(st.top[m] - (top == -INFINITY ? 0.f : top));
+          st.top[m] = top;
+          st.sum[m] *= keep;
 #pragma unroll
-        for (int j = 0; j < J; ++j) st.o[m][j] *= keep;
+          for (int j = 0; j < J; ++j) st.o[m][j] *= keep;
+        }
+        const float ref = st.top[m] == -INFINITY ? 0.f : st.top[m];  // nothing seen so far
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < U; ++u) {
           f32x8 e;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             e[i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i >> 2][i & 3], scale2, -ref));
             st.sum[m] += e[i];
           }
-          p[m][u] = to_16<T>(e);                                     // the operand type: p is at most 1, off by half a step of it
+          p[m][u] = to_16<T>(e);                                     // off by half a step of the operand type
         }
       }
-      if (t * PA_K < keys.lo || t * PA_K + PA_K > keys.hi) {         // slots that hold no key may hold anything: 0 * NaN is not 0
+      if (t * KT < keys.lo || t * KT + KT > keys.hi) {         // slots that hold no key may hold anything: 0 * NaN is not 0
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int key0 = t * PA_K + 32 * u + 8 * hi;
+        for (int u = 0; u < U; ++u) {
+          const int key0 = t * KT + 32 * u + 8 * hi;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const int key = key0 + 2 * w;
@@ -154,7 +164,7 @@ struct Attend {
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) st.o[m][j] = T::mma16(v[u][j], p[m][u], st.o[m][j]);
+          for (int u = 0; u < U; ++u) st.o[m][j] = T::mma16(v[u][j], p[m][u], st.o[m][j]);
       if (more) load_v(t + step, now, v);
     }
   }
@@ -166,6 +176,7 @@ struct RowTile {
   Span keys, clear;                // keys that some row sees, keys that all see
   int t0, tiles;                   // tiles of keys; at least one, so that rows without keys are written too
 };
+template <int KT>
 __device__ __forceinline__ RowTile rows_of_sequence(const PagedAttnArgs& a, const Seq& sq, int b, int i0, int most) {
   RowTile r;
   r.b = b;
@@ -175,21 +186,22 @@ __device__ __forceinline__ RowTile rows_of_sequence(const PagedAttnArgs& a, cons
   const int last = min(r.pos0 + r.n - 1, (a.s.width << a.kv.lps) - 1);
   r.keys = Span{max(a.window <= r.pos0 ? r.pos0 - a.window + 1 : 0, 0), last + 1};
   r.clear = Span{a.window <= last ? last - a.window + 1 : 0, r.pos0 + 1};
-  r.t0 = r.keys.lo / PA_K;
-  r.tiles = r.n > 0 ? max((max(r.keys.hi, 0) + PA_K - 1) / PA_K - r.t0, 1) : 0;
+  r.t0 = r.keys.lo / KT;
+  r.tiles = r.n > 0 ? max((max(r.keys.hi, 0) + KT - 1) / KT - r.t0, 1) : 0;
   return r;
 }
 
-template <int D, int MB>
-struct JoinLds {
-  __attribute__((aligned(16))) float o[PA_W][16][D + 4];
-  float top[PA_W][MB][16], sum[PA_W][MB][16];
+template <int D, int MB, int W>
+struct JoinLds {                   // of the W waves of a block: they take tiles of keys in turn
+  __attribute__((aligned(16))) u32x4 q[queries_in_lds(D, MB) ? MB * (D / 32) : 1][64];
+  __attribute__((aligned(16))) float o[W][16][D + 4];
+  float top[W][MB][16], sum[W][MB][16];
 };
 
 // Keys of tiles t0 .. t1 - 1 for the rows of `r` and head h; the waves' parts are joined and leave as results, or as a part of
 // them (part != nullptr): [rows_cap][D] sums, then [rows_cap][2] maximum and sum.
-template <class T, int D, int MB>
-__device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTile& r, int h, int t0, int t1, float* part, int rows_cap, JoinLds<D, MB>& lds) {
+template <class T, int D, int MB, int W>
+__device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTile& r, int h, int t0, int t1, float* part, int rows_cap, JoinLds<D, MB, W>& lds) {
   constexpr int S = D / 32, J = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, hi = lane >> 4;
   const int rows = r.n * a.G;
@@ -205,10 +217,14 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
       low[m] = a.window <= lim[m] ? lim[m] - a.window + 1 : 0;
       const char* x = a.q + (r.row0 + i) * a.q_t + (h * a.G + row - i * a.G) * a.q_h + hi * 16;
 #pragma unroll
-      for (int s = 0; s < S; ++s) q[m][s] = *(const u32x4*)(x + s * 64);
+      for (int s = 0; s < S; ++s) {
+        if (!queries_in_lds(D, MB)) q[m][s] = *(const u32x4*)(x + s * 64);
+        else if ((m * S + s) % W == wave) lds.q[m * S + s][lane] = *(const u32x4*)(x + s * 64);
+      }
     }
+    if (queries_in_lds(D, MB)) __syncthreads();
     Attend<T, D, MB> at = {a.kv, a.s.table + (long)r.b * a.s.tstride, r.keys.lo >> a.kv.lps, max(r.keys.hi - 1, 0) >> a.kv.lps, h, l16, hi, {}};
-    at.run(t0 + wave, t1, PA_W, r.keys, r.clear, lim, low, q, a.scale2, st);
+    at.run(t0 + wave, t1, W, r.keys, r.clear, lim, low, q, lds.q, a.scale2, st);
   }
   // o and sum relative to the largest maximum of the waves
 #pragma unroll
@@ -222,7 +238,7 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
     if (16 * m >= rows) break;
     float top = lds.top[0][m][l16];
 #pragma unroll
-    for (int w = 1; w < PA_W; ++w) top = fmaxf(top, lds.top[w][m][l16]);
+    for (int w = 1; w < W; ++w) top = fmaxf(top, lds.top[w][m][l16]);
     const float keep = __builtin_amdgcn_exp2f(st.top[m] - (top == -INFINITY ? 0.f : top));
     if (m) __syncthreads();
 #pragma unroll
@@ -232,10 +248,10 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
     if (r16 < 16 && row < rows) {
       float t = lds.top[0][m][r16], sum = 0.f;
 #pragma unroll
-      for (int w = 1; w < PA_W; ++w) t = fmaxf(t, lds.top[w][m][r16]);
+      for (int w = 1; w < W; ++w) t = fmaxf(t, lds.top[w][m][r16]);
       f32x8 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < PA_W; ++w) {
+      for (int w = 0; w < W; ++w) {
         sum += lds.sum[w][m][r16] * __builtin_amdgcn_exp2f(lds.top[w][m][r16] - (t == -INFINITY ? 0.f : t));
         const f32x4 y0 = *(const f32x4*)&lds.o[w][r16][oct * 8], y1 = *(const f32x4*)&lds.o[w][r16][oct * 8 + 4];
 #pragma unroll
@@ -254,12 +270,12 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
 }
 
 // Two blocks on a CU where the registers allow it: 8 waves with 16 KB and more under way each
-constexpr int blocks_of(int D, int MB) { return MB * D <= 128 ? 2 : 1; }
+constexpr int blocks_of(int D, int MB) { return MB * D <= 256 ? 2 : 1; }
 
 // A block for each tile of rows and key / value head
-template <class T, int D, int MB>
-__global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_rows_kernel(const PagedAttnArgs a) {
-  __shared__ JoinLds<D, MB> lds;
+template <class T, int D, int MB, int W>
+__global__ __launch_bounds__(64 * W, blocks_of(D, MB)) void paged_rows_kernel(const PagedAttnArgs a) {
+  __shared__ JoinLds<D, MB, W> lds;
   const int tile = blockIdx.x;
   int b = tile, i0 = 0;
   if (a.max_new > a.tpt) {
@@ -267,26 +283,29 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_rows_kernel
     b = last_at_most(a.s.B, tile, tile0);
     i0 = (tile - tile0(b)) * a.tpt;
   }
-  const RowTile r = rows_of_sequence(a, sequence(a.s, b), b, i0, a.tpt);
-  if (r.n > 0) attend_rows<T, D, MB>(a, r, blockIdx.y, r.t0, r.t0 + r.tiles, nullptr, 0, lds);
+  const RowTile r = rows_of_sequence<tile_keys(D, MB)>(a, sequence(a.s, b), b, i0, a.tpt);
+  if (r.n > 0) attend_rows<T, D, MB, W>(a, r, blockIdx.y, r.t0, r.t0 + r.tiles, nullptr, 0, lds);
 }
 
 // Tiles of keys of all tiles of a sequence's rows, for one head; none where the sequence has more rows than are taken here
+template <int KT>
 __device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) {
   const Seq sq = sequence(a.s, b);
   if (sq.n > a.most) return 0;
   int n = 0;
-  for (int i0 = 0; i0 < sq.n; i0 += a.tpt) n += rows_of_sequence(a, sq, b, i0, a.tpt).tiles;
+  for (int i0 = 0; i0 < sq.n; i0 += a.tpt) n += rows_of_sequence<KT>(a, sq, b, i0, a.tpt).tiles;
   return n;
 }
 // The keys of all tiles of rows and heads, laid end to end, in equal shares over the blocks: what a share cuts off of a
 // (tile of rows, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what
 // a later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
-struct First { int b, i0, h, last; };
+struct First { int row0, n, h, last; };                              // first row, tokens (0: none was begun), head, block
+constexpr int kSplitW = 4;         // waves of a block
 __host__ __device__ constexpr long part_floats(long rows, int D) { return (rows * (D + 2) + 3) & ~3l; }    // 16-byte aligned
 template <class T, int D, int MB>
-__global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
-  __shared__ JoinLds<D, MB> lds;
+__global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
+  __shared__ JoinLds<D, MB, kSplitW> lds;
+  constexpr int KT = tile_keys(D, MB);
   const int p = blockIdx.x, lane = threadIdx.x & 63, heads = a.kv.heads;
   First* first = (First*)a.parts;
   float* parts = (float*)(first + a.blocks);
@@ -297,7 +316,7 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
   for (bool top = true;; top = false) {
     const int per = (count + 63) >> 6, b0 = lo + lane * per, b1 = min(lo + count, b0 + per);
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles_of_sequence(a, b);
+    for (int b = b0; b < b1; ++b) mine += tiles_of_sequence<KT>(a, b);
     int up = mine;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
@@ -309,7 +328,7 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
       share = max((all + a.blocks - 1) / a.blocks, a.least);          // blocks: a power of two
       x = p * share;
       if (x >= all) {
-        if (threadIdx.x == 0) first[p].b = -1;
+        if (threadIdx.x == 0) first[p].n = 0;
         return;
       }
     }
@@ -322,12 +341,12 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
   // its first tile of rows, head and tile of keys
   int b = uniform(lo), i0 = 0;
   Seq sq = uniform(sequence(a.s, b));
-  RowTile r = rows_of_sequence(a, sq, b, 0, a.tpt);
+  RowTile r = rows_of_sequence<KT>(a, sq, b, 0, a.tpt);
   int rel = x - before * heads;
   while (rel >= r.tiles * heads && i0 + a.tpt < sq.n) {
     rel -= r.tiles * heads;
     i0 += a.tpt;
-    r = rows_of_sequence(a, sq, b, i0, a.tpt);
+    r = rows_of_sequence<KT>(a, sq, b, i0, a.tpt);
   }
   int h = clamped(rel / max(r.tiles, 1), 0, heads - 1), t = clamped(rel - h * r.tiles, 0, max(r.tiles - 1, 0)), left = share, at = 0;     // at: tiles done, of this share
   bool begun = false;
@@ -336,9 +355,9 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
     const bool whole = n == r.tiles;
     if (!whole && t == 0) {
       begun = true;
-      if (threadIdx.x == 0) first[p] = First{b, i0, h, min((x + at + r.tiles - 1) / share, a.blocks - 1)};
+      if (threadIdx.x == 0) first[p] = First{r.row0, r.n, h, min((x + at + r.tiles - 1) / share, a.blocks - 1)};
     }
-    if (r.n > 0) attend_rows<T, D, MB>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
+    if (r.n > 0) attend_rows<T, D, MB, kSplitW>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
     left -= n;
     at += n;
     t = 0;
@@ -354,11 +373,11 @@ __global__ __launch_bounds__(64 * PA_W, blocks_of(D, MB)) void paged_split_kerne
         } while (sq.n <= 0 || sq.n > a.most);
         if (b >= a.s.B) break;
       }
-      r = rows_of_sequence(a, sq, b, i0, a.tpt);
+      r = rows_of_sequence<KT>(a, sq, b, i0, a.tpt);
     }
     __syncthreads();                                                 // the next part's joining
   }
-  if (!begun && threadIdx.x == 0) first[p].b = -1;
+  if (!begun && threadIdx.x == 0) first[p].n = 0;
 }
 
 // Parts joined: JN_Y blocks for each (tile of rows, head) that was cut.  A thread has four dims of a row; the 256 / (D / 4)
@@ -372,9 +391,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) 
   __shared__ float2 ss[N];
   const int p = blockIdx.x, g = threadIdx.x / W, d = threadIdx.x % W * 4;
   const First f = ((const First*)a.parts)[p];
-  if (f.b < 0) return;
-  const RowTile r = rows_of_sequence(a, sequence(a.s, f.b), f.b, f.i0, a.tpt);
-  const int n = f.last - p + 1, rows = r.n * a.G;
+  if (f.n == 0) return;
+  const int n = f.last - p + 1, rows = f.n * a.G;
   int share = 1;                                                     // groups that share a row
   while (share < N && n > U * share) share *= 2;
   const int at_once = N / share;
@@ -422,7 +440,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) 
     if (row >= rows) continue;
     x *= sum == 0.f ? 0.f : 1.f / sum;
     const int i = row / a.G;
-    *(uint2*)(a.o + (r.row0 + i) * a.o_t + (f.h * a.G + row - i * a.G) * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
+    *(uint2*)(a.o + (f.row0 + i) * a.o_t + (f.h * a.G + row - i * a.G) * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
   }
 }
 
@@ -432,18 +450,22 @@ template <class T, int D, int MB>
 static void rows_grid(PagedAttnArgs a, hipStream_t s) {
   a.tpt = 16 * MB / a.G;
   if (a.parts) {
-    const int blocks = 256 * blocks_of(D, MB);                       // what the chip holds at once
     if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
     a.rows_cap = a.tpt * a.G;
     a.least = kSplitLeast;
-    a.blocks = blocks;
-    hipLaunchKernelGGL((paged_split_kernel<T, D, MB>), dim3(blocks), dim3(64 * PA_W), 0, s, a);
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_split_kernel<T, D, MB>), dim3(a.blocks), dim3(64 * kSplitW), 0, s, a);
+    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
     return;
   }
   a.by_tpt = FastDiv::by(a.tpt);
   const int tiles = a.max_new > a.tpt ? a.s.T / a.tpt + a.s.B : a.s.B;
-  hipLaunchKernelGGL((paged_rows_kernel<T, D, MB>), dim3(tiles, a.kv.heads), dim3(64 * PA_W), 0, s, a);
+  const dim3 grid(tiles, a.kv.heads);
+  if constexpr (blocks_of(D, MB) == 2)
+    if (a.waves == 8) {
+      hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 8>), grid, dim3(512), 0, s, a);
+      return;
+    }
+  hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 4>), grid, dim3(256), 0, s, a);
 }
 template <class T, int D>
 static void rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
@@ -451,19 +473,26 @@ static void rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
   else if (mb == 2) rows_grid<T, D, 2>(a, s);
   else rows_grid<T, D, 4>(a, s);
 }
-static size_t parts_bytes(int head_dim, int mb, long rows_cap) {
-  return 256 * blocks_of(head_dim, mb) * (sizeof(First) + 2 * part_floats(rows_cap, head_dim) * sizeof(float));
-}
 
-// Blocks of whole (tile of rows, head)s walk the longest sequence in turns of a tile for each wave, as many times over as the chip
-// has to be filled; shared out, the keys take the mean instead, but their parts are written and joined in a second launch.
-// Sequences are taken to be 0.6 of the longest on average.
-constexpr long kSplitGain = 6;     // turns that sharing has to save
+// Blocks of whole (tile of rows, head)s walk the longest sequence, which a CU reads at 60 to 70 GB/s; shared out, the keys take
+// what the chip reads at, but their parts are written and joined in a second launch, 6 us.  One tile of rows a sequence (decoding):
+// shared from 1024 keys of 128 on (8 sequences of up to 2048, 8 heads: 18.1 us shared, 23.7 whole; 32 of up to 1000: 21.9 and
+// 16.5), from half of that where most of the chip would be idle (one of 1000: 11.0 and 13.3).
+// Several: where sharing saves kSplitGain turns of a tile for each wave, with sequences of 0.6 of the longest on average (60
+// tokens over 4096 keys, 32 heads: 26.6 us shared, 55 whole; 512 over their own 512: 60 and 22.6, since there every block has to
+// find its way through many short rows of tiles).
+constexpr long kSplitKeys = 1024 * 128, kSplitGain = 6;
+
+// Blocks that share the keys.  One on each CU keeps 128 KB under way (heads of 128) and cuts fewer parts off than two: one sequence
+// of 131071 keys 97 us and 104, 64 of up to 8192 193 and 195; two where (tile of rows, head)s are many and few of them are cut
+// (200 sequences of up to 2500: 219 and 228), or half as long (64 of up to 8192, heads of 64: 61.7 and 63.7).
+static int split_blocks(int head_dim, int mb, long units) { return 256 * (head_dim == 128 && units <= 512 ? 1 : blocks_of(head_dim, mb)); }
 
 // How a step is launched, from what the host knows of it.
 struct AttnPlan {
   int mb;                          // 16 rows of a block of the few-rows kernel, of which there are 1, 2 or 4; 0: not launched
-  bool split;                      // its keys shared out over the blocks
+  int blocks;                      // that its keys are shared out over; 0: a block walks all of its rows' keys
+  int waves;                       // of a block that walks all keys of its rows
   int most;                        // tokens of a sequence up to which it takes it
   bool chunks;                     // the many-rows kernel takes the other sequences
   int splits;                      // shares of their keys
@@ -475,19 +504,22 @@ static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
   if (rows <= 64 || (long)n_tokens * group * kv_heads * keys <= kFewScores) {
     p.mb = rows <= 16 ? 1 : group <= 32 ? 2 : 4;
     p.most = max_new;
-    const long units = (n_tokens / std::max(16 * p.mb / group, 1) + n_seqs) * (long)kv_heads, room = 256 * blocks_of(head_dim, p.mb), turns = (keys + PA_W * PA_K - 1) / (PA_W * PA_K);
-    p.split = (units + room - 1) / room * turns - units * turns * 6 / (10 * room) > kSplitGain && units * ((keys >> 6) + 2) < 1l << 30;
+    const long units = (n_tokens / std::max(16 * p.mb / group, 1) + n_seqs) * (long)kv_heads, room = 256 * blocks_of(head_dim, p.mb), kt = tile_keys(head_dim, p.mb), tiles = (keys + kt - 1) / kt;
+    p.waves = blocks_of(head_dim, p.mb) == 2 && units <= 256 && tiles * kt > 512 ? 8 : 4;
+    const long whole = (units + room - 1) / room * ((tiles + p.waves - 1) / p.waves), shared = units * tiles * 6 / (10 * kSplitW * room);
+    const bool split = (max_new * group <= 16 * p.mb ? keys * head_dim > (units <= 32 ? kSplitKeys / 2 : kSplitKeys) : whole - shared > kSplitGain * 64 / kt) && units * (tiles + 2) < 1l << 30;
+    if (split) p.blocks = split_blocks(head_dim, p.mb, units);
   } else {
     p.chunks = true;
     p.splits = paged_chunk_splits(n_tokens, kv_heads, group, max_new, keys);
     if (p.splits > 1) p.chunk_parts = (size_t)p.splits * n_tokens * kv_heads * group * (head_dim + 2) * sizeof(float);
-    if (n_seqs > 1 && (long)n_seqs * max_new != n_tokens && group <= 16 && n_seqs * (long)kv_heads * ((keys >> 6) + 2) < 1l << 30) {    // there may be sequences of few rows
+    if (n_seqs > 1 && (long)n_seqs * max_new != n_tokens && group <= 16 && n_seqs * (long)kv_heads * ((keys >> 5) + 2) < 1l << 30) {    // there may be sequences of few rows
       p.mb = 1;
-      p.split = true;
+      p.blocks = split_blocks(head_dim, 1, n_seqs * (long)kv_heads);
       p.most = 16 / group;
     }
   }
-  if (p.mb && p.split) p.parts = (parts_bytes(head_dim, p.mb, (long)std::min(16 * p.mb / group, max_new) * group) + 255) & ~(size_t)255;
+  if (p.blocks) p.parts = (p.blocks * (sizeof(First) + 2 * part_floats((long)std::min(16 * p.mb / group, max_new) * group, head_dim) * sizeof(float)) + 255) & ~(size_t)255;
   return p;
 }
 
@@ -501,7 +533,9 @@ hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int 
   a.most = p.most;
   if (p.mb) {
     PagedAttnArgs r = a;
-    r.parts = p.split ? workspace : nullptr;
+    r.parts = p.blocks ? workspace : nullptr;
+    r.blocks = p.blocks;
+    r.waves = p.waves;
     if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? rows_of<Fp16, 64>(r, p.mb, s) : rows_of<Fp16, 128>(r, p.mb, s);
     else head_dim == 64 ? rows_of<Bf16, 64>(r, p.mb, s) : rows_of<Bf16, 128>(r, p.mb, s);
   }

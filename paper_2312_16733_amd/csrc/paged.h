@@ -144,6 +144,7 @@ struct PagedAttnArgs {
   // filled by the launchers
   int most;                                      // tokens of a sequence up to which the few-rows kernel takes it, not the other
   void* parts;                                   // parts of sums, where the keys are shared out over blocks
+  int waves;                                     // few rows: of a block that walks all keys of its rows
   int tpt;                                       // tokens of a tile of rows
   FastDiv by_tpt;
   int rows_cap, least, blocks;                   // rows of a part; least tiles of a share; blocks that share
