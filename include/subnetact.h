@@ -389,7 +389,8 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
  * keys of positions p - window + 1 .. p (window 0: all up to p).  Query head i reads key / value head
  * i / (q_heads / kv_heads); scale is positive.  Statistics and sums are fp32, the probabilities of a product are rounded to
  * the element type, the result once more.  A token that sees no key (its position is negative) gives zeros.
- * Slots that no visible key of the sequence lies in may hold anything.
+ * Slots that no visible key of the sequence lies in may hold anything; a value that is no number reaches the tokens that see
+ * its key and no others.
  * The workspace (16-byte aligned) holds parts of sums of sequences whose keys several blocks share; its contents need not
  * survive or precede a call.  sna_paged_attention_workspace_bytes: how much a call with these sizes wants (0: none), or a
  * negative sna_status.

@@ -24,8 +24,36 @@ template <int D, int MB>
 struct RowState {
   f32x4 o[MB][D / 16];
   float top[MB], sum[MB];          // maximum that o and sum are relative to (base 2); sum over this lane's keys
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      top[m] = -INFINITY;
+      sum[m] = 0.f;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  __device__ __forceinline__ bool is_odd() const {                   // for some row of the wave: 0 x is 0 for a number, and only then
+    float x = 0.f;
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < D / 4; ++i) x = fmaf(o[m][i >> 2][i & 3], 0.f, x);
+    return __any(x != 0.f);
+  }
 };
 struct Span { int lo, hi; };       // keys lo .. hi - 1
+
+// All ones for those of key .. key + 7 that lie in the span
+__device__ __forceinline__ u32x4 slots_of(int key, Span keys) {
+  u32x4 v;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int k = key + 2 * w;
+    v[w] = (k >= keys.lo && k < keys.hi ? 0xffffu : 0u) | (k + 1 >= keys.lo && k + 1 < keys.hi ? 0xffff0000u : 0u);
+  }
+  return v;
+}
 
 // Queries are in registers, or in LDS where they would take those of a second block on the CU; every wave of a block has the same
 constexpr bool queries_in_lds(int D, int MB) { return MB * D > 128; }
@@ -70,17 +98,89 @@ struct Attend {
     }
   }
 
+  // What run() does, at leisure, for a wave whose sums came out as no numbers: in tiles whose rows differ in the keys they see, a
+  // value that is none would have reached the rows that do not see its key, too.
+  __device__ __forceinline__ void run_carefully(int t0, int t1, int step, Span keys, Span clear, const int (&lim)[MB], const int (&low)[MB],
+                                                const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<D, MB>& st) const {
+    st.clear();
+#pragma unroll 1
+    for (int t = t0; t < t1; t += step) {
+      int id[2 * U];
+      const char* at[U];
+      u32x4 ok[U], k[U][2][S];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int key = t * KT + 32 * u + 8 * hi;
+        id[u] = page(t * KT + 32 * u + 8 * (l16 >> 2));
+        at[u] = kv.v + in_pool(page(key)) * kv.vstride + ((((long)h * D + l16) << kv.lps) + (key & ((1 << kv.lps) - 1))) * 2;
+        ok[u] = slots_of(key, keys);
+      }
+      load_k(t, id, k);
+      const bool differ = t * KT < clear.lo || t * KT + KT > clear.hi;
+#pragma unroll
+      for (int m = 0; m < MB; ++m) {
+        f32x4 sc[U][2];
+#pragma unroll
+        for (int i = 0; i < 2 * U; ++i) sc[i >> 1][i & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          const u32x4 x = queries_in_lds(D, MB) ? q_lds[m * S + s][hi * 16 + l16] : q[m][s];
+#pragma unroll
+          for (int i = 0; i < 2 * U; ++i) sc[i >> 1][i & 1] = T::mma16(k[i >> 1][i & 1][s], x, sc[i >> 1][i & 1]);
+        }
+        float x = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8 * U; ++i) {
+          const int key = t * KT + 8 * hi + 32 * (i >> 3) + (i & 7);
+          const float y = key <= lim[m] && key >= low[m] ? sc[i >> 3][(i >> 2) & 1][i & 3] * scale2 : -INFINITY;
+          sc[i >> 3][(i >> 2) & 1][i & 3] = y;
+          x = fmaxf(x, y);
+        }
+        const float top = fmaxf(st.top[m], max_of_4(x)), ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(st.top[m] - ref);
+        st.top[m] = top;
+        st.sum[m] *= keep;
+        u32x4 p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          f32x8 e;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            e[i] = __builtin_amdgcn_exp2f(sc[u][i >> 2][i & 3] - ref);
+            st.sum[m] += e[i];
+          }
+          p[u] = to_16<T>(e);
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          u32x4 v[U];
+          st.o[m][j] *= keep;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            v[u] = *(const u32x4*)(at[u] + ((long)j * 32 << kv.lps));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v[u][w] &= ok[u][w];
+            st.o[m][j] = T::mma16(differ ? without_odd<T>(v[u]) : v[u], p[u], st.o[m][j]);
+          }
+          if (differ)
+#pragma unroll
+            for (int kind = 0; kind < ODD_KINDS; ++kind) {
+              f32x4 n = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int u = 0; u < U; ++u) n = T::mma16(ones_where_odd<T>(v[u], kind), ones_where_seen<T>(t * KT + 32 * u + 8 * hi, low[m], lim[m]), n);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) st.o[m][j][c] += odd_sum(n[c] > 0.f, kind);
+            }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+
   // Tiles t0, t0 + step, .. below t1.  lim / low: the last and first key that the lane's row of each m sees; all of them
   // see the keys from `clear.lo` to `clear.hi - 1`, none sees any outside `keys`.
   __device__ __forceinline__ void run(int t0, int t1, int step, Span keys, Span clear, const int (&lim)[MB], const int (&low)[MB],
                                       const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<D, MB>& st) {
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      st.top[m] = -INFINITY;
-      st.sum[m] = 0.f;
-#pragma unroll
-      for (int j = 0; j < J; ++j) st.o[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    st.clear();
     if (t0 >= t1) return;
     u32x4 k[U][2][S], v[U][J];
     int now[2 * U];
@@ -146,17 +246,14 @@ struct Attend {
           p[m][u] = to_16<T>(e);                                     // off by half a step of the operand type
         }
       }
-      if (t * KT < keys.lo || t * KT + KT > keys.hi) {         // slots that hold no key may hold anything: 0 * NaN is not 0
+      if (t * KT < keys.lo || t * KT + KT > keys.hi) {               // slots that hold no key may hold anything: 0 * NaN is not 0
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int key0 = t * KT + 32 * u + 8 * hi;
+          const u32x4 ok = slots_of(t * KT + 32 * u + 8 * hi, keys);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int key = key0 + 2 * w;
-            const unsigned ok = (key >= keys.lo && key < keys.hi ? 0xffffu : 0u) | (key + 1 >= keys.lo && key + 1 < keys.hi ? 0xffff0000u : 0u);
+          for (int w = 0; w < 4; ++w)
 #pragma unroll
-            for (int j = 0; j < J; ++j) v[u][j][w] &= ok;
-          }
+            for (int j = 0; j < J; ++j) v[u][j][w] &= ok[w];
         }
       }
 #pragma unroll
@@ -200,7 +297,7 @@ struct JoinLds {                   // of the W waves of a block: they take tiles
 
 // Keys of tiles t0 .. t1 - 1 for the rows of `r` and head h; the waves' parts are joined and leave as results, or as a part of
 // them (part != nullptr): [rows_cap][D] sums, then [rows_cap][2] maximum and sum.
-template <class T, int D, int MB, int W>
+template <class T, int D, int MB, int W, bool ONE>
 __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTile& r, int h, int t0, int t1, float* part, int rows_cap, JoinLds<D, MB, W>& lds) {
   constexpr int S = D / 32, J = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, hi = lane >> 4;
@@ -225,6 +322,7 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
     if (queries_in_lds(D, MB)) __syncthreads();
     Attend<T, D, MB> at = {a.kv, a.s.table + (long)r.b * a.s.tstride, r.keys.lo >> a.kv.lps, max(r.keys.hi - 1, 0) >> a.kv.lps, h, l16, hi, {}};
     at.run(t0 + wave, t1, W, r.keys, r.clear, lim, low, q, lds.q, a.scale2, st);
+    if (!ONE && __builtin_expect(r.n > 1 && st.is_odd(), 0)) at.run_carefully(t0 + wave, t1, W, r.keys, r.clear, lim, low, q, lds.q, a.scale2, st);
   }
   // o and sum relative to the largest maximum of the waves
 #pragma unroll
@@ -272,8 +370,9 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
 // Two blocks on a CU where the registers allow it: 8 waves with 16 KB and more under way each
 constexpr int blocks_of(int D, int MB) { return MB * D <= 256 ? 2 : 1; }
 
-// A block for each tile of rows and key / value head
-template <class T, int D, int MB, int W>
+// A block for each tile of rows and key / value head.  ONE: no sequence brings more than one token, and the rows of a tile see the
+// same keys
+template <class T, int D, int MB, int W, bool ONE>
 __global__ __launch_bounds__(64 * W, blocks_of(D, MB)) void paged_rows_kernel(const PagedAttnArgs a) {
   __shared__ JoinLds<D, MB, W> lds;
   const int tile = blockIdx.x;
@@ -284,7 +383,7 @@ __global__ __launch_bounds__(64 * W, blocks_of(D, MB)) void paged_rows_kernel(co
     i0 = (tile - tile0(b)) * a.tpt;
   }
   const RowTile r = rows_of_sequence<tile_keys(D, MB)>(a, sequence(a.s, b), b, i0, a.tpt);
-  if (r.n > 0) attend_rows<T, D, MB, W>(a, r, blockIdx.y, r.t0, r.t0 + r.tiles, nullptr, 0, lds);
+  if (r.n > 0) attend_rows<T, D, MB, W, ONE>(a, r, blockIdx.y, r.t0, r.t0 + r.tiles, nullptr, 0, lds);
 }
 
 // Tiles of keys of all tiles of a sequence's rows, for one head; none where the sequence has more rows than are taken here
@@ -302,7 +401,7 @@ __device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) 
 struct First { int row0, n, h, last; };                              // first row, tokens (0: none was begun), head, block
 constexpr int kSplitW = 4;         // waves of a block
 __host__ __device__ constexpr long part_floats(long rows, int D) { return (rows * (D + 2) + 3) & ~3l; }    // 16-byte aligned
-template <class T, int D, int MB>
+template <class T, int D, int MB, bool ONE>
 __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
   __shared__ JoinLds<D, MB, kSplitW> lds;
   constexpr int KT = tile_keys(D, MB);
@@ -357,7 +456,7 @@ __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_ke
       begun = true;
       if (threadIdx.x == 0) first[p] = First{r.row0, r.n, h, min((x + at + r.tiles - 1) / share, a.blocks - 1)};
     }
-    if (r.n > 0) attend_rows<T, D, MB, kSplitW>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
+    if (r.n > 0) attend_rows<T, D, MB, kSplitW, ONE>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
     left -= n;
     at += n;
     t = 0;
@@ -446,14 +545,14 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) 
 
 constexpr int kSplitLeast = 4;     // tiles of a share: one for each wave
 
-template <class T, int D, int MB>
+template <class T, int D, int MB, bool ONE>
 static void rows_grid(PagedAttnArgs a, hipStream_t s) {
   a.tpt = 16 * MB / a.G;
   if (a.parts) {
     if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
     a.rows_cap = a.tpt * a.G;
     a.least = kSplitLeast;
-    hipLaunchKernelGGL((paged_split_kernel<T, D, MB>), dim3(a.blocks), dim3(64 * kSplitW), 0, s, a);
+    hipLaunchKernelGGL((paged_split_kernel<T, D, MB, ONE>), dim3(a.blocks), dim3(64 * kSplitW), 0, s, a);
     hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
     return;
   }
@@ -462,16 +561,17 @@ static void rows_grid(PagedAttnArgs a, hipStream_t s) {
   const dim3 grid(tiles, a.kv.heads);
   if constexpr (blocks_of(D, MB) == 2)
     if (a.waves == 8) {
-      hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 8>), grid, dim3(512), 0, s, a);
+      hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 8, ONE>), grid, dim3(512), 0, s, a);
       return;
     }
-  hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 4>), grid, dim3(256), 0, s, a);
+  hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 4, ONE>), grid, dim3(256), 0, s, a);
 }
 template <class T, int D>
 static void rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
-  if (mb == 1) rows_grid<T, D, 1>(a, s);
-  else if (mb == 2) rows_grid<T, D, 2>(a, s);
-  else rows_grid<T, D, 4>(a, s);
+  if (mb == 1 && a.max_new == 1) rows_grid<T, D, 1, true>(a, s);
+  else if (mb == 1) rows_grid<T, D, 1, false>(a, s);
+  else if (mb == 2) rows_grid<T, D, 2, false>(a, s);
+  else rows_grid<T, D, 4, false>(a, s);
 }
 
 // Blocks of whole (tile of rows, head)s walk the longest sequence, which a CU reads at 60 to 70 GB/s; shared out, the keys take

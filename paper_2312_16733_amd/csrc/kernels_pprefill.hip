@@ -195,6 +195,73 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
 #pragma unroll
       for (int j = 0; j < J; ++j) o[j] = T::mma32(*(const u32x4*)(vt + j * (32 * 128) + v_at[s ^ 2 * (j & 1)]), p[s], o[j]);
   }
+  // The same again, at leisure and straight from the pages, for a wave whose sums are no numbers: see `Odd`
+  float left = 0.f;                                                  // 0 x is 0 for a number, and only then
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) left = fmaf(o[j][i], 0.f, left);
+  if (__builtin_expect(__any(left != 0.f), 0)) {
+    top = -INFINITY;
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+#pragma unroll 1
+    for (int key0 = t0 * PF_K; key0 < t1 * PF_K; key0 += 32) {
+      const int row = key0 + key_of;
+      const char* k = a.kv.k + in_pool(page(row)) * a.kv.kstride + ((long)h * ps + (row & (ps - 1))) * (D * 2) + hi * 16;
+      f32x16 sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+      for (int s = 0; s < S; ++s) sc = T::mma32(*(const u32x4*)(k + s * 32), q[s], sc);
+      float x = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = key0 + 16 * (i >> 3) + 8 * hi + (i & 7);
+        sc[i] = key <= lim && key >= low ? sc[i] : -INFINITY;
+        x = fmaxf(x, sc[i]);
+      }
+      const float now = fmaxf(top, max_of_2(x)), ref = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f((top - ref) * a.scale2);
+      top = now;
+      sum *= keep;
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[j][i] *= keep;
+#pragma unroll 1
+      for (int s = 0; s < 2; ++s) {
+        f32x8 e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(((s ? sc[8 + i] : sc[i]) - ref) * a.scale2);
+          sum += e[i];
+        }
+        const u32x4 p = to_16<T>(e);
+        const int key = key0 + 16 * s + 8 * hi;
+        const char* vp = a.kv.v + in_pool(page(key)) * a.kv.vstride + (((long)h * D + l32) * ps + (key & (ps - 1))) * 2;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          u32x4 v = *(const u32x4*)(vp + (long)j * 64 * ps);
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            v[w] &= (key + 2 * w >= first && key + 2 * w <= last ? 0xffffu : 0u) | (key + 2 * w + 1 >= first && key + 2 * w + 1 <= last ? 0xffff0000u : 0u);
+          o[j] = T::mma32(without_odd<T>(v), p, o[j]);
+#pragma unroll 1
+          for (int kind = 0; kind < ODD_KINDS; ++kind) {
+            f32x16 n;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) n[i] = 0.f;
+            n = T::mma32(ones_where_odd<T>(v, kind), ones_where_seen<T>(key, low, lim), n);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[j][i] += odd_sum(n[i] > 0.f, kind);
+          }
+        }
+      }
+    }
+  }
   sum = sum_of_2(sum);
   if (!mine) return;
   if (a.splits > 1) {                                                // a part: sums, then maximum and sum

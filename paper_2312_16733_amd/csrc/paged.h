@@ -11,6 +11,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
 // Element types: eight of them are one 16-byte access and one operand of the matrix instructions.
 struct Bf16 {
+  static constexpr unsigned kInf = 0x7f80u, kOne = 0x3f80u;
   typedef __attribute__((ext_vector_type(8))) __bf16 v8;
   typedef __attribute__((ext_vector_type(4))) __bf16 v4;
   static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {     // 16 x 16 += 16 x 32 by 32 x 16
@@ -27,6 +28,7 @@ struct Bf16 {
   }
 };
 struct Fp16 {
+  static constexpr unsigned kInf = 0x7c00u, kOne = 0x3c00u;
   typedef __attribute__((ext_vector_type(8))) _Float16 v8;
   typedef __attribute__((ext_vector_type(4))) _Float16 v4;
   static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
@@ -46,6 +48,44 @@ template <class T>
 __device__ __forceinline__ f32x8 to_f32(u32x4 u) { return __builtin_convertvector(__builtin_bit_cast(typename T::v8, u), f32x8); }
 template <class T>
 __device__ __forceinline__ u32x4 to_16(f32x8 x) { return __builtin_bit_cast(u32x4, __builtin_convertvector(x, typename T::v8)); }   // to the nearest, ties to even
+
+// Values that are no numbers, where the rows of a product differ in the keys they see: 0 * inf is not 0, so that such a value
+// would reach rows that do not see its key.  They are taken out of the product, and counted for the rows that do see them by
+// products of ones.  All of it happens in a second pass over the keys, of waves whose sums come out as no numbers: in the first,
+// a look at the values of such tiles alone cost 4 to 11 % of a chunk.
+enum Odd { ODD_NAN, ODD_INF, ODD_MINUS_INF, ODD_KINDS };
+// In integers throughout: a comparison for each of a wave's values would take the scalar registers of the ordinary case.
+__device__ __forceinline__ int ones_if_zero(int x) { return (x - 1) >> 31; }             // all ones, for x >= 0
+template <class T>
+__device__ __forceinline__ u32x4 without_odd(u32x4 v) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    v[w] &= ~((unsigned)ones_if_zero((int)(~v[w] & T::kInf)) & 0xffffu) & ~((unsigned)ones_if_zero((int)(~v[w] >> 16 & T::kInf)) << 16);
+  return v;
+}
+template <class T>
+__device__ __forceinline__ unsigned one_if_odd(unsigned h, int kind) {
+  const int m = kind == ODD_NAN ? ((int)T::kInf - (int)(h & 0x7fffu)) >> 31 : ones_if_zero((int)(h ^ (kind == ODD_INF ? T::kInf : T::kInf | 0x8000u)));
+  return (unsigned)m & T::kOne;
+}
+template <class T>
+__device__ __forceinline__ u32x4 ones_where_odd(u32x4 v, int kind) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v[w] = one_if_odd<T>(v[w] & 0xffffu, kind) | one_if_odd<T>(v[w] >> 16, kind) << 16;
+  return v;
+}
+// Ones for the keys of key .. key + 7 that a row sees
+template <class T>
+__device__ __forceinline__ u32x4 ones_where_seen(int key, int low, int lim) {
+  u32x4 v;
+  const auto one = [&](int k) { return (unsigned)(~((k - low) | (lim - k)) >> 31) & T::kOne; };
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v[w] = one(key + 2 * w) | one(key + 2 * w + 1) << 16;
+  return v;
+}
+__device__ __forceinline__ float odd_sum(bool some, int kind) {      // what they add
+  return some ? kind == ODD_NAN ? __builtin_nanf("") : kind == ODD_INF ? INFINITY : -INFINITY : 0.f;
+}
 
 // The rows of a step.  Sequence b brings rows starts[b] .. starts[b + 1] - 1; with them lens[b] of its tokens are cached.
 // The arrays are the device's: what they hold is not known to the host, so every use below is clamped to what the host

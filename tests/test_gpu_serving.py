@@ -361,3 +361,62 @@ def test_attention_of_mixed_steps(dtype, heads, page, seqs, window):
     a = sna.paged_attention(cache, batch, s["q"], window=window, workspace=workspace)
     within(a, want, err, "out")
     assert torch.equal(sna.paged_attention(cache, batch, s["q"], window=window), a)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,seqs,window", [((8, 2, 128), [(100, 4), (70, 1)], 0), ((4, 4, 64), [(300, 16), (50, 50)], 9), ((8, 2, 64), [(90, 30)], 0),
+                                               ((8, 1, 128), [(3000, 2500), (100, 64)], 0), ((32, 8, 64), [(2100, 2000)], 100), ((16, 16, 128), [(700, 600), (80, 2)], 0)])
+def test_attention_of_values_that_are_no_numbers(dtype, heads, seqs, window):
+    """Infinities and NaN in values and keys reach the tokens that see them, and no others."""
+    s = ref.make(seqs, *heads, 16, ref.DT[dtype], seed=17)
+    want, err = ref.attention(s, window)                               # as if they were not there
+    bad = torch.zeros_like(want, dtype=torch.bool)
+    row = 0
+    for b, (l, n) in enumerate(seqs):
+        for back, dim, value in ((2, 3, float("nan")), (n // 2 + 1, 17, float("inf")), (n - 1, 40, -float("inf")), (min(l - 1, n + 20), 41, float("inf"))):
+            p = l - 1 - back                                           # its position
+            if not 0 <= p < l:
+                continue
+            s["v_pages"][s["table"][b, p // 16].long(), 0, dim, p % 16] = value
+            for i in range(n):
+                q = l - n + i
+                if p <= q and (not window or p > q - window):
+                    bad[row + i, : heads[0] // heads[1], dim] = True
+        row += n
+    cache, batch = parts(s)
+    out = sna.paged_attention(cache, batch, s["q"], window=window).double()
+    assert not torch.isfinite(out[bad]).any()
+    off = (out - want).abs()
+    assert (off <= err)[~bad].all(), ((off > err) & ~bad).nonzero()[:5]
+    for b, (l, n) in enumerate(seqs):                                  # a key of NaN: whole rows, of the tokens that see it
+        s["k_pages"][s["table"][b, (l - 1) // 16].long(), 0, (l - 1) % 16, 5] = float("nan")
+    out = sna.paged_attention(cache, batch, s["q"], window=window).double()
+    ends = [sum(n for _, n in seqs[: b + 1]) - 1 for b in range(len(seqs)) if seqs[b][1]]
+    assert torch.isnan(out[ends][:, : heads[0] // heads[1]]).all()
+    rest = ~bad
+    rest[ends, : heads[0] // heads[1]] = False
+    assert ((out - want).abs() <= err)[rest].all()
+
+
+# Whatever launch a step gets: 16, 32 or 64 rows a block; keys shared out or walked whole by 4 or 8 waves; chunks of 128 or 256 rows
+# a block, their keys whole or in shares
+LAUNCHES = {
+    "16 rows": ((8, 2), [(300, 1), (65, 4), (1, 1)]), "16 rows, 8 waves": ((8, 2), [(900 + 7 * i, 1 + i % 4) for i in range(20)]),
+    "16 rows, shared": ((8, 2), [(5000, 4), (2100, 1), (3, 2)]), "16 rows, many": ((4, 4), [(2100 + i, 1) for i in range(150)]),
+    "32 rows": ((20, 2), [(300, 3), (65, 1), (70, 2)]), "32 rows, 8 waves": ((20, 2), [(990 + i, 3) for i in range(20)]), "32 rows, shared": ((20, 2), [(5000, 3), (2100, 1), (3, 2)]),
+    "64 rows": ((40, 1), [(300, 3), (65, 1), (70, 2)]), "64 rows, 8 waves": ((64, 1), [(990 + i, 1) for i in range(40)]), "64 rows, shared": ((64, 1), [(5000, 3), (2100, 1), (3, 2)]),
+    "several tiles": ((8, 2), [(300, 100), (40, 40), (200, 1)]), "several tiles, shared": ((8, 2), [(4200, 100), (40, 40), (2000, 1)]),
+    "128-row chunks": ((8, 2), [(4000 + i, 31) for i in range(32)]), "256-row chunks": ((16, 2), [(3000, 1500), (1200, 1200), (900, 100)]),
+    "chunks, shared": ((4, 1), [(9000, 2000)]), "chunks and single tokens": ((16, 2), [(3000, 1500), (2500, 1), (1800, 2)])}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("window", [0, 777])
+@pytest.mark.parametrize("launch", LAUNCHES)
+def test_attention_in_every_launch(launch, window, dim, dtype):
+    heads, seqs = LAUNCHES[launch]
+    s = ref.make(seqs, *heads, dim, 32, ref.DT[dtype], seed=18)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, window)
+    within(sna.paged_attention(cache, batch, s["q"], window=window), want, err, "out")
