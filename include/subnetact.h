@@ -387,7 +387,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
 
 /* out = softmax(scale * q k^T) v over each sequence's cached keys, causal: a token of position p sees the
  * keys of positions p - window + 1 .. p (window 0: all up to p).  Query head i reads key / value head
- * i / (q_heads / kv_heads); scale is positive.  Statistics and sums are fp32, the probabilities of a product are rounded to
+ * i / (q_heads / kv_heads); scale is positive.  Statistics and sums are fp32, the probabilities of a product are rounded (at most) to
  * the element type, the result once more.  A token that sees no key (its position is negative) gives zeros.
  * Slots that no visible key of the sequence lies in may hold anything; a value that is no number reaches the tokens that see
  * its key and no others.

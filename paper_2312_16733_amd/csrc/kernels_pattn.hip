@@ -60,6 +60,7 @@ constexpr bool queries_in_lds(int D, int MB) { return MB * D > 128; }
 template <class T, int D, int MB>
 struct Attend {
   static constexpr int S = D / 32, J = D / 16, KT = tile_keys(D, MB), U = KT / 32;
+  static constexpr bool PRECISE = MB == 1;
   const PagedKV kv;
   const int* table;                // the sequence's
   int c_lo, c_hi, h, l16, hi;
@@ -192,7 +193,7 @@ struct Attend {
     find(t0 + step);
     for (int t = t0; t < t1; t += step) {
       const bool more = t + step < t1;
-      u32x4 p[MB][U];
+      u32x4 p[MB][U], p_rest[MB][U];
       int lane = hi * 16 + l16;
 #if defined(__HIP_DEVICE_COMPILE__)
       if (queries_in_lds(D, MB)) asm volatile("" : "+v"(lane));        // read anew for each tile, not kept in registers
@@ -243,7 +244,10 @@ struct Attend {
             e[i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i >> 2][i & 3], scale2, -ref));
             st.sum[m] += e[i];
           }
-          p[m][u] = to_16<T>(e);                                     // off by half a step of the operand type
+          // the operand type, and what it leaves over in a second operand: the bytes of the cache bound these launches, not
+          // its products, and rounded once p would be off by as much as the result's own rounding
+          p[m][u] = to_16<T>(e);
+          if (PRECISE) p_rest[m][u] = to_16<T>(e - to_f32<T>(p[m][u]));
         }
       }
       if (t * KT < keys.lo || t * KT + KT > keys.hi) {               // slots that hold no key may hold anything: 0 * NaN is not 0
@@ -261,7 +265,10 @@ struct Attend {
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-          for (int u = 0; u < U; ++u) st.o[m][j] = T::mma16(v[u][j], p[m][u], st.o[m][j]);
+          for (int u = 0; u < U; ++u) {
+            st.o[m][j] = T::mma16(v[u][j], p[m][u], st.o[m][j]);
+            if (PRECISE) st.o[m][j] = T::mma16(v[u][j], p_rest[m][u], st.o[m][j]);
+          }
       if (more) load_v(t + step, now, v);
     }
   }
