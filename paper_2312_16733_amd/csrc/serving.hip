@@ -36,9 +36,11 @@ static sna_status check_batch(const sna_paged_batch* b) {
   return SNA_OK;
 }
 
-static sna_status check_heads(const sna_paged_cache* c, int32_t q_heads) {
+static sna_status check_heads(const sna_paged_cache* c, const sna_paged_batch* b, int32_t q_heads) {
   if (q_heads < 1 || q_heads % c->kv_heads || q_heads / c->kv_heads > 64)
     return fail(SNA_E_CFG_RANGE, "%d query heads over %d key / value heads (a multiple, up to 64 times, is supported)", q_heads, c->kv_heads);
+  if (((int64_t)b->n_tokens + 2 * (int64_t)b->n_seqs) * q_heads > 1 << 30)         // blocks of a launch are fewer than these
+    return fail(SNA_E_CFG_RANGE, "%d tokens of %d sequences and %d heads are more than one step takes", b->n_tokens, b->n_seqs, q_heads);
   return SNA_OK;
 }
 
@@ -66,7 +68,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
                          int32_t rot_dim, int32_t interleaved, const float* q_norm_dev, const float* k_norm_dev, float eps,
                          void* hip_stream) {
   sna_status st;
-  if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, q_heads)) != SNA_OK) return st;
+  if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, batch, q_heads)) != SNA_OK) return st;
   if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16) return fail(SNA_E_CFG_RANGE, "rot_dim %d (a multiple of 16 up to head_dim is supported)", rot_dim);
   if (rot_dim && !inv_freq_dev) return fail(SNA_E_NULL, "inv_freq is NULL");
   if (!q_norm_dev != !k_norm_dev) return fail(SNA_E_NULL, "one of q_norm and k_norm is NULL");
@@ -94,7 +96,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
 
 int64_t sna_paged_attention_workspace_bytes(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, int32_t window) {
   sna_status st;
-  if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, q_heads)) != SNA_OK) return st;
+  if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, batch, q_heads)) != SNA_OK) return st;
   if (window < 0) return fail(SNA_E_CFG_RANGE, "window %d", window);
   if (batch->n_seqs == 0 || batch->n_tokens == 0) return 0;
   return (int64_t)paged_attention_workspace(batch->n_seqs, batch->n_tokens, cache->kv_heads, q_heads / cache->kv_heads, batch->max_new, batch->max_len, window, cache->head_dim);

@@ -8,7 +8,7 @@
 
 Rows are the new tokens of all sequences of a step, one after the other.  Nothing here reads device memory or waits for it;
 `PagedBatch.validate` does, for a caller in doubt about what its arrays hold.  Every call enqueues on the current stream, or on
-`stream` (a torch stream or a raw handle), which its outputs and workspace then belong to.
+`stream` (a torch stream or a raw handle), which its outputs and workspace then belong to.  No gradients: these are serving steps.
 """
 import torch
 

@@ -50,6 +50,7 @@ def test_caches_and_batches_are_refused(call):
         assert call(b=batch(**bad)) == status, bad
     for heads in (0, 3, -2, 130):
         assert call(heads=heads) == RANGE, heads
+    assert call(b=batch(n_seqs=1 << 20, n_tokens=1 << 26, max_new=1 << 10, max_len=1 << 10), heads=128) == RANGE      # more blocks than a launch has
 
 
 def test_rows_are_refused():
