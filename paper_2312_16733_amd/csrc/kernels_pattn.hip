@@ -613,9 +613,14 @@ static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
   const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
   AttnPlan p = {};
   if (rows <= 64 || (long)n_tokens * group * kv_heads * keys <= kFewScores) {
+    const auto units_of = [&](int mb) { return (n_tokens / std::max(16 * mb / group, 1) + n_seqs) * (long)kv_heads; };
     p.mb = rows <= 16 ? 1 : group <= 32 ? 2 : 4;
+    // Chunks with heads of 64: 64 rows a block instead of 32, which takes 1.45 times as long, where that saves rounds of a block on
+    // each CU (500 tokens and 7 single ones, 4 heads: 15.6 and 17.4 us; 600 of 8 sequences and 56: 31 and 44; 500 of 12 heads: 20.4
+    // and 16.9).  With heads of 128 there is no second block on a CU then, and 32 rows are faster throughout.
+    if (head_dim == 64 && rows > 64 && p.mb == 2 && (units_of(4) + 255) / 256 * 145 < (units_of(2) + 255) / 256 * 100) p.mb = 4;
     p.most = max_new;
-    const long units = (n_tokens / std::max(16 * p.mb / group, 1) + n_seqs) * (long)kv_heads, room = 256 * blocks_of(head_dim, p.mb), kt = tile_keys(head_dim, p.mb), tiles = (keys + kt - 1) / kt;
+    const long units = units_of(p.mb), room = 256 * blocks_of(head_dim, p.mb), kt = tile_keys(head_dim, p.mb), tiles = (keys + kt - 1) / kt;
     p.waves = blocks_of(head_dim, p.mb) == 2 && units <= 256 && tiles * kt > 512 ? 8 : 4;
     const long whole = (units + room - 1) / room * ((tiles + p.waves - 1) / p.waves), shared = units * tiles * 6 / (10 * kSplitW * room);
     const bool split = (max_new * group <= 16 * p.mb ? keys * head_dim > (units <= 32 ? kSplitKeys / 2 : kSplitKeys) : whole - shared > kSplitGain * 64 / kt) && units * (tiles + 2) < 1l << 30;

@@ -147,6 +147,24 @@ def test_attention_without_keys_and_unused_rows():
     within(out[15:], want, err, "the others")
 
 
+def test_attention_of_chunks_without_keys():
+    """The same where the many-rows kernel takes the step; and steps without tokens, or sequences."""
+    s = ref.make([(1300, 1300), (700, 2), (0, 0)], 32, 8, 128, 16, torch.bfloat16, seed=19)
+    s["lens"][0] = 1200
+    cache, batch = parts(s)
+    out = torch.full_like(s["q"].contiguous(), 3.0)
+    sna.paged_attention(cache, batch, s["q"], out=out)
+    assert (out[:100] == 0).all()
+    t = dict(s, seqs=[(1200, 1200), (700, 2), (0, 0)], q=s["q"][100:])
+    want, err = ref.attention(t)
+    within(out[100:], want, err, "the others")
+    none = s["starts"] * 0
+    for b, n in ((sna.PagedBatch(none, s["lens"], s["table"], 1, 1300), 3), (sna.PagedBatch(none[:1], s["lens"][:0], s["table"][:0], 1, 1), 0)):
+        assert b.n_seqs == n
+        q = sna.kv_append(cache, b, s["q"][:0], s["k"][:0], s["v"][:0])
+        assert q.shape == (0, 32, 128) and sna.paged_attention(cache, b, q).shape == (0, 32, 128)
+
+
 @pytest.mark.parametrize("heads,seqs", [((8, 2, 128), [(100, 1), (60, 3)]), ((8, 2, 128), [(300, 90), (500, 1)])])
 def test_attention_with_bad_pages(heads, seqs):
     """Pages that are none, lengths beyond the table: whatever comes back for those sequences, the others are right."""
@@ -406,7 +424,7 @@ LAUNCHES = {
     "32 rows": ((20, 2), [(300, 3), (65, 1), (70, 2)]), "32 rows, 8 waves": ((20, 2), [(990 + i, 3) for i in range(20)]), "32 rows, shared": ((20, 2), [(5000, 3), (2100, 1), (3, 2)]),
     "64 rows": ((40, 1), [(300, 3), (65, 1), (70, 2)]), "64 rows, 8 waves": ((64, 1), [(990 + i, 1) for i in range(40)]), "64 rows, shared": ((64, 1), [(5000, 3), (2100, 1), (3, 2)]),
     "several tiles": ((8, 2), [(300, 100), (40, 40), (200, 1)]), "several tiles, shared": ((8, 2), [(4200, 100), (40, 40), (2000, 1)]),
-    "128-row chunks": ((8, 2), [(4000 + i, 31) for i in range(32)]), "256-row chunks": ((16, 2), [(3000, 1500), (1200, 1200), (900, 100)]),
+    "several tiles of 64 rows": ((16, 4), [(1500, 500), (900, 30)] + [(700, 1)] * 20), "128-row chunks": ((8, 2), [(4000 + i, 31) for i in range(32)]), "256-row chunks": ((16, 2), [(3000, 1500), (1200, 1200), (900, 100)]),
     "chunks, shared": ((4, 1), [(9000, 2000)]), "chunks and single tokens": ((16, 2), [(3000, 1500), (2500, 1), (1800, 2)])}
 
 
