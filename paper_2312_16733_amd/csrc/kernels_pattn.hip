@@ -606,7 +606,7 @@ struct AttnPlan {
   int waves;                       // of a block that walks all keys of its rows
   int most;                        // tokens of a sequence up to which it takes it
   bool chunks;                     // the many-rows kernel takes the other sequences
-  int splits;                      // shares of their keys
+  ChunkPlan chunk;
   size_t parts, chunk_parts;       // bytes of the workspace, for either
 };
 static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
@@ -627,8 +627,8 @@ static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
     if (split) p.blocks = split_blocks(head_dim, p.mb, units);
   } else {
     p.chunks = true;
-    p.splits = paged_chunk_splits(n_tokens, kv_heads, group, max_new, keys);
-    if (p.splits > 1) p.chunk_parts = (size_t)p.splits * n_tokens * kv_heads * group * (head_dim + 2) * sizeof(float);
+    p.chunk = plan_of_chunks(n_tokens, kv_heads, group, max_new, keys, head_dim);
+    if (p.chunk.splits > 1) p.chunk_parts = (size_t)p.chunk.splits * n_tokens * kv_heads * group * (head_dim + 2) * sizeof(float);
     if (n_seqs > 1 && (long)n_seqs * max_new != n_tokens && group <= 16 && n_seqs * (long)kv_heads * ((keys >> 5) + 2) < 1l << 30) {    // there may be sequences of few rows
       p.mb = 1;
       p.blocks = split_blocks(head_dim, 1, n_seqs * (long)kv_heads);
@@ -656,7 +656,8 @@ hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int 
     else head_dim == 64 ? rows_of<Bf16, 64>(r, p.mb, s) : rows_of<Bf16, 128>(r, p.mb, s);
   }
   if (!p.chunks) return hipGetLastError();
-  a.splits = p.splits;
+  a.waves = p.chunk.waves;
+  a.splits = p.chunk.splits;
   a.parts = (char*)workspace + p.parts;
   return launch_paged_chunks(a, dtype, head_dim, s);
 }

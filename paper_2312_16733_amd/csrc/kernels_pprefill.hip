@@ -289,51 +289,62 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
     }
 }
 
-// The parts of a token's rows joined: a block for each token, four dims a thread
+// The parts of a token's rows joined: four dims a thread, all of a token's over gridDim.y blocks, four parts under way
 template <class T, int D>
 __global__ __launch_bounds__(256) void paged_chunk_join_kernel(const PagedAttnArgs a) {
-  const int t = blockIdx.x, b = last_at_most(a.s.B, t, [&](int i) { return clamped(a.s.starts[i], 0, a.s.T); });
+  constexpr int U = 4;
+  const int t = blockIdx.x, heads = a.kv.heads * a.G, i = blockIdx.y * 256 + threadIdx.x, h = i / (D / 4), d = i % (D / 4) * 4;
+  const int b = last_at_most(a.s.B, t, [&](int k) { return clamped(a.s.starts[k], 0, a.s.T); });
   const Seq sq = sequence(a.s, b);
-  if (t >= sq.row0 + sq.n || sq.n <= a.most) return;                 // nobody's row, or one that the other kernel has written
-  const int heads = a.kv.heads * a.G;
-  const long step = (long)a.s.T * heads;
+  if (t >= sq.row0 + sq.n || sq.n <= a.most || h >= heads) return;   // nobody's row, or one that the other kernel has written
+  const long step = (long)a.s.T * heads, r = (long)t * heads + h;
   const float* parts = (const float*)a.parts;
   const float2* stats = (const float2*)(parts + a.splits * step * D);
-  for (int i = threadIdx.x; i < heads * (D / 4); i += 256) {
-    const int h = i / (D / 4), d = i % (D / 4) * 4;
-    const long r = (long)t * heads + h;
-    float top = -INFINITY;
-    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, stats[p * step + r].x);
-    if (top == -INFINITY) top = 0.f;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int p = 0; p < a.splits; ++p) {
-      const float2 st = stats[p * step + r];
-      if (st.y == 0.f) continue;                                     // no key of it is seen, and its sums are not written
-      const float w = __builtin_amdgcn_exp2f(st.x - top);
-      x += *(const f32x4*)(parts + (p * step + r) * D + d) * w;
-      sum += st.y * w;
+  float top = -INFINITY, sum = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < a.splits; p0 += U) {
+    f32x4 y[U];
+    float2 st[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long at = min(p0 + u, a.splits - 1) * step + r;
+      st[u] = stats[at];
+      y[u] = *(const f32x4*)(parts + at * D + d);
     }
-    x *= sum == 0.f ? 0.f : 1.f / sum;
-    *(uint2*)(a.o + t * a.o_t + h * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p0 + u < a.splits && st[u].y != 0.f) {                     // 0: no key of the part is seen, and its sums are not written
+        const float now = fmaxf(top, st[u].x), ref = now == -INFINITY ? 0.f : now;
+        const float keep = __builtin_amdgcn_exp2f(top - ref), w = __builtin_amdgcn_exp2f(st[u].x - ref);
+        x = x * keep + y[u] * w;
+        sum = sum * keep + st[u].y * w;
+        top = now;
+      }
   }
+  x *= sum == 0.f ? 0.f : 1.f / sum;
+  *(uint2*)(a.o + t * a.o_t + h * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
 }
 
-// Rows of a block: 32 a wave, 8 waves, or 4 where no sequence has more of them
-static int chunk_waves(int max_new, int group) { return (long)max_new * group <= 128 ? 4 : 8; }
-
-// Shares of the keys.  A step of fewer blocks than the chip holds leaves CUs idle; with S shares it takes ceil(blocks S /
-// capacity) rounds of 1 / S of the time each, and writing and joining the parts costs some percent for each share.  A share
-// has 8 tiles of keys or more.
-int paged_chunk_splits(int n_tokens, int kv_heads, int group, int max_new, long keys) {
-  const int waves = chunk_waves(max_new, group);
-  const long tpt = 32 * waves / group, blocks = (n_tokens + tpt - 1) / tpt * kv_heads, room = 256 * (8 / waves);
-  if (blocks >= room) return 1;
-  int best = 1;
+// Waves of a block, of 32 rows each, and shares of the keys.  The time of a launch is taken to be its rounds of blocks times a
+// block's tiles times a tile, 2 us on a full CU (one block of 8 waves, or two of 4) and 1.5 for a lone block of 4, 1.24 and 1.18 with
+// heads of 64, and where the keys are shared a second launch and the parts, written and read at 4.5 TB/s.  A share has 4 tiles or
+// more.  Measured, 32 heads over 8 of 128: 512 tokens over 8192 keys in shares 81 us (162 by blocks of few rows), 300 in shares 57 (113),
+// 100 in shares 32 (68); four chunks of up to 500 over 2000 whole 68, in 4 shares 128.
+ChunkPlan plan_of_chunks(int n_tokens, int kv_heads, int group, int max_new, long keys, int head_dim) {
+  const long tiles = (keys + PF_K - 1) / PF_K, like = (n_tokens + max_new - 1) / max_new;                // sequences, if all were as long
+  const double tile_us = head_dim == 128 ? 2.0 : 1.24, lone_us = head_dim == 128 ? 1.5 : 1.18, part_us = (double)n_tokens * kv_heads * group * (head_dim + 2) * 8 / 4.5e6;
+  ChunkPlan best = {};
   double least = 1e30;
-  for (int s = 1; s <= 8 && (s == 1 || keys >= 8l * PF_K * s); ++s) {
-    const double cost = (double)((blocks * s + room - 1) / room) / s + 0.03 * (s - 1);
-    if (cost < least) { least = cost; best = s; }
+  for (int waves = 8; waves >= 4; waves -= 4) {
+    const long tpt = 32 * waves / group, blocks = like * ((max_new + tpt - 1) / tpt) * kv_heads, room = 256 * (8 / waves);
+    for (int s = 1; s <= 16 && (s == 1 || tiles >= 4 * s); ++s) {
+      const double one = waves == 4 && blocks * s <= 256 ? lone_us : tile_us;
+      const double us = (double)((blocks * s + room - 1) / room * ((tiles + s - 1) / s)) * one + (s > 1 ? 8 + s * part_us : 0.0);
+      if (us < least) {
+        least = us;
+        best = ChunkPlan{waves, s};
+      }
+    }
   }
   return best;
 }
@@ -343,11 +354,11 @@ static void chunk_grid(PagedAttnArgs a, hipStream_t s) {
   a.tpt = 32 * W / a.G;
   a.by_tpt = FastDiv::by(a.tpt);
   hipLaunchKernelGGL((paged_chunk_kernel<T, D, W>), dim3((a.s.T / a.tpt + a.s.B) * a.kv.heads * a.splits), dim3(64 * W), 0, s, a);
-  if (a.splits > 1) hipLaunchKernelGGL((paged_chunk_join_kernel<T, D>), dim3(a.s.T), dim3(256), 0, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((paged_chunk_join_kernel<T, D>), dim3(a.s.T, (a.kv.heads * a.G * (D / 4) + 255) / 256), dim3(256), 0, s, a);
 }
 template <class T, int D>
 static void chunk_of(const PagedAttnArgs& a, hipStream_t s) {
-  chunk_waves(a.max_new, a.G) == 4 ? chunk_grid<T, D, 4>(a, s) : chunk_grid<T, D, 8>(a, s);
+  a.waves == 4 ? chunk_grid<T, D, 4>(a, s) : chunk_grid<T, D, 8>(a, s);
 }
 
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) {

@@ -184,14 +184,15 @@ struct PagedAttnArgs {
   // filled by the launchers
   int most;                                      // tokens of a sequence up to which the few-rows kernel takes it, not the other
   void* parts;                                   // parts of sums, where the keys are shared out over blocks
-  int waves;                                     // few rows: of a block that walks all keys of its rows
+  int waves;                                     // of a block (few rows: of one that walks all keys of its rows)
   int tpt;                                       // tokens of a tile of rows
   FastDiv by_tpt;
   int rows_cap, least, blocks;                   // rows of a part; least tiles of a share; blocks that share
   int splits;                                    // many rows: shares of the keys
 };
 size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
-int paged_chunk_splits(int n_tokens, int kv_heads, int group, int max_new, long keys);
+struct ChunkPlan { int waves, splits; };         // waves of a block, shares of the keys
+ChunkPlan plan_of_chunks(int n_tokens, int kv_heads, int group, int max_new, long keys, int head_dim);
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
 
