@@ -19,9 +19,12 @@ namespace sna {
 
 // Keys of a wave's tile: 64, or 32 where more rows of sums would leave room in the registers for one block on a CU only
 constexpr int tile_keys(int D, int MB) { return MB * D > 128 ? 32 : 64; }
-// Scores of a step (rows, all heads, times keys) up to which this kernel is used for chunks, too: 60 tokens over 4096 keys, 32
-// heads (8 M) 27 us here and 46 with the many-rows kernel, 100 over 8192 (26 M) 74 and 65, 16 x 30 over 4096 (63 M) 102 and 78.
-constexpr long kFewScores = 24l << 20;
+// Scores of a step (rows, all heads, times keys) up to which this kernel is used for chunks, too, in us here and with the
+// many-rows kernel.  Heads of 64: 500 tokens over 2000 keys, 12 heads (12 M) 16.8 and 20.7; 32 x 40 over 1000, 16 heads (20 M)
+// 19.7 and 26.3.  Beside single tokens, which the many-rows kernel leaves to launches of their own: 200 over 2000, 32 heads, and
+// seven tokens (13 M) 39.7 and 46.0.  Chunks of one length of 128-wide heads: 60 over 4096, 32 heads (8 M) 27.2 and 24.2; 250 over
+// 2000, 40 heads (19 M) 41.5 and 30.9.
+constexpr long kFewScores = 24l << 20, kFewScoresEqual = 7l << 20;
 
 // One wave's statistics of MB x 16 rows: row of queries 16 m + lane % 16, element of o[m][j][c]: dim 16 j + 4 (lane / 16) + c
 template <int D, int MB>
@@ -611,8 +614,9 @@ struct AttnPlan {
 };
 static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
   const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
+  const bool equal = (long)n_seqs * max_new == n_tokens;               // all sequences bring max_new tokens
   AttnPlan p = {};
-  if (rows <= 64 || (long)n_tokens * group * kv_heads * keys <= kFewScores) {
+  if (rows <= 64 || (long)n_tokens * group * kv_heads * keys <= (equal && head_dim == 128 ? kFewScoresEqual : kFewScores)) {
     const auto units_of = [&](int mb) { return (n_tokens / std::max(16 * mb / group, 1) + n_seqs) * (long)kv_heads; };
     p.mb = rows <= 16 ? 1 : group <= 32 ? 2 : 4;
     // Chunks with heads of 64: 64 rows a block instead of 32, which takes 1.45 times as long, where that saves rounds of a block on
@@ -629,7 +633,7 @@ static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
     p.chunks = true;
     p.chunk = plan_of_chunks(n_tokens, kv_heads, group, max_new, keys, head_dim);
     if (p.chunk.splits > 1) p.chunk_parts = (size_t)p.chunk.splits * n_tokens * kv_heads * group * (head_dim + 2) * sizeof(float);
-    if (n_seqs > 1 && (long)n_seqs * max_new != n_tokens && group <= 16 && n_seqs * (long)kv_heads * ((keys >> 5) + 2) < 1l << 30) {    // there may be sequences of few rows
+    if (!equal && group <= 16 && n_seqs * (long)kv_heads * ((keys >> 5) + 2) < 1l << 30) {    // there may be sequences of few rows
       p.mb = 1;
       p.blocks = split_blocks(head_dim, 1, n_seqs * (long)kv_heads);
       p.most = 16 / group;
