@@ -438,3 +438,53 @@ def test_attention_in_every_launch(launch, window, dim, dtype):
     cache, batch = parts(s)
     want, err = ref.attention(s, window)
     within(sna.paged_attention(cache, batch, s["q"], window=window), want, err, "out")
+
+
+@pytest.mark.parametrize("heads,seqs", [((32, 8, 128), [(5000, 1), (3000, 1)]), ((8, 2, 64), [(4000, 5), (2500, 3)]), ((16, 2, 128), [(3000, 1500), (2500, 1)]), ((4, 1, 64), [(9000, 2000)])])
+def test_shared_keys_in_a_graph(heads, seqs):
+    """Launches that join parts, captured with their workspace and replayed between eager calls of the same step."""
+    s = ref.make(seqs, *heads, 16, torch.bfloat16, seed=21)
+    cache, batch = parts(s)
+    q = s["q"].contiguous()
+    eager = sna.paged_attention(cache, batch, q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = sna.paged_attention(cache, batch, q)
+    for i in range(3):
+        q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(i)).to(q))
+        eager = sna.paged_attention(cache, batch, q)
+        out.zero_()
+        graph.replay()
+        again = sna.paged_attention(cache, batch, q)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(again, eager)
+    want, err = ref.attention(dict(s, q=q))
+    within(out, want, err, "the last replay")
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    s = ref.make([(3000, 1), (40, 1)], 8, 2, 128, 16, torch.bfloat16, seed=22)
+    cache, batch = parts(s)
+    q, k, v = (s[n].contiguous() for n in "qkv")
+    inv = torch.ones(64, device="cuda")
+    bad = [lambda: sna.PagedCache(s["k_pages"], s["v_pages"].half()), lambda: sna.PagedCache(s["k_pages"][:, :, ::2], s["v_pages"][..., ::2]),
+           lambda: sna.PagedCache(s["k_pages"].cpu(), s["v_pages"]), lambda: sna.PagedBatch(s["starts"][:-1], s["lens"], s["table"], 1, 3000),
+           lambda: sna.PagedBatch(s["starts"].long(), s["lens"], s["table"], 1, 3000), lambda: sna.PagedBatch(s["starts"], s["lens"], s["table"].t(), 1, 3000),
+           lambda: sna.PagedBatch(s["starts"], s["lens"], s["table"], -1, 3000), lambda: sna.paged_attention(cache, batch, q.half()),
+           lambda: sna.paged_attention(cache, batch, q.cpu()), lambda: sna.paged_attention(cache, batch, q[..., :64]), lambda: sna.paged_attention(cache, batch, q[0]),
+           lambda: sna.paged_attention(cache, batch, q.transpose(1, 2).contiguous().transpose(1, 2)), lambda: sna.paged_attention(cache, batch, q, out=q[:1]),
+           lambda: sna.paged_attention(cache, batch, q, window=-1), lambda: sna.paged_attention(cache, batch, q, workspace=torch.empty(1 << 24, device="cuda")),
+           lambda: sna.kv_append(cache, batch, q, k[:1], v), lambda: sna.kv_append(cache, batch, q, k, q), lambda: sna.kv_append(cache, batch, q, k, v, inv_freq=inv.double()),
+           lambda: sna.kv_append(cache, batch, q, k, v, inv_freq=torch.ones(129, device="cuda")), lambda: sna.kv_append(cache, batch, q, k, v, q_norm=inv, k_norm=inv),
+           lambda: sna.verify_draft(torch.ones(2, 3, 9, device="cuda"), torch.zeros(2, 2, device="cuda"), torch.ones(2, 3, device="cuda")),
+           lambda: sna.verify_draft(torch.ones(2, 3, 9, device="cuda"), torch.zeros(2, 2, dtype=torch.int32, device="cuda"), torch.ones(2, 2, device="cuda")),
+           lambda: sna.verify_draft(torch.ones(2, 3, 9, device="cuda"), torch.zeros(2, 2, dtype=torch.int32, device="cuda"), torch.ones(2, 3, device="cuda"), draft_probs=torch.ones(2, 3, 9, device="cuda"))]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: sna.paged_attention(cache, batch, q, scale=-1.0), lambda: sna.paged_attention(cache, batch, q[:, :7]), lambda: sna.kv_append(cache, batch, q, k, v, inv_freq=inv[:3]),
+                 lambda: sna.kv_append(cache, batch, q, k, v, inv_freq=torch.ones(65, device="cuda")), lambda: sna.kv_append(cache, batch, q, k, v, q_norm=torch.ones(128, device="cuda"))):
+        with pytest.raises(sna.SnaError):
+            call()
+    want, err = ref.attention(dict(s, q=q))
+    within(sna.paged_attention(cache, batch, q), want, err, "and what fits still runs")
