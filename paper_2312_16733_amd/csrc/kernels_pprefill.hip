@@ -6,8 +6,6 @@
 // Forming the next tile's scores among this one's exponentials was worth under 1 % (393 us), forced interleaving of products,
 // reads and vector instructions cost 2 %, four waves a block instead of eight 4 %.  As where rows are few, the scores are formed transposed: a lane has one row, and the keys of a product's 32
 // rows are chosen so (row 16 s + 8 a + 4 h + c is key 16 s + 8 h + 4 a + c) that its scores are what the second product wants.
-#include <algorithm>
-
 #include "paged.h"
 
 namespace sna {
