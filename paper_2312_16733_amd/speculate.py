@@ -47,10 +47,12 @@ class Decoder:
 
 
 def generate(model, prompts, n_new, drafts=4, depth=2, temperature=1.0, seed=0):
-    """Continues every prompt (a list of token lists) by at least n_new tokens.  Returns (token lists, share of drafts accepted, rounds)."""
+    """Continues every prompt (a list of token lists) by at least n_new tokens, and at most `drafts` more.  Returns (token lists, share
+    of drafts accepted, rounds).  A sequence that has its tokens leaves the step, so that its pages are bounded whatever the
+    others still need."""
     device, B, K = model.device, len(prompts), drafts
     g = torch.Generator(device=device).manual_seed(seed)
-    most = max(len(p) for p in prompts) + n_new + 2 * K + 2
+    most = max(len(p) for p in prompts) + n_new + K
     width = -(-most // PAGE)
     if B * width > model.k.shape[0]:
         raise ValueError(f"{B} sequences of up to {most} tokens need {B * width} pages, the pool has {model.k.shape[0]}")
@@ -64,26 +66,30 @@ def generate(model, prompts, n_new, drafts=4, depth=2, temperature=1.0, seed=0):
         starts = ints([0] + n).cumsum(0).int()
         model.forward(torch.tensor([t for p in prompts for t in p[:-1]], device=device), PagedBatch(starts, ints(n), table, max(n), max(n)))
     lens, last = ints(n), torch.tensor([p[-1] for p in prompts], device=device)
-    longest, done, taken, rounds = max(n), [list(p) for p in prompts], 0, 0
-    one, many = torch.arange(B + 1, dtype=torch.int32, device=device), torch.arange(B + 1, dtype=torch.int32, device=device) * (K + 1)
-    while min(len(d) - len(p) for d, p in zip(done, prompts)) < n_new:
+    done, drafted, taken, rounds = [list(p) for p in prompts], 0, 0, 0
+    at_work = list(range(B)) if n_new > 0 else []                      # lens, last and table hold these sequences
+    while at_work:
+        B, longest = len(at_work), max(len(done[b]) for b in at_work) - 1
+        one = torch.arange(B + 1, dtype=torch.int32, device=device)
         step, tokens, q = last, [last], []
         for i in range(K):
             q.append(probs(model.forward(step, PagedBatch(one, lens + (i + 1), table, 1, longest + i + 1), depth)))
             step = torch.multinomial(q[-1], 1, generator=g)[:, 0]
             tokens.append(step)
         rows = torch.stack(tokens, 1)
-        p = probs(model.forward(rows.flatten(), PagedBatch(many, lens + (K + 1), table, K + 1, longest + K + 1))).view(B, K + 1, -1)
+        p = probs(model.forward(rows.flatten(), PagedBatch(one * (K + 1), lens + (K + 1), table, K + 1, longest + K + 1))).view(B, K + 1, -1)
         out, accepted = verify_draft(p, rows[:, 1:].contiguous(), torch.rand(B, K + 1, generator=g, device=device), draft_probs=torch.stack(q, 1) if K else None)
         last = out.gather(1, accepted[:, None].long())[:, 0].long()
         lens = lens + accepted + 1
-        for d, row, a in zip(done, out.tolist(), accepted.tolist()):
-            d.extend(row[: a + 1])
+        for b, row, a in zip(at_work, out.tolist(), accepted.tolist()):
+            done[b].extend(row[: a + 1])
             taken += a
-        longest, rounds = max(len(d) for d in done) - 1, rounds + 1
-        if longest + K + 1 > width * PAGE:                             # a sequence of luckier drafts has used its pages up
-            break
-    return done, taken / max(rounds * B * K, 1), rounds
+        drafted, rounds = drafted + B * K, rounds + 1
+        left = [i for i, b in enumerate(at_work) if len(done[b]) - len(prompts[b]) < n_new]
+        if len(left) < B:
+            kept = torch.tensor(left, dtype=torch.long, device=device)
+            lens, last, table, at_work = lens[kept], last[kept], table[kept], [at_work[i] for i in left]
+    return done, taken / max(drafted, 1), rounds
 
 
 def main():
@@ -91,7 +97,7 @@ def main():
     for name, value in (("drafts", 4), ("depth", 2), ("seqs", 16), ("tokens", 128), ("prompt", 100)):
         a.add_argument("--" + name, type=int, default=value)
     a = a.parse_args()
-    model = Decoder(pages=a.seqs * (-(-(a.prompt + 2 * a.tokens + 4 * a.drafts) // PAGE) + 1))
+    model = Decoder(pages=a.seqs * -(-(a.prompt + a.tokens + a.drafts) // PAGE))
     g = torch.Generator().manual_seed(1)
     prompts = [torch.randint(0, model.vocab, (a.prompt - i % 7,), generator=g).tolist() for i in range(a.seqs)]
     for drafts in (0, a.drafts):
