@@ -17,6 +17,8 @@ namespace {
 
 PyObject* sna_error = nullptr;             // SnaError of the package
 
+// What the tensors were when the object was made.  A tensor can be given other memory or another shape in place (resize_, set_,
+// .data), so every call looks at them again and refuses what has changed.
 struct Cache {
   PyObject_HEAD
   PyObject *k_pages, *v_pages;
@@ -138,7 +140,7 @@ class On {
 };
 
 // ---- PagedCache, PagedBatch ------------------------------------------------------------------------------------------------
-int fill_cache(Cache* c, PyObject* ko, PyObject* vo) {
+int describe_cache(PyObject* ko, PyObject* vo, sna_paged_cache* c) {
   const at::Tensor *k = tensor_of(ko, "k_pages"), *v = k ? tensor_of(vo, "v_pages") : nullptr;
   if (!v) return 0;
   NEED(k->dim() == 4 && v->dim() == 4, "k_pages and v_pages have four dimensions");
@@ -151,12 +153,26 @@ int fill_cache(Cache* c, PyObject* ko, PyObject* vo) {
   NEED(n >= 1 && n <= INT32_MAX && h >= 1 && h <= 4096 && ps <= 1024 && d <= 1024, "k_pages: %s is out of range", shape_of(*k).c_str());
   NEED(k->stride(3) == 1 && k->stride(2) == d && (h == 1 || k->stride(1) == ps * d) && v->stride(3) == 1 && v->stride(2) == ps && (h == 1 || v->stride(1) == d * ps), "pages have to be dense");
   const int64_t dense = h * ps * d;
-  c->c = sna_paged_cache{k->data_ptr(), v->data_ptr(), n > 1 ? k->stride(0) : dense, n > 1 ? v->stride(0) : dense, (int32_t)n, (int32_t)h, (int32_t)ps, (int32_t)d,
-                         t == at::kHalf ? SNA_DTYPE_FP16 : SNA_DTYPE_BF16};
-  c->type = t;
-  c->device = new c10::Device(k->device());
+  *c = sna_paged_cache{k->data_ptr(), v->data_ptr(), n > 1 ? k->stride(0) : dense, n > 1 ? v->stride(0) : dense, (int32_t)n, (int32_t)h, (int32_t)ps, (int32_t)d,
+                       t == at::kHalf ? SNA_DTYPE_FP16 : SNA_DTYPE_BF16};
+  return 1;
+}
+int fill_cache(Cache* c, PyObject* ko, PyObject* vo) {
+  if (!describe_cache(ko, vo, &c->c)) return 0;
+  c->type = c->c.dtype == SNA_DTYPE_FP16 ? at::kHalf : at::kBFloat16;
+  c->device = new c10::Device(THPVariable_Unpack(ko).device());
   c->k_pages = Py_NewRef(ko);
   c->v_pages = Py_NewRef(vo);
+  return 1;
+}
+int is_current(const Cache* c) {
+  sna_paged_cache now;
+  if (!describe_cache(c->k_pages, c->v_pages, &now)) return 0;
+  const sna_paged_cache& was = c->c;
+  NEED(now.k_pages_dev == was.k_pages_dev && now.v_pages_dev == was.v_pages_dev && now.k_page_stride == was.k_page_stride && now.v_page_stride == was.v_page_stride &&
+           now.n_pages == was.n_pages && now.kv_heads == was.kv_heads && now.page_size == was.page_size && now.head_dim == was.head_dim && now.dtype == was.dtype &&
+           THPVariable_Unpack(c->k_pages).device() == *c->device,
+       "the pages were resized or replaced in place: a new PagedCache is needed");
   return 1;
 }
 PyObject* cache_new(PyTypeObject* type, PyObject* args, PyObject* kw) {
@@ -185,7 +201,7 @@ bool int32_on(const at::Tensor* t, const char* name, c10::Device device) {
   NEED(t->scalar_type() == at::kInt && t->device() == device, "%s: int32 on %s is needed, got %s", name, device.str().c_str(), shape_of(*t).c_str());
   return true;
 }
-int fill_batch(Batch* b, PyObject* so, PyObject* lo, PyObject* to, int64_t max_new, int64_t max_len) {
+int describe_batch(PyObject* so, PyObject* lo, PyObject* to, int64_t max_new, int64_t max_len, sna_paged_batch* b) {
   const at::Tensor *s = tensor_of(so, "starts"), *l = s ? tensor_of(lo, "lens") : nullptr, *t = l ? tensor_of(to, "page_table") : nullptr;
   if (!t) return 0;
   NEED(l->dim() == 1 && l->is_cuda(), "lens: one dimension on a GPU is needed, got %s", shape_of(*l).c_str());
@@ -195,12 +211,25 @@ int fill_batch(Batch* b, PyObject* so, PyObject* lo, PyObject* to, int64_t max_n
   NEED(t->dim() == 2 && t->size(0) == n, "page_table: %lld rows are needed, got %s", (long long)n, shape_of(*t).c_str());
   NEED((n <= 1 || l->stride(0) == 1) && (n == 0 || s->stride(0) == 1) && (t->size(1) <= 1 || t->stride(1) == 1), "starts, lens and the rows of page_table have to be dense");
   NEED(n <= INT32_MAX && t->size(1) <= INT32_MAX && max_new >= 0 && max_new <= INT32_MAX && max_len >= 0 && max_len <= INT32_MAX, "the batch is out of range");
-  b->c = sna_paged_batch{(const int32_t*)s->data_ptr(), (const int32_t*)l->data_ptr(), (const int32_t*)t->data_ptr(), t->stride(0), (int32_t)n, 0, (int32_t)t->size(1),
-                         (int32_t)max_new, (int32_t)max_len};
-  b->device = new c10::Device(l->device());
+  *b = sna_paged_batch{(const int32_t*)s->data_ptr(), (const int32_t*)l->data_ptr(), (const int32_t*)t->data_ptr(), t->stride(0), (int32_t)n, 0, (int32_t)t->size(1),
+                       (int32_t)max_new, (int32_t)max_len};
+  return 1;
+}
+int fill_batch(Batch* b, PyObject* so, PyObject* lo, PyObject* to, int64_t max_new, int64_t max_len) {
+  if (!describe_batch(so, lo, to, max_new, max_len, &b->c)) return 0;
+  b->device = new c10::Device(THPVariable_Unpack(lo).device());
   b->starts = Py_NewRef(so);
   b->lens = Py_NewRef(lo);
   b->page_table = Py_NewRef(to);
+  return 1;
+}
+int is_current(const Batch* b) {
+  sna_paged_batch now;
+  const sna_paged_batch& was = b->c;
+  if (!describe_batch(b->starts, b->lens, b->page_table, was.max_new, was.max_len, &now)) return 0;
+  NEED(now.starts_dev == was.starts_dev && now.lens_dev == was.lens_dev && now.page_table_dev == was.page_table_dev && now.table_stride == was.table_stride &&
+           now.n_seqs == was.n_seqs && now.table_width == was.table_width && THPVariable_Unpack(b->lens).device() == *b->device,
+       "starts, lens or page_table were resized or replaced in place: a new PagedBatch is needed");
   return 1;
 }
 PyObject* batch_new(PyTypeObject* type, PyObject* args, PyObject* kw) {
@@ -270,6 +299,7 @@ int step_of(Step* s, PyObject* cache, PyObject* batch, PyObject* q, PyObject* ou
   }
   s->cache = (Cache*)cache;
   const Batch* b = (Batch*)batch;
+  if (!is_current(s->cache) || !is_current(b)) return 0;
   NEED(*b->device == *s->cache->device, "the batch is on %s, the cache on %s", b->device->str().c_str(), s->cache->device->str().c_str());
   if (!(s->q = tensor_of(q, "q")) || !rows_of(*s->q, "q", -1, s->cache, &s->q_rows)) return 0;
   NEED(s->q->size(0) <= INT32_MAX && s->q->size(1) <= INT32_MAX, "q: %s is out of range", shape_of(*s->q).c_str());

@@ -26,7 +26,8 @@ kv_append, paged_attention, verify_draft = _serving.kv_append, _serving.paged_at
 class PagedCache(_serving.PagedCache):
     """PagedCache(k_pages, v_pages): one layer's pages, keys [pages][kv_heads][page_size][head_dim], values
     [pages][kv_heads][head_dim][page_size], bf16 or fp16, dense within a page; the layers of a pool may take turns (any stride
-    between pages).  Borrowed, not copied."""
+    between pages).  Borrowed, not copied: pages that are resized or replaced in place (resize_, set_, .data) need a new
+    PagedCache, which the calls say."""
     __slots__ = ()
 
 
@@ -34,7 +35,8 @@ class PagedBatch(_serving.PagedBatch):
     """PagedBatch(starts, lens, page_table, max_new, max_len): the sequences of one step.  starts int32 [n + 1]: sequence b
     brings rows starts[b] .. starts[b + 1] - 1 (none is fine); lens int32 [n]: its cached tokens once these are in; page_table
     int32 [n][width].  max_new and max_len bound the new tokens and the length of any sequence; they choose the launches, so
-    bounds near the truth are faster."""
+    bounds near the truth are faster.  Borrowed as the pages are: the arrays' contents may change from call to call, their
+    memory and shapes may not."""
     __slots__ = ()
 
     def validate(self, cache, n_tokens):

@@ -488,3 +488,46 @@ def test_tensors_that_do_not_fit_are_refused():
             call()
     want, err = ref.attention(dict(s, q=q))
     within(sna.paged_attention(cache, batch, q), want, err, "and what fits still runs")
+
+
+def test_tensors_that_were_replaced_in_place_are_refused():
+    """A cache or batch whose tensors were resized, or given other memory, since it was made: an error, and no launch."""
+    s = ref.make([(300, 2), (40, 1)], 8, 2, 64, 16, torch.bfloat16, seed=23)
+    q, k, v = (s[n].contiguous() for n in "qkv")
+
+    def refused(cache, batch):
+        for call in (lambda: sna.paged_attention(cache, batch, q), lambda: sna.kv_append(cache, batch, q, k, v)):
+            with pytest.raises(ValueError, match="in place|needed"):
+                call()
+
+    def grow(t):
+        t.resize_(t.shape[0] + 5, *t.shape[1:])
+
+    def swap(t):
+        t.data = t.clone()
+
+    def reset(t):
+        t.set_(torch.zeros_like(t))
+
+    def view(t):
+        t.data = t.cpu()
+
+    for change in (grow, swap, reset, view):
+        for name in ("k_pages", "v_pages"):
+            t = dict(s, k_pages=s["k_pages"].clone(), v_pages=s["v_pages"].clone())
+            cache, batch = parts(t)
+            change(t[name])
+            refused(cache, batch)
+        for name in ("starts", "lens", "table"):
+            t = dict(s, **{name: s[name].clone()})
+            cache, batch = parts(t)
+            change(t[name])
+            refused(cache, batch)
+    t = dict(s, table=s["table"].clone())
+    cache, batch = parts(t)
+    t["table"].resize_(2, t["table"].shape[1] - 1)                      # smaller: the memory stays
+    refused(cache, batch)
+    cache, batch = parts(s)
+    s["table"].add_(0)                                                  # other contents are no other tensor
+    want, err = ref.attention(dict(s, q=q))
+    within(sna.paged_attention(cache, batch, q), want, err, "and what has not changed still runs")
