@@ -27,7 +27,8 @@ static sna_status check_batch(const sna_paged_batch* b) {
   if (!b) return fail(SNA_E_NULL, "paged batch: NULL");
   if (b->n_seqs < 0 || b->n_seqs > (1 << 20) || b->n_tokens < 0 || b->n_tokens > (1 << 26))
     return fail(SNA_E_CFG_RANGE, "paged batch: %d sequences, %d tokens", b->n_seqs, b->n_tokens);
-  if (b->n_seqs == 0 || b->n_tokens == 0) return SNA_OK;             // no work
+  if (b->n_tokens == 0) return SNA_OK;                               // no work
+  if (b->n_seqs == 0) return fail(SNA_E_CFG_RANGE, "paged batch: %d tokens of no sequence", b->n_tokens);
   if (!b->starts_dev || !b->lens_dev || !b->page_table_dev) return fail(SNA_E_NULL, "paged batch: NULL starts, lens or page table");
   if (b->table_width < 1 || b->table_stride < 0 || b->table_stride > INT32_MAX) return fail(SNA_E_CFG_RANGE, "paged batch: page table of %d columns", b->table_width);
   if (b->max_new < 1 || b->max_new > b->n_tokens || (int64_t)b->max_new * b->n_seqs < b->n_tokens)
@@ -72,7 +73,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
   if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16) return fail(SNA_E_CFG_RANGE, "rot_dim %d (a multiple of 16 up to head_dim is supported)", rot_dim);
   if (rot_dim && !inv_freq_dev) return fail(SNA_E_NULL, "inv_freq is NULL");
   if (!q_norm_dev != !k_norm_dev) return fail(SNA_E_NULL, "one of q_norm and k_norm is NULL");
-  if (batch->n_seqs == 0 || batch->n_tokens == 0) return SNA_OK;
+  if (batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_rows(k, "k")) != SNA_OK || (st = check_rows(v, "v")) != SNA_OK ||
       (st = check_rows(q_out, "q_out")) != SNA_OK) return st;
   AppendArgs a = {};
@@ -98,7 +99,7 @@ int64_t sna_paged_attention_workspace_bytes(const sna_paged_cache* cache, const 
   sna_status st;
   if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, batch, q_heads)) != SNA_OK) return st;
   if (window < 0) return fail(SNA_E_CFG_RANGE, "window %d", window);
-  if (batch->n_seqs == 0 || batch->n_tokens == 0) return 0;
+  if (batch->n_tokens == 0) return 0;
   return (int64_t)paged_attention_workspace(batch->n_seqs, batch->n_tokens, cache->kv_heads, q_heads / cache->kv_heads, batch->max_new, batch->max_len, window, cache->head_dim);
 }
 
@@ -109,7 +110,7 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   const int64_t need = sna_paged_attention_workspace_bytes(cache, batch, q_heads, window);
   if (need < 0) return (sna_status)need;
   if (!(scale > 0.f && scale < INFINITY)) return fail(SNA_E_CFG_RANGE, "scale %g (a positive number is needed)", (double)scale);
-  if (batch->n_seqs == 0 || batch->n_tokens == 0) return SNA_OK;
+  if (batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_rows(out, "out")) != SNA_OK) return st;
   if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))
     return fail(SNA_E_WORKSPACE, "paged_attention: a workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);

@@ -83,6 +83,13 @@ def test_a_step_without_tokens_is_no_launch():
         assert append(b=batch(**none)) == 0 and attention(b=batch(**none)) == 0
 
 
+def test_tokens_without_sequences_are_refused():
+    """Rows that belong to nobody would come back as the allocator left them."""
+    for b in (batch(n_seqs=0), batch(n_seqs=0, n_tokens=1, max_new=1), batch(n_seqs=0, n_tokens=1, max_new=0, max_len=0)):
+        assert append(b=b) == RANGE and attention(b=b) == RANGE
+        assert sna.lib().sna_paged_attention_workspace_bytes(cache(), b, 4, 0) == RANGE
+
+
 def test_tensors_are_refused():
     k, v = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 64, 16, dtype=torch.bfloat16)
     for bad in ((k[0], v), (k, k), (k, v.half()), (k.float(), v.float()), (k, v)):                   # the last: not on a GPU
