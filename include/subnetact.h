@@ -351,7 +351,8 @@ int64_t sna_profile_read_launches(sna_supernet* net, char* buf, int64_t cap);
  *
  * Calls are stateless, enqueue on `hip_stream` and may be captured into a graph (the sizes and bounds
  * are the graph's, the arrays' contents are read by every replay).  Device pointers of rows and pages
- * are aligned to 16 bytes and their strides, in elements, are multiples of 8. */
+ * are aligned to 16 bytes and their strides, in elements, are multiples of 8.  Rows that are written do
+ * not overlap (SNA_E_CFG_RANGE); rows that are read may. */
 typedef struct {
   void* k_pages_dev;              /* [n_pages][kv_heads][page_size][head_dim], dense within a page */
   void* v_pages_dev;              /* [n_pages][kv_heads][head_dim][page_size]: transposed, as the matrix operand reads it */

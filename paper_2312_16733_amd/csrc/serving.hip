@@ -51,6 +51,20 @@ static sna_status check_rows(const sna_rows* r, const char* name) {
   return SNA_OK;
 }
 
+// Rows that are written: none shares an element with another.  Of tokens and heads one changes fastest, and the other steps over
+// all of its rows (so it is for every slice and transposition of a dense tensor).
+static sna_status check_out(const sna_rows* r, const char* name, int64_t tokens, int64_t heads, int64_t dim) {
+  const sna_status st = check_rows(r, name);
+  if (st != SNA_OK) return st;
+  typedef __int128 wide;                                             // strides are any 64-bit numbers
+  const wide far = (wide)1 << 100, ts = r->token_stride, hs = r->head_stride;
+  const wide t = tokens == 1 ? far : ts < 0 ? -ts : ts, h = heads == 1 ? far : hs < 0 ? -hs : hs;
+  const wide inner = t < h ? t : h, outer = t < h ? h : t, rows = t < h ? tokens : heads;
+  if (inner < dim || (outer != far && outer < inner * (rows - 1) + dim))
+    return fail(SNA_E_CFG_RANGE, "%s: rows overlap", name);
+  return SNA_OK;
+}
+
 static PagedSeqs seqs_of(const sna_paged_batch* b) {
   return PagedSeqs{b->starts_dev, b->lens_dev, b->page_table_dev, b->n_seqs, b->n_tokens, b->table_width < (1 << 20) ? b->table_width : 1 << 20, (int)b->table_stride, b->max_len};   // 2^30 slots
 }
@@ -75,7 +89,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
   if (!q_norm_dev != !k_norm_dev) return fail(SNA_E_NULL, "one of q_norm and k_norm is NULL");
   if (batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_rows(k, "k")) != SNA_OK || (st = check_rows(v, "v")) != SNA_OK ||
-      (st = check_rows(q_out, "q_out")) != SNA_OK) return st;
+      (st = check_out(q_out, "q_out", batch->n_tokens, q_heads, cache->head_dim)) != SNA_OK) return st;
   AppendArgs a = {};
   a.s = seqs_of(batch);
   a.s.max_len = 1 << 30;                                             // a token is stored at its place, or nowhere
@@ -111,7 +125,7 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   if (need < 0) return (sna_status)need;
   if (!(scale > 0.f && scale < INFINITY)) return fail(SNA_E_CFG_RANGE, "scale %g (a positive number is needed)", (double)scale);
   if (batch->n_tokens == 0) return SNA_OK;
-  if ((st = check_rows(q, "q")) != SNA_OK || (st = check_rows(out, "out")) != SNA_OK) return st;
+  if ((st = check_rows(q, "q")) != SNA_OK || (st = check_out(out, "out", batch->n_tokens, q_heads, cache->head_dim)) != SNA_OK) return st;
   if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))
     return fail(SNA_E_WORKSPACE, "paged_attention: a workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
   PagedAttnArgs a = {};

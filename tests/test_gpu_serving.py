@@ -531,3 +531,19 @@ def test_tensors_that_were_replaced_in_place_are_refused():
     s["table"].add_(0)                                                  # other contents are no other tensor
     want, err = ref.attention(dict(s, q=q))
     within(sna.paged_attention(cache, batch, q), want, err, "and what has not changed still runs")
+
+
+def test_expanded_outputs_are_refused():
+    s = ref.make([(300, 3), (40, 1)], 8, 2, 64, 16, torch.bfloat16, seed=24)
+    cache, batch = parts(s)
+    q, k, v = (s[n].contiguous() for n in "qkv")
+    one = torch.zeros(1, 8, 64, dtype=torch.bfloat16, device="cuda")
+    for out in (one.expand(4, 8, 64), one[:, :1].expand(4, 8, 64), torch.zeros(4, 1, 64, dtype=torch.bfloat16, device="cuda").expand(4, 8, 64),
+                torch.zeros(4096, dtype=torch.bfloat16, device="cuda").as_strided((4, 8, 64), (64, 64, 1))):
+        for call in (lambda: sna.paged_attention(cache, batch, q, out=out), lambda: sna.kv_append(cache, batch, q, k, v, out=out)):
+            with pytest.raises(sna.SnaError):
+                call()
+        assert (out == 0).all()
+    want, err = ref.attention(dict(s, q=q))
+    out = torch.zeros(3, 8, 4, 192, dtype=torch.bfloat16, device="cuda").permute(0, 2, 1, 3)[1, :, :, 64:128]       # heads outside tokens, inside more
+    within(sna.paged_attention(cache, batch, q, out=out), want, err, "an output inside a larger tensor")

@@ -67,6 +67,21 @@ def test_rows_are_refused():
     assert append(qn=AT) == NULL and append(kn=AT) == NULL
 
 
+def test_outputs_that_overlap_themselves_are_refused():
+    """Rows of an expanded or windowed output would be written by several blocks."""
+    one = dict(n_seqs=1, n_tokens=1, max_new=1)
+    for bad in (rows(token_stride=0), rows(head_stride=0), rows(token_stride=248), rows(token_stride=-248), rows(head_stride=56, token_stride=1024),
+                rows(token_stride=64, head_stride=64), rows(token_stride=64, head_stride=312), rows(token_stride=56, head_stride=1024), rows(token_stride=1 << 62, head_stride=0)):
+        assert attention(out=bad) == RANGE and append(out=bad) == RANGE, bad
+    assert attention(b=batch(**one), out=rows(head_stride=0)) == RANGE                               # one token, four heads
+    # what does not overlap passes this check and fails at the next one, or at the launch that needs a GPU
+    for good in (rows(), rows(token_stride=256), rows(token_stride=-256), rows(token_stride=64, head_stride=320), rows(token_stride=128, head_stride=640),
+                 rows(token_stride=768, head_stride=128)):
+        assert append(out=good, k=rows(dev=None)) == NULL, good
+        assert attention(out=good, b=batch(max_len=100000), ws=None) == -7, good
+    assert append(b=batch(**one), out=rows(token_stride=0), k=rows(dev=None)) == NULL
+
+
 def test_workspaces_are_refused():
     long = batch(max_len=100000)
     need = sna.lib().sna_paged_attention_workspace_bytes(cache(), long, 4, 0)
