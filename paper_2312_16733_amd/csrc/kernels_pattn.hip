@@ -1,5 +1,5 @@
 // Attention of a step's new tokens over the paged cache, few rows of queries per key / value head.
-//   out = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q.k_j - m),   m the running maximum
+//   out = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q.k_j - m),   m near the running maximum (see Reference)
 // All query heads of a key / value head (and a sequence's new tokens) are rows of one product, so that the cache is read once:
 // its bytes bound these launches (32 heads over 8 of 128: one sequence of 131071 keys 97 us, 5.5 TB/s; 64 of up to 8192 195 us,
 // 5.5 TB/s; 16 of up to 4096 with five tokens each 46 us, 3.8 TB/s; a copy reaches 4.9 of read and write).  A wave takes 64 keys
@@ -27,14 +27,15 @@ constexpr int tile_keys(int D, int MB) { return MB * D > 128 ? 32 : 64; }
 constexpr long kFewScores = 24l << 20, kFewScoresEqual = 7l << 20;
 
 // One wave's statistics of MB x 16 rows: row of queries 16 m + lane % 16, element of o[m][j][c]: dim 16 j + 4 (lane / 16) + c
-template <int D, int MB>
+template <class T, int D, int MB>
 struct RowState {
   f32x4 o[MB][D / 16];
-  float top[MB], sum[MB];          // maximum that o and sum are relative to (base 2); sum over this lane's keys
+  Reference<T> ref[MB];            // of o and sum
+  float sum[MB];                   // over this lane's keys
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
-      top[m] = -INFINITY;
+      ref[m].clear();
       sum[m] = 0.f;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) o[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -109,7 +110,7 @@ struct Attend {
   // What run() does, at leisure, for a wave whose sums came out as no numbers: in tiles whose rows differ in the keys they see, a
   // value that is none would have reached the rows that do not see its key, too.
   __device__ __forceinline__ void run_carefully(int t0, int t1, int step, Span keys, Span clear, const int (&lim)[MB], const int (&low)[MB],
-                                                const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<D, MB>& st) const {
+                                                const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<T, D, MB>& st) const {
     st.clear();
 #pragma unroll 1
     for (int t = t0; t < t1; t += step) {
@@ -144,8 +145,8 @@ struct Attend {
           sc[i >> 3][(i >> 2) & 1][i & 3] = y;
           x = fmaxf(x, y);
         }
-        const float top = fmaxf(st.top[m], max_of_4(x)), ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(st.top[m] - ref);
-        st.top[m] = top;
+        x = max_of_4(x);
+        const float keep = __any(st.ref[m].moves(x)) ? st.ref[m].move(x) : 1.f, ref = st.ref[m].from();
         st.sum[m] *= keep;
         u32x4 p[U];
 #pragma unroll
@@ -187,7 +188,7 @@ struct Attend {
   // Tiles t0, t0 + step, .. below t1.  lim / low: the last and first key that the lane's row of each m sees; all of them
   // see the keys from `clear.lo` to `clear.hi - 1`, none sees any outside `keys`.
   __device__ __forceinline__ void run(int t0, int t1, int step, Span keys, Span clear, const int (&lim)[MB], const int (&low)[MB],
-                                      const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<D, MB>& st) {
+                                      const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<T, D, MB>& st) {
     st.clear();
     if (t0 >= t1) return;
     u32x4 k[U][2][S], v[U][J];
@@ -232,17 +233,14 @@ struct Attend {
         float x = sc[0][0][0];
 #pragma unroll
         for (int i = 1; i < 8 * U; ++i) x = fmaxf(x, sc[i >> 3][(i >> 2) & 1][i & 3]);
-        // the reference is raised only where a score exceeds it by a factor of 2^8 and more: below that the exponentials, their
-        // sums and the products are exact enough as they are (p up to 2^8 in the operand type, fp32 sums), and o stays untouched
         x = max_of_4(x) * scale2;
-        if (__any(x - st.top[m] > 8.f)) {
-          const float top = fmaxf(st.top[m], x), keep = __builtin_amdgcn_exp2f(st.top[m] - (top == -INFINITY ? 0.f : top));
-          st.top[m] = top;
+        if (__any(st.ref[m].moves(x))) {
+          const float keep = st.ref[m].move(x);
           st.sum[m] *= keep;
 #pragma unroll
           for (int j = 0; j < J; ++j) st.o[m][j] *= keep;
         }
-        const float ref = st.top[m] == -INFINITY ? 0.f : st.top[m];  // nothing seen so far
+        const float ref = st.ref[m].from();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           f32x8 e;
@@ -310,14 +308,14 @@ struct JoinLds {                   // of the W waves of a block: they take tiles
 };
 
 // Keys of tiles t0 .. t1 - 1 for the rows of `r` and head h; the waves' parts are joined and leave as results, or as a part of
-// them (part != nullptr): [rows_cap][D] sums, then [rows_cap][2] maximum and sum.
+// them (part != nullptr): [rows_cap][D] sums, then [rows_cap][2] reference and sum.
 template <class T, int D, int MB, int W, bool ONE>
 __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTile& r, int h, int t0, int t1, float* part, int rows_cap, JoinLds<D, MB, W>& lds) {
   constexpr int S = D / 32, J = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, hi = lane >> 4;
   const int rows = r.n * a.G;
   const unsigned inv = 65536u / a.G + 1;                             // row / G for row * G < 65536
-  RowState<D, MB> st;
+  RowState<T, D, MB> st;
   {
     int lim[MB], low[MB];
     u32x4 q[MB][S];
@@ -338,11 +336,11 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
     at.run(t0 + wave, t1, W, r.keys, r.clear, lim, low, q, lds.q, a.scale2, st);
     if (!ONE && __builtin_expect(r.n > 1 && st.is_odd(), 0)) at.run_carefully(t0 + wave, t1, W, r.keys, r.clear, lim, low, q, lds.q, a.scale2, st);
   }
-  // o and sum relative to the largest maximum of the waves
+  // o and sum relative to the largest reference of the waves
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
     st.sum[m] = sum_of_4(st.sum[m]);
-    if (hi == 0) { lds.top[wave][m][l16] = st.top[m]; lds.sum[wave][m][l16] = st.sum[m]; }
+    if (hi == 0) { lds.top[wave][m][l16] = st.ref[m].at; lds.sum[wave][m][l16] = st.sum[m]; }
   }
   __syncthreads();
 #pragma unroll
@@ -351,7 +349,7 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
     float top = lds.top[0][m][l16];
 #pragma unroll
     for (int w = 1; w < W; ++w) top = fmaxf(top, lds.top[w][m][l16]);
-    const float keep = __builtin_amdgcn_exp2f(st.top[m] - (top == -INFINITY ? 0.f : top));
+    const float keep = __builtin_amdgcn_exp2f(st.ref[m].at - (top == -INFINITY ? 0.f : top));
     if (m) __syncthreads();
 #pragma unroll
     for (int j = 0; j < J; ++j) *(f32x4*)&lds.o[wave][l16][16 * j + 4 * hi] = st.o[m][j] * keep;

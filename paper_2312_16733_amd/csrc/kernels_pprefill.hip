@@ -110,7 +110,9 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
   for (int j = 0; j < J; ++j)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
-  float top = -INFINITY, sum = 0.f;                                  // top: of the scores before the scale
+  Reference<T> ref;
+  ref.clear();
+  float sum = 0.f;
   const int key_of = (l32 & 19) | (l32 & 4) << 1 | (l32 & 8) >> 1;   // of the product's row l32
   int k_at[S], v_at[4];                                              // octets of the lane's rows; dims 32 and more further on differ by constants
 #pragma unroll
@@ -167,26 +169,23 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
     float x = sc[0][0];
 #pragma unroll
     for (int i = 1; i < 32; ++i) x = fmaxf(x, sc[i >> 4][i & 15]);
-    x = max_of_2(x);
-    // the reference is raised only where a score exceeds it by a factor of 2^8 and more: below that the exponentials, their
-    // sums and the products are exact enough as they are (p up to 2^8 in the operand type, fp32 sums), and o stays untouched
-    if (__any((x - top) * a.scale2 > 8.f)) {
-      const float now = fmaxf(top, x), keep = __builtin_amdgcn_exp2f((top - (now == -INFINITY ? 0.f : now)) * a.scale2);
-      top = now;
+    x = max_of_2(x) * a.scale2;
+    if (__any(ref.moves(x))) {
+      const float keep = ref.move(x);
       sum *= keep;
 #pragma unroll
       for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[j][i] *= keep;
     }
-    const float ref = top == -INFINITY ? 0.f : -top * a.scale2;
+    const float from = -ref.from();
     u32x4 p[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       f32x8 e;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + i], a.scale2, ref));
+        e[i] = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + i], a.scale2, from));
         sum += e[i];
       }
       p[s] = to_16<T>(e);                                            // off by half a step of the operand type
@@ -203,7 +202,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
 #pragma unroll
     for (int i = 0; i < 16; ++i) left = fmaf(o[j][i], 0.f, left);
   if (__builtin_expect(__any(left != 0.f), 0)) {
-    top = -INFINITY;
+    ref.clear();
     sum = 0.f;
 #pragma unroll
     for (int j = 0; j < J; ++j)
@@ -225,8 +224,8 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
         sc[i] = key <= lim && key >= low ? sc[i] : -INFINITY;
         x = fmaxf(x, sc[i]);
       }
-      const float now = fmaxf(top, max_of_2(x)), ref = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f((top - ref) * a.scale2);
-      top = now;
+      x = max_of_2(x) * a.scale2;
+      const float keep = __any(ref.moves(x)) ? ref.move(x) : 1.f, from = -ref.from();
       sum *= keep;
 #pragma unroll
       for (int j = 0; j < J; ++j)
@@ -237,7 +236,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
         f32x8 e;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(((s ? sc[8 + i] : sc[i]) - ref) * a.scale2);
+          e[i] = __builtin_amdgcn_exp2f(fmaf(s ? sc[8 + i] : sc[i], a.scale2, from));
           sum += e[i];
         }
         const u32x4 p = to_16<T>(e);
@@ -265,7 +264,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
   }
   sum = sum_of_2(sum);
   if (!mine) return;
-  if (a.splits > 1) {                                                // a part: sums, then maximum and sum
+  if (a.splits > 1) {                                                // a part: sums, then reference and sum
     const long r = ((long)part * a.s.T + qi) * (a.kv.heads * a.G) + qh;
     float* out = (float*)a.parts + r * D + hi * 4;
     if (sum != 0.f)
@@ -273,7 +272,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
       for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) *(f32x4*)(out + 32 * j + 8 * i) = f32x4{o[j][4 * i], o[j][4 * i + 1], o[j][4 * i + 2], o[j][4 * i + 3]};
-    if (hi == 0) ((float2*)((float*)a.parts + (long)a.splits * a.s.T * a.kv.heads * a.G * D))[r] = make_float2(top * a.scale2, sum);
+    if (hi == 0) ((float2*)((float*)a.parts + (long)a.splits * a.s.T * a.kv.heads * a.G * D))[r] = make_float2(ref.at, sum);
     return;
   }
   const float f = sum == 0.f ? 0.f : 1.f / sum;                      // a row that sees no key is zero

@@ -12,6 +12,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 // Element types: eight of them are one 16-byte access and one operand of the matrix instructions.
 struct Bf16 {
   static constexpr unsigned kInf = 0x7f80u, kOne = 0x3f80u;
+  static constexpr bool kNarrow = false;                             // few powers of two: see Reference
   typedef __attribute__((ext_vector_type(8))) __bf16 v8;
   typedef __attribute__((ext_vector_type(4))) __bf16 v4;
   static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {     // 16 x 16 += 16 x 32 by 32 x 16
@@ -29,6 +30,7 @@ struct Bf16 {
 };
 struct Fp16 {
   static constexpr unsigned kInf = 0x7c00u, kOne = 0x3c00u;
+  static constexpr bool kNarrow = true;
   typedef __attribute__((ext_vector_type(8))) _Float16 v8;
   typedef __attribute__((ext_vector_type(4))) _Float16 v4;
   static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
@@ -156,6 +158,33 @@ __device__ __forceinline__ float sum_of_4(float v) {
 #endif
   return v;
 }
+
+// What a row's exponentials, their sum and the products are relative to, in powers of two: p = 2^(score - at).  It moves only where
+// a tile's largest score x lies too far from it, so that the sums stay untouched in most tiles.  All lanes of a wave move at once.
+//   bf16 has fp32's powers of two: `at` is the largest score at the last move, and goes up where x exceeds it by 2^8; p and the
+//   products are as exact there as they are at 1.
+//   fp16 loses bits below 2^-14 and everything below 2^-25: with one key that takes nearly all of the weight, the others' p would
+//   vanish from the products while the sum still counts them (of 32768 keys with 0.001 of the weight, 2 % of their value).  So a
+//   tile's largest p is kept within 2^-1 .. 2^15: `at` also goes down, after the high keys, 2^60 below the largest score at most,
+//   behind which a tile is nothing in fp32 sums and the sums would leave fp32.  What 64 keys lose below 2^-14 is then less than
+//   2^-18 of the largest's part.
+template <class T>
+struct Reference {
+  float at, high;
+  __device__ __forceinline__ void clear() { at = high = -INFINITY; }
+  __device__ __forceinline__ bool moves(float x) {
+    if (!T::kNarrow) return x - at > 8.f;
+    high = fmaxf(high, x);
+    return x - at > 15.f || (x - at < -1.f && x != -INFINITY && at > high - 60.f);
+  }
+  __device__ __forceinline__ float move(float x) {                   // what the sums are scaled by
+    const float was = at;
+    if (!T::kNarrow) at = fmaxf(at, x);
+    else if (x != -INFINITY) at = fmaxf(x - 7.f, high - 60.f);
+    return __builtin_amdgcn_exp2f(was - from());
+  }
+  __device__ __forceinline__ float from() const { return at == -INFINITY ? 0.f : at; }             // nothing seen so far: p is 0 anyway
+};
 
 struct AppendArgs {
   PagedSeqs s;
