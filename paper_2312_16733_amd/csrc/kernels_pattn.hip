@@ -108,7 +108,8 @@ struct Attend {
   }
 
   // What run() does, at leisure, for a wave whose sums came out as no numbers: in tiles whose rows differ in the keys they see, a
-  // value that is none would have reached the rows that do not see its key, too.
+  // value that is none would have reached the rows that do not see its key, too.  Operation by operation the same, so that those
+  // rows get what they would get without that value.
   __device__ __forceinline__ void run_carefully(int t0, int t1, int step, Span keys, Span clear, const int (&lim)[MB], const int (&low)[MB],
                                                 const u32x4 (&q)[MB][S], const u32x4 (*q_lds)[64], float scale2, RowState<T, D, MB>& st) const {
     st.clear();
@@ -141,23 +142,24 @@ struct Attend {
 #pragma unroll
         for (int i = 0; i < 8 * U; ++i) {
           const int key = t * KT + 8 * hi + 32 * (i >> 3) + (i & 7);
-          const float y = key <= lim[m] && key >= low[m] ? sc[i >> 3][(i >> 2) & 1][i & 3] * scale2 : -INFINITY;
+          const float y = key <= lim[m] && key >= low[m] ? sc[i >> 3][(i >> 2) & 1][i & 3] : -INFINITY;
           sc[i >> 3][(i >> 2) & 1][i & 3] = y;
           x = fmaxf(x, y);
         }
-        x = max_of_4(x);
+        x = max_of_4(x) * scale2;
         const float keep = __any(st.ref[m].moves(x)) ? st.ref[m].move(x) : 1.f, ref = st.ref[m].from();
         st.sum[m] *= keep;
-        u32x4 p[U];
+        u32x4 p[U], p_rest[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           f32x8 e;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(sc[u][i >> 2][i & 3] - ref);
+            e[i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i >> 2][i & 3], scale2, -ref));
             st.sum[m] += e[i];
           }
           p[u] = to_16<T>(e);
+          if (PRECISE) p_rest[u] = to_16<T>(e - to_f32<T>(p[u]));
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
@@ -168,7 +170,9 @@ struct Attend {
             v[u] = *(const u32x4*)(at[u] + ((long)j * 32 << kv.lps));
 #pragma unroll
             for (int w = 0; w < 4; ++w) v[u][w] &= ok[u][w];
-            st.o[m][j] = T::mma16(differ ? without_odd<T>(v[u]) : v[u], p[u], st.o[m][j]);
+            const u32x4 x = differ ? without_odd<T>(v[u]) : v[u];
+            st.o[m][j] = T::mma16(x, p[u], st.o[m][j]);
+            if (PRECISE) st.o[m][j] = T::mma16(x, p_rest[u], st.o[m][j]);
           }
           if (differ)
 #pragma unroll

@@ -547,3 +547,24 @@ def test_expanded_outputs_are_refused():
     want, err = ref.attention(dict(s, q=q))
     out = torch.zeros(3, 8, 4, 192, dtype=torch.bfloat16, device="cuda").permute(0, 2, 1, 3)[1, :, :, 64:128]       # heads outside tokens, inside more
     within(sna.paged_attention(cache, batch, q, out=out), want, err, "an output inside a larger tensor")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,seqs,window", [((8, 2, 128), [(300, 4), (70, 2)], 0), ((4, 4, 64), [(500, 16), (90, 7)], 100), ((8, 2, 128), [(5000, 4), (2100, 3)], 0),
+                                               ((20, 2, 64), [(400, 3)], 0), ((40, 1, 128), [(300, 3)], 0), ((8, 2, 64), [(300, 100)], 0)])
+def test_no_number_in_one_tokens_sight_leaves_the_others_bit_for_bit(dtype, heads, seqs, window):
+    """Where some token of a block sees an infinity or NaN, the keys are walked a second time: what the others get has to be
+    what they get without it, to the last bit."""
+    s = ref.make(seqs, *heads, 16, ref.DT[dtype], seed=25)
+    cache, batch = parts(s)
+    plain = sna.paged_attention(cache, batch, s["q"], window=window)
+    seen = torch.zeros_like(plain, dtype=torch.bool)
+    row = 0
+    for b, (l, n) in enumerate(seqs):
+        for back, dim, value in ((0, 3, float("nan")), (1, 17, float("inf"))):
+            s["v_pages"][s["table"][b, (l - 1 - back) // 16].long(), 0, dim, (l - 1 - back) % 16] = value
+            seen[row + n - 1 - back: row + n, : heads[0] // heads[1], dim] = True                  # by the last token, or the last two
+        row += n
+    got = sna.paged_attention(cache, batch, s["q"], window=window)
+    assert not torch.isfinite(got[seen]).any()
+    assert torch.equal(got[~seen], plain[~seen])
