@@ -68,7 +68,12 @@ constexpr bool queries_in_lds(int D, int MB) { return MB * D > 128; }
 template <class T, int D, int MB>
 struct Attend {
   static constexpr int S = D / 32, J = D / 16, KT = tile_keys(D, MB), U = KT / 32;
-  static constexpr bool PRECISE = MB == 1;
+  // What rounding to the element type leaves of a probability goes through a second product, so that the result is off by its own
+  // rounding alone (rounded once, the probabilities add as much again: 2.3e-3 of the norm in bf16, not 1.7e-3).  Up to 32 rows, single
+  // and drafted tokens, the cache's bytes bound a launch, and this costs little: 16 sequences of up to 4096 keys with five tokens 46.5
+  // us with and without, 64 of up to 2048 with eight and heads of 64 18.7 and 17.9.  Blocks of 64 rows are chunks, bound by their
+  // products and exponentials (a mixed step 17.3 and 15.0 us), and round once.
+  static constexpr bool PRECISE = MB <= 2;
   const PagedKV kv;
   const int* table;                // the sequence's
   int c_lo, c_hi, h, l16, hi;
@@ -253,8 +258,6 @@ struct Attend {
             e[i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i >> 2][i & 3], scale2, -ref));
             st.sum[m] += e[i];
           }
-          // the operand type, and what it leaves over in a second operand: the bytes of the cache bound these launches, not
-          // its products, and rounded once p would be off by as much as the result's own rounding
           p[m][u] = to_16<T>(e);
           if (PRECISE) p_rest[m][u] = to_16<T>(e - to_f32<T>(p[m][u]));
         }

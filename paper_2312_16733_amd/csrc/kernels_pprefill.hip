@@ -188,7 +188,9 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
         e[i] = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + i], a.scale2, from));
         sum += e[i];
       }
-      p[s] = to_16<T>(e);                                            // off by half a step of the operand type
+      // off by half a step of the operand type, which adds as much to the result as its own rounding (2.3e-3 of the norm in bf16
+      // instead of 1.7e-3); a second product with what the rounding leaves took 542 us instead of 396 for 4096 tokens over 8192
+      p[s] = to_16<T>(e);
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s)
