@@ -369,7 +369,9 @@ typedef struct {
   const int32_t* page_table_dev;  /* [n_seqs][table_width]; entries behind a sequence's last page are not used */
   int64_t table_stride;           /* elements between the table's rows */
   int32_t n_seqs, n_tokens, table_width;
-  int32_t max_new, max_len;       /* bounds on the new tokens and the length of any sequence: they choose the launch */
+  int32_t max_new, max_len;       /* bounds on the new tokens and the length of any sequence: they choose the launch.
+                                   * max_new <= n_tokens, max_len >= max_new, n_seqs * max_new >= n_tokens: other
+                                   * bounds are refused (SNA_E_CFG_RANGE) */
 } sna_paged_batch;
 
 typedef struct { void* dev; int64_t token_stride, head_stride; } sna_rows;   /* [n_tokens][heads][head_dim] */

@@ -305,6 +305,9 @@ int step_of(Step* s, PyObject* cache, PyObject* batch, PyObject* q, PyObject* ou
   NEED(s->q->size(0) <= INT32_MAX && s->q->size(1) <= INT32_MAX, "q: %s is out of range", shape_of(*s->q).c_str());
   s->batch = b->c;
   s->batch.n_tokens = (int32_t)s->q->size(0);
+  // bounds that this step cannot reach say nothing about it: the C entries take the nearest ones that it can
+  if (s->batch.n_tokens > 0 && s->batch.max_new > s->batch.n_tokens) s->batch.max_new = s->batch.n_tokens;
+  if (s->batch.max_len < s->batch.max_new) s->batch.max_len = s->batch.max_new;
   if (!none(out)) {
     const at::Tensor* t = tensor_of(out, "out");
     if (!t) return 0;

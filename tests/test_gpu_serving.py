@@ -584,3 +584,19 @@ def test_single_and_drafted_tokens_are_off_by_their_own_rounding(dtype, heads, s
     own = (want.to(ref.DT[dtype]).double() - want).norm()
     print(f"{float(off / own):.3f} of the result's own rounding", flush=True)
     assert off <= 1.1 * own
+
+
+def test_bounds_that_are_loose():
+    """max_new and max_len are bounds: a server may keep the same ones for every step, however few rows a step has."""
+    s = ref.make([(30, 4), (9, 1)], 8, 2, 64, 16, torch.bfloat16, seed=27)
+    cache = sna.PagedCache(s["k_pages"], s["v_pages"])
+    want, err = ref.attention(s)
+    (wq, eq), _, _ = ref.append(s)
+    bounds = [sna.PagedBatch(s["starts"], s["lens"], s["table"], *b) for b in ((4, 30), (5, 30), (8, 30), (64, 40), (4096, 131072), (4096, 30))]
+    for batch in bounds:
+        within(sna.paged_attention(cache, batch, s["q"]), want, err, f"out, bounds {batch.max_new} and {batch.max_len}")
+    for batch in bounds:
+        within(sna.kv_append(cache, batch, s["q"], s["k"], s["v"]), wq, eq, f"q, bounds {batch.max_new} and {batch.max_len}")
+    for max_new in (0, 2):                                              # no bounds of five tokens of two sequences
+        with pytest.raises(sna.SnaError):
+            sna.paged_attention(cache, sna.PagedBatch(s["starts"], s["lens"], s["table"], max_new, 30), s["q"])
