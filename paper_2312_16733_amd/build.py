@@ -40,14 +40,14 @@ def build_library(verbose: bool = True) -> str:
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
-    _serving_binding()
     if verbose:
         print(f"built {LIB}")
     return LIB
 
 
-def _serving_binding():
-    """The serving operators' Python binding (host code only) against the installed torch."""
+def build_serving(verbose: bool = True) -> str:
+    """The serving operators' Python binding (host code only) against the built library and the installed torch.  The C ABI
+    and the rest of the package do without it."""
     import sysconfig
 
     from torch.utils.cpp_extension import include_paths, library_paths
@@ -62,7 +62,16 @@ def _serving_binding():
         raise RuntimeError("serving binding failed:\n" + r.stderr)
     if r.stderr.strip():
         sys.stderr.write(r.stderr)
+    if verbose:
+        print(f"built {SERVING}")
+    return SERVING
 
 
 if __name__ == "__main__":
     build_library()
+    try:
+        import torch  # noqa: F401
+    except ImportError as e:
+        print(f"not built: {SERVING}, the serving operators' Python side, needs torch ({e})")
+    else:
+        build_serving()
