@@ -12,9 +12,8 @@ __all__ = ["ArchDesc", "SubnetCfgC", "Supernet", "lib", "library_path", "arch_de
            "tensor_infos", "norm_infos", "pack_weights", "pack_stats", "cfg_to_c",
            "supernet_load", "subnet_forward", "SnaError"]
 
-# Autoregressive serving: needs torch, which the rest of the package's import does not
+# Autoregressive serving: needs torch, which the rest of the package does not, and so comes when it is asked for by name
 _SERVING = ("PagedCache", "PagedBatch", "kv_append", "paged_attention", "verify_draft")
-__all__ += _SERVING
 
 
 def __getattr__(name):
@@ -24,3 +23,7 @@ def __getattr__(name):
             globals()[n] = getattr(serving, n)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+
+
+def __dir__():
+    return sorted({*globals(), *_SERVING})
