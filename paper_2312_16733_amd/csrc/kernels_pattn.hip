@@ -17,15 +17,6 @@
 
 namespace sna {
 
-// Keys of a wave's tile: 64, or 32 where more rows of sums would leave room in the registers for one block on a CU only
-constexpr int tile_keys(int D, int MB) { return MB * D > 128 ? 32 : 64; }
-// Scores of a step (rows, all heads, times keys) up to which this kernel is used for chunks, too, in us here and with the
-// many-rows kernel.  Heads of 64: 500 tokens over 2000 keys, 12 heads (12 M) 16.8 and 20.7; 32 x 40 over 1000, 16 heads (20 M)
-// 19.7 and 26.3.  Beside single tokens, which the many-rows kernel leaves to launches of their own: 200 over 2000, 32 heads, and
-// seven tokens (13 M) 39.7 and 46.0.  Chunks of one length of 128-wide heads: 60 over 4096, 32 heads (8 M) 27.2 and 24.2; 250 over
-// 2000, 40 heads (19 M) 41.5 and 30.9.
-constexpr long kFewScores = 24l << 20, kFewScoresEqual = 7l << 20;
-
 // One wave's statistics of MB x 16 rows: row of queries 16 m + lane % 16, element of o[m][j][c]: dim 16 j + 4 (lane / 16) + c
 template <class T, int D, int MB>
 struct RowState {
@@ -386,9 +377,6 @@ __device__ __forceinline__ void attend_rows(const PagedAttnArgs& a, const RowTil
   }
 }
 
-// Two blocks on a CU where the registers allow it: 8 waves with 16 KB and more under way each
-constexpr int blocks_of(int D, int MB) { return MB * D <= 256 ? 2 : 1; }
-
 // A block for each tile of rows and key / value head.  ONE: no sequence brings more than one token, and the rows of a tile see the
 // same keys
 template <class T, int D, int MB, int W, bool ONE>
@@ -417,9 +405,6 @@ __device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) 
 // The keys of all tiles of rows and heads, laid end to end, in equal shares over the blocks: what a share cuts off of a
 // (tile of rows, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what
 // a later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
-struct First { int row0, n, h, last; };                              // first row, tokens (0: none was begun), head, block
-constexpr int kSplitW = 4;         // waves of a block
-__host__ __device__ constexpr long part_floats(long rows, int D) { return (rows * (D + 2) + 3) & ~3l; }    // 16-byte aligned
 template <class T, int D, int MB, bool ONE>
 __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
   __shared__ JoinLds<D, MB, kSplitW> lds;
@@ -591,61 +576,6 @@ static void rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
   else if (mb == 1) rows_grid<T, D, 1, false>(a, s);
   else if (mb == 2) rows_grid<T, D, 2, false>(a, s);
   else rows_grid<T, D, 4, false>(a, s);
-}
-
-// Blocks of whole (tile of rows, head)s walk the longest sequence, which a CU reads at 60 to 70 GB/s; shared out, the keys take
-// what the chip reads at, but their parts are written and joined in a second launch, 6 us.  One tile of rows a sequence (decoding):
-// shared from 1024 keys of 128 on (8 sequences of up to 2048, 8 heads: 18.1 us shared, 23.7 whole; 32 of up to 1000: 21.9 and
-// 16.5), from half of that where most of the chip would be idle (one of 1000: 11.0 and 13.3).
-// Several: where sharing saves kSplitGain turns of a tile for each wave, with sequences of 0.6 of the longest on average (60
-// tokens over 4096 keys, 32 heads: 26.6 us shared, 55 whole; 512 over their own 512: 60 and 22.6, since there every block has to
-// find its way through many short rows of tiles).
-constexpr long kSplitKeys = 1024 * 128, kSplitGain = 6;
-
-// Blocks that share the keys.  One on each CU keeps 128 KB under way (heads of 128) and cuts fewer parts off than two: one sequence
-// of 131071 keys 97 us and 104, 64 of up to 8192 193 and 195; two where (tile of rows, head)s are many and few of them are cut
-// (200 sequences of up to 2500: 219 and 228), or half as long (64 of up to 8192, heads of 64: 61.7 and 63.7).
-static int split_blocks(int head_dim, int mb, long units) { return 256 * (head_dim == 128 && units <= 512 ? 1 : blocks_of(head_dim, mb)); }
-
-// How a step is launched, from what the host knows of it.
-struct AttnPlan {
-  int mb;                          // 16 rows of a block of the few-rows kernel, of which there are 1, 2 or 4; 0: not launched
-  int blocks;                      // that its keys are shared out over; 0: a block walks all of its rows' keys
-  int waves;                       // of a block that walks all keys of its rows
-  int most;                        // tokens of a sequence up to which it takes it
-  bool chunks;                     // the many-rows kernel takes the other sequences
-  ChunkPlan chunk;
-  size_t parts, chunk_parts;       // bytes of the workspace, for either
-};
-static AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
-  const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
-  const bool equal = (long)n_seqs * max_new == n_tokens;               // all sequences bring max_new tokens
-  AttnPlan p = {};
-  if (rows <= 64 || (long)n_tokens * group * kv_heads * keys <= (equal && head_dim == 128 ? kFewScoresEqual : kFewScores)) {
-    const auto units_of = [&](int mb) { return (n_tokens / std::max(16 * mb / group, 1) + n_seqs) * (long)kv_heads; };
-    p.mb = rows <= 16 ? 1 : group <= 32 ? 2 : 4;
-    // Chunks with heads of 64: 64 rows a block instead of 32, which takes 1.45 times as long, where that saves rounds of a block on
-    // each CU (500 tokens and 7 single ones, 4 heads: 15.6 and 17.4 us; 600 of 8 sequences and 56: 31 and 44; 500 of 12 heads: 20.4
-    // and 16.9).  With heads of 128 there is no second block on a CU then, and 32 rows are faster throughout.
-    if (head_dim == 64 && rows > 64 && p.mb == 2 && (units_of(4) + 255) / 256 * 145 < (units_of(2) + 255) / 256 * 100) p.mb = 4;
-    p.most = max_new;
-    const long units = units_of(p.mb), room = 256 * blocks_of(head_dim, p.mb), kt = tile_keys(head_dim, p.mb), tiles = (keys + kt - 1) / kt;
-    p.waves = blocks_of(head_dim, p.mb) == 2 && units <= 256 && tiles * kt > 512 ? 8 : 4;
-    const long whole = (units + room - 1) / room * ((tiles + p.waves - 1) / p.waves), shared = units * tiles * 6 / (10 * kSplitW * room);
-    const bool split = (max_new * group <= 16 * p.mb ? keys * head_dim > (units <= 32 ? kSplitKeys / 2 : kSplitKeys) : whole - shared > kSplitGain * 64 / kt) && units * (tiles + 2) < 1l << 30;
-    if (split) p.blocks = split_blocks(head_dim, p.mb, units);
-  } else {
-    p.chunks = true;
-    p.chunk = plan_of_chunks(n_tokens, kv_heads, group, max_new, keys, head_dim);
-    if (p.chunk.splits > 1) p.chunk_parts = (size_t)p.chunk.splits * n_tokens * kv_heads * group * (head_dim + 2) * sizeof(float);
-    if (!equal && group <= 16 && n_seqs * (long)kv_heads * ((keys >> 5) + 2) < 1l << 30) {    // there may be sequences of few rows
-      p.mb = 1;
-      p.blocks = split_blocks(head_dim, 1, n_seqs * (long)kv_heads);
-      p.most = 16 / group;
-    }
-  }
-  if (p.blocks) p.parts = (p.blocks * (sizeof(First) + 2 * part_floats((long)std::min(16 * p.mb / group, max_new) * group, head_dim) * sizeof(float)) + 255) & ~(size_t)255;
-  return p;
 }
 
 size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {

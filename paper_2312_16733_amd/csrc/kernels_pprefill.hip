@@ -11,7 +11,6 @@
 namespace sna {
 
 typedef __attribute__((address_space(3))) char lds_char;
-constexpr int PF_K = 64;           // keys of a tile
 
 template <int D>
 struct PrefillLds {                // two tiles
@@ -322,30 +321,6 @@ __global__ __launch_bounds__(256) void paged_chunk_join_kernel(const PagedAttnAr
   }
   x *= sum == 0.f ? 0.f : 1.f / sum;
   *(uint2*)(a.o + t * a.o_t + h * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
-}
-
-// Waves of a block, of 32 rows each, and shares of the keys.  The time of a launch is taken to be its rounds of blocks times a
-// block's tiles times a tile, 2 us on a full CU (one block of 8 waves, or two of 4) and 1.5 for a lone block of 4, 1.24 and 1.18 with
-// heads of 64, and where the keys are shared a second launch and the parts, written and read at 4.5 TB/s.  A share has 4 tiles or
-// more.  Measured, 32 heads over 8 of 128: 512 tokens over 8192 keys in shares 81 us (162 by blocks of few rows), 300 in shares 57 (113),
-// 100 in shares 32 (68); four chunks of up to 500 over 2000 whole 68, in 4 shares 128.
-ChunkPlan plan_of_chunks(int n_tokens, int kv_heads, int group, int max_new, long keys, int head_dim) {
-  const long tiles = (keys + PF_K - 1) / PF_K, like = (n_tokens + max_new - 1) / max_new;                // sequences, if all were as long
-  const double tile_us = head_dim == 128 ? 2.0 : 1.24, lone_us = head_dim == 128 ? 1.5 : 1.18, part_us = (double)n_tokens * kv_heads * group * (head_dim + 2) * 8 / 4.5e6;
-  ChunkPlan best = {};
-  double least = 1e30;
-  for (int waves = 8; waves >= 4; waves -= 4) {
-    const long tpt = 32 * waves / group, blocks = like * ((max_new + tpt - 1) / tpt) * kv_heads, room = 256 * (8 / waves);
-    for (int s = 1; s <= 16 && (s == 1 || tiles >= 4 * s); ++s) {
-      const double one = waves == 4 && blocks * s <= 256 ? lone_us : tile_us;
-      const double us = (double)((blocks * s + room - 1) / room * ((tiles + s - 1) / s)) * one + (s > 1 ? 8 + s * part_us : 0.0);
-      if (us < least) {
-        least = us;
-        best = ChunkPlan{waves, s};
-      }
-    }
-  }
-  return best;
 }
 
 template <class T, int D, int W>

@@ -1,6 +1,7 @@
 // What the autoregressive serving kernels share: the step's sequences, the paged key / value cache, 16-bit element types.
 #pragma once
 #include "common.h"
+#include "paged_plan.h"
 
 namespace sna {
 
@@ -220,8 +221,6 @@ struct PagedAttnArgs {
   int splits;                                    // many rows: shares of the keys
 };
 size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
-struct ChunkPlan { int waves, splits; };         // waves of a block, shares of the keys
-ChunkPlan plan_of_chunks(int n_tokens, int kv_heads, int group, int max_new, long keys, int head_dim);
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
 

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2312_16733_amd as sna
+import paged_launches as launches
 import paged_reference as ref
 
 pytestmark = pytest.mark.gpu
@@ -600,3 +601,15 @@ def test_bounds_that_are_loose():
     for max_new in (0, 2):                                              # no bounds of five tokens of two sequences
         with pytest.raises(sna.SnaError):
             sna.paged_attention(cache, sna.PagedBatch(s["starts"], s["lens"], s["table"], max_new, 30), s["q"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("launch,several,dim,step", launches.STEPS)
+def test_attention_in_each_launch_by_its_plan(launch, several, dim, step, dtype):
+    """What test_paged_plan_host.py finds these steps to be launched as, unused slots full of NaN and workspaces, too."""
+    heads, kv_heads, length, new, n, ragged, singles, window = step
+    s = ref.make(launches.seqs(length, new, n, ragged, singles), heads, kv_heads, dim, 16, ref.DT[dtype], seed=28)
+    cache, batch = parts(s)
+    want, err = ref.attention(s, window)
+    workspace = torch.full((256 << 20,), 255, dtype=torch.uint8, device="cuda")
+    within(sna.paged_attention(cache, batch, s["q"], window=window, workspace=workspace), want, err, "out")
