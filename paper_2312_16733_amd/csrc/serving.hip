@@ -123,7 +123,8 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   sna_status st;
   const int64_t need = sna_paged_attention_workspace_bytes(cache, batch, q_heads, window);
   if (need < 0) return (sna_status)need;
-  if (!(scale > 0.f && scale < INFINITY)) return fail(SNA_E_CFG_RANGE, "scale %g (a positive number is needed)", (double)scale);
+  const float scale2 = scale * 1.44269504088896340736f;              // of powers of two
+  if (!(scale > 0.f && scale2 < INFINITY)) return fail(SNA_E_CFG_RANGE, "scale %g (a positive number is needed)", (double)scale);
   if (batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_out(out, "out", batch->n_tokens, q_heads, cache->head_dim)) != SNA_OK) return st;
   if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))
@@ -136,7 +137,7 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   a.o_t = 2 * out->token_stride; a.o_h = 2 * out->head_stride;
   a.G = q_heads / cache->kv_heads;
   a.window = window ? window : INT32_MAX;
-  a.scale2 = scale * 1.44269504088896340736f;
+  a.scale2 = scale2;
   a.max_new = batch->max_new;
   const hipError_t e = launch_paged_attention(a, cache->dtype, cache->head_dim, batch->max_len, workspace_dev, (hipStream_t)hip_stream);
   return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "paged_attention: %s", hipGetErrorString(e));

@@ -82,6 +82,13 @@ def test_outputs_that_overlap_themselves_are_refused():
     assert append(b=batch(**one), out=rows(token_stride=0), k=rows(dev=None)) == NULL
 
 
+def test_scales_beyond_fp32_are_refused():
+    """The kernels take powers of two: scale * log2(e) has to be a number, too."""
+    for scale in (3e38, 2.4e38):
+        assert attention(scale=scale) == RANGE, scale
+    assert attention(scale=2.3e38, b=batch(max_len=100000), ws=None) == -7                          # passes, and fails at the next check
+
+
 def test_workspaces_are_refused():
     long = batch(max_len=100000)
     need = sna.lib().sna_paged_attention_workspace_bytes(cache(), long, 4, 0)
