@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
 }
 
 template <class T, int D>
-static void append_grid(AppendArgs a, hipStream_t s) {
+static hipError_t append_grid(AppendArgs a, hipStream_t s) {
   constexpr int L = D / 16;
   const int hp = a.one ? 64 / L : AP_IT * 256 / (L * AP_TOK), vh = a.one ? 64 / (D / 8) : AP_IT * 256 / (D / 8 * AP_VT);
   a.q_parts = (a.Hq + hp - 1) / hp;
@@ -210,15 +210,17 @@ static void append_grid(AppendArgs a, hipStream_t s) {
   a.v_parts = (a.kv.heads + vh - 1) / vh;
   a.qk_tiles = a.one ? a.s.B : a.s.T / AP_TOK + 2 * a.s.B;
   const int v_tiles = a.one ? a.s.B : a.s.T / AP_VT + 2 * a.s.B;
-  const dim3 grid(a.qk_tiles * (a.q_parts + a.k_parts) + v_tiles * a.v_parts), block(a.one ? 64 : 256);
+  const long blocks = (long)a.qk_tiles * (a.q_parts + a.k_parts) + (long)v_tiles * a.v_parts;
+  const dim3 grid((unsigned)blocks), block(a.one ? 64 : 256);
+  if (!fits_a_launch(blocks, block.x)) return hipErrorInvalidConfiguration;
   if (a.q_norm) hipLaunchKernelGGL((append_kernel<T, D, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((append_kernel<T, D, false>), grid, block, 0, s, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_append(const AppendArgs& a, int dtype, int head_dim, hipStream_t s) {
-  if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? append_grid<Fp16, 64>(a, s) : append_grid<Fp16, 128>(a, s);
-  else head_dim == 64 ? append_grid<Bf16, 64>(a, s) : append_grid<Bf16, 128>(a, s);
-  return hipGetLastError();
+  if (dtype == SNA_DTYPE_FP16) return head_dim == 64 ? append_grid<Fp16, 64>(a, s) : append_grid<Fp16, 128>(a, s);
+  return head_dim == 64 ? append_grid<Bf16, 64>(a, s) : append_grid<Bf16, 128>(a, s);
 }
 
 }  // namespace sna

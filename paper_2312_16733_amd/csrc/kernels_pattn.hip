@@ -550,7 +550,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) 
 constexpr int kSplitLeast = 4;     // tiles of a share: one for each wave
 
 template <class T, int D, int MB, bool ONE>
-static void rows_grid(PagedAttnArgs a, hipStream_t s) {
+static hipError_t rows_grid(PagedAttnArgs a, hipStream_t s) {
   a.tpt = 16 * MB / a.G;
   if (a.parts) {
     if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
@@ -558,24 +558,25 @@ static void rows_grid(PagedAttnArgs a, hipStream_t s) {
     a.least = kSplitLeast;
     hipLaunchKernelGGL((paged_split_kernel<T, D, MB, ONE>), dim3(a.blocks), dim3(64 * kSplitW), 0, s, a);
     hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
-    return;
+    return hipGetLastError();
   }
   a.by_tpt = FastDiv::by(a.tpt);
   const int tiles = a.max_new > a.tpt ? a.s.T / a.tpt + a.s.B : a.s.B;
   const dim3 grid(tiles, a.kv.heads);
+  if (!fits_a_launch(tiles, a.waves * 64)) return hipErrorInvalidConfiguration;
   if constexpr (blocks_of(D, MB) == 2)
     if (a.waves == 8) {
       hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 8, ONE>), grid, dim3(512), 0, s, a);
-      return;
+      return hipGetLastError();
     }
   hipLaunchKernelGGL((paged_rows_kernel<T, D, MB, 4, ONE>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 template <class T, int D>
-static void rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
-  if (mb == 1 && a.max_new == 1) rows_grid<T, D, 1, true>(a, s);
-  else if (mb == 1) rows_grid<T, D, 1, false>(a, s);
-  else if (mb == 2) rows_grid<T, D, 2, false>(a, s);
-  else rows_grid<T, D, 4, false>(a, s);
+static hipError_t rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
+  if (mb == 1 && a.max_new == 1) return rows_grid<T, D, 1, true>(a, s);
+  if (mb == 1) return rows_grid<T, D, 1, false>(a, s);
+  return mb == 2 ? rows_grid<T, D, 2, false>(a, s) : rows_grid<T, D, 4, false>(a, s);
 }
 
 size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
@@ -586,17 +587,19 @@ size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int gro
 hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s) {
   const AttnPlan p = plan_of(a.s.B, a.s.T, a.kv.heads, a.G, a.max_new, max_len, a.window == INT_MAX ? 0 : a.window, head_dim);
   a.most = p.most;
+  a.waves = p.chunk.waves;
+  a.splits = p.chunk.splits;
+  if (p.chunks && !chunks_fit_a_launch(a)) return hipErrorInvalidConfiguration;        // before anything is launched
   if (p.mb) {
     PagedAttnArgs r = a;
     r.parts = p.blocks ? workspace : nullptr;
     r.blocks = p.blocks;
     r.waves = p.waves;
-    if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? rows_of<Fp16, 64>(r, p.mb, s) : rows_of<Fp16, 128>(r, p.mb, s);
-    else head_dim == 64 ? rows_of<Bf16, 64>(r, p.mb, s) : rows_of<Bf16, 128>(r, p.mb, s);
+    hipError_t e;
+    if (dtype == SNA_DTYPE_FP16) e = head_dim == 64 ? rows_of<Fp16, 64>(r, p.mb, s) : rows_of<Fp16, 128>(r, p.mb, s);
+    else e = head_dim == 64 ? rows_of<Bf16, 64>(r, p.mb, s) : rows_of<Bf16, 128>(r, p.mb, s);
+    if (e != hipSuccess || !p.chunks) return e;
   }
-  if (!p.chunks) return hipGetLastError();
-  a.waves = p.chunk.waves;
-  a.splits = p.chunk.splits;
   a.parts = (char*)workspace + p.parts;
   return launch_paged_chunks(a, dtype, head_dim, s);
 }

@@ -323,11 +323,16 @@ __global__ __launch_bounds__(256) void paged_chunk_join_kernel(const PagedAttnAr
   *(uint2*)(a.o + t * a.o_t + h * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
 }
 
+static long chunk_blocks(const PagedAttnArgs& a) { return (a.s.T / (32 * a.waves / a.G) + a.s.B) * (long)a.kv.heads * a.splits; }
+bool chunks_fit_a_launch(const PagedAttnArgs& a) {
+  return fits_a_launch(chunk_blocks(a), 64 * a.waves) && (a.splits == 1 || fits_a_launch(a.s.T, 256));
+}
+
 template <class T, int D, int W>
 static void chunk_grid(PagedAttnArgs a, hipStream_t s) {
   a.tpt = 32 * W / a.G;
   a.by_tpt = FastDiv::by(a.tpt);
-  hipLaunchKernelGGL((paged_chunk_kernel<T, D, W>), dim3((a.s.T / a.tpt + a.s.B) * a.kv.heads * a.splits), dim3(64 * W), 0, s, a);
+  hipLaunchKernelGGL((paged_chunk_kernel<T, D, W>), dim3((unsigned)chunk_blocks(a)), dim3(64 * W), 0, s, a);
   if (a.splits > 1) hipLaunchKernelGGL((paged_chunk_join_kernel<T, D>), dim3(a.s.T, (a.kv.heads * a.G * (D / 4) + 255) / 256), dim3(256), 0, s, a);
 }
 template <class T, int D>

@@ -220,6 +220,7 @@ __global__ __launch_bounds__(64 * VD_W) void verify_kernel(const VerifyArgs a) {
 }
 
 hipError_t launch_verify(const VerifyArgs& a, int token_bytes, int n_seqs, hipStream_t s) {
+  if (!fits_a_launch(n_seqs, 64 * VD_W)) return hipErrorInvalidConfiguration;
   if (token_bytes == 8) hipLaunchKernelGGL(verify_kernel<long>, dim3(n_seqs), dim3(64 * VD_W), 0, s, a);
   else hipLaunchKernelGGL(verify_kernel<int>, dim3(n_seqs), dim3(64 * VD_W), 0, s, a);
   return hipGetLastError();

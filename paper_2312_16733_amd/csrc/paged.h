@@ -187,6 +187,9 @@ struct Reference {
   __device__ __forceinline__ float from() const { return at == -INFINITY ? 0.f : at; }             // nothing seen so far: p is 0 anyway
 };
 
+// A launch has fewer than 2^32 threads along x: steps of more are refused, not cut off
+inline bool fits_a_launch(long blocks, int threads) { return blocks * threads < 1l << 32; }
+
 struct AppendArgs {
   PagedSeqs s;
   PagedKV kv;
@@ -221,6 +224,7 @@ struct PagedAttnArgs {
   int splits;                                    // many rows: shares of the keys
 };
 size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
+bool chunks_fit_a_launch(const PagedAttnArgs& a);
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
 

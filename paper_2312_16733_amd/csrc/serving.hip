@@ -40,7 +40,7 @@ static sna_status check_batch(const sna_paged_batch* b) {
 static sna_status check_heads(const sna_paged_cache* c, const sna_paged_batch* b, int32_t q_heads) {
   if (q_heads < 1 || q_heads % c->kv_heads || q_heads / c->kv_heads > 64)
     return fail(SNA_E_CFG_RANGE, "%d query heads over %d key / value heads (a multiple, up to 64 times, is supported)", q_heads, c->kv_heads);
-  if (((int64_t)b->n_tokens + 2 * (int64_t)b->n_seqs) * q_heads > 1 << 30)         // blocks of a launch are fewer than these
+  if (((int64_t)b->n_tokens + 2 * (int64_t)b->n_seqs) * q_heads > 1 << 30)         // so that no count of rows or blocks leaves 31 bits
     return fail(SNA_E_CFG_RANGE, "%d tokens of %d sequences and %d heads are more than one step takes", b->n_tokens, b->n_seqs, q_heads);
   return SNA_OK;
 }
@@ -63,6 +63,11 @@ static sna_status check_out(const sna_rows* r, const char* name, int64_t tokens,
   if (inner < dim || (outer != far && outer < inner * (rows - 1) + dim))
     return fail(SNA_E_CFG_RANGE, "%s: rows overlap", name);
   return SNA_OK;
+}
+
+static sna_status launched(hipError_t e, const char* what) {
+  if (e == hipErrorInvalidConfiguration) return fail(SNA_E_CFG_RANGE, "%s: more blocks than a launch has", what);
+  return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
 static PagedSeqs seqs_of(const sna_paged_batch* b) {
@@ -105,7 +110,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
   a.interleaved = interleaved != 0;
   a.one = batch->max_new == 1 && batch->n_tokens == batch->n_seqs;
   const hipError_t e = launch_append(a, cache->dtype, cache->head_dim, (hipStream_t)hip_stream);
-  return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "kv_append: %s", hipGetErrorString(e));
+  return launched(e, "kv_append");
 }
 
 
@@ -140,7 +145,7 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   a.scale2 = scale2;
   a.max_new = batch->max_new;
   const hipError_t e = launch_paged_attention(a, cache->dtype, cache->head_dim, batch->max_len, workspace_dev, (hipStream_t)hip_stream);
-  return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "paged_attention: %s", hipGetErrorString(e));
+  return launched(e, "paged_attention");
 }
 
 sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, int64_t target_row_stride, const float* draft_dev,
@@ -159,7 +164,7 @@ sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, 
   const VerifyArgs a = {target_dev, draft_dev, target_seq_stride, target_row_stride, draft_seq_stride, draft_row_stride, tokens_dev, uniforms_dev,
                         n_draft_dev, out_dev, accepted_dev, n_steps, vocab};
   const hipError_t e = launch_verify(a, token_bytes, n_seqs, (hipStream_t)hip_stream);
-  return e == hipSuccess ? SNA_OK : fail(SNA_E_HIP, "verify_draft: %s", hipGetErrorString(e));
+  return launched(e, "verify_draft");
 }
 
 }

@@ -89,6 +89,16 @@ def test_scales_beyond_fp32_are_refused():
     assert attention(scale=2.3e38, b=batch(max_len=100000), ws=None) == -7                          # passes, and fails at the next check
 
 
+def test_steps_of_more_threads_than_a_launch_has_are_refused():
+    c = cache(kv_heads=256, k_page_stride=256 * 16 * 64, v_page_stride=256 * 16 * 64)
+    many, wide = dict(n_seqs=1 << 20, max_len=1 << 20), rows(token_stride=256 * 64)
+    calls = [lambda: append(c=c, b=batch(**many, n_tokens=1 << 20, max_new=1), heads=256, out=wide), lambda: append(c=c, b=batch(**many, n_tokens=1 << 21, max_new=1 << 20), heads=256, out=wide),
+             lambda: attention(c=c, b=batch(**many, n_tokens=1 << 21, max_new=1 << 20), heads=256, out=wide), lambda: verify(n=1 << 22)]
+    for call in calls:
+        assert call() == RANGE
+        assert b"more blocks than a launch has" in sna.lib().sna_last_error()
+
+
 def test_workspaces_are_refused():
     long = batch(max_len=100000)
     need = sna.lib().sna_paged_attention_workspace_bytes(cache(), long, 4, 0)
