@@ -390,8 +390,9 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
 
 /* out = softmax(scale * q k^T) v over each sequence's cached keys, causal: a token of position p sees the
  * keys of positions p - window + 1 .. p (window 0: all up to p).  Query head i reads key / value head
- * i / (q_heads / kv_heads); scale is positive.  Statistics and sums are fp32, the probabilities of a product are rounded (at most) to
- * the element type, the result once more.  A token that sees no key (its position is negative) gives zeros.
+ * i / (q_heads / kv_heads); scale is positive.  Statistics and sums are fp32.  The result is
+ * rounded once to the element type; where a sequence may bring more than 32 rows of a key / value head (max_new * q_heads /
+ * kv_heads), the probabilities may be rounded to it, too.  A token that sees no key (its position is negative) gives zeros.
  * Slots that no visible key of the sequence lies in may hold anything; a value that is no number reaches the tokens that see
  * its key and no others.
  * The workspace (16-byte aligned) holds parts of sums of sequences whose keys several blocks share; its contents need not

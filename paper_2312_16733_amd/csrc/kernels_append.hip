@@ -1,8 +1,8 @@
 // New tokens enter the paged cache: per-head RMS norm and position rotation of q and k, k and v into their pages.
 //   x' = x * rsqrt(mean(x^2) + eps) * w            (with a norm)
 //   (x'_a, x'_b) -> (x'_a cos - x'_b sin, x'_a sin + x'_b cos),   angle = position * inv_freq[pair]
-// Bound by memory: every element is read once and written once (13551 tokens of 32 + 8 + 8 heads of 128: 69.6 us, 4.8 TB/s,
-// what a large copy reaches).  A block takes the new tokens of 16 aligned slots of a page and some heads of q or k, so that an
+// Bound by memory: every element is read once and written once (13551 tokens of 32 + 8 + 8 heads of 128: 69.6 to 71.3 us by card,
+// 4.7 TB/s; a large copy reaches 4.9 to 5.0).  A block takes the new tokens of 16 aligned slots of a page and some heads of q or k, so that an
 // angle is evaluated once a block instead of once a head, or of 64 slots and some heads of v: the cache keeps v transposed, and
 // 64 slots are a line of 128 bytes (runs of 16 slots, written by four blocks, made it 85 to 97 us).  Two rows' loads a thread
 // are under way: four took the registers of the fifth wave of a SIMD (85 us).  An angle is formed in 64 bits, in turns, and

@@ -2,7 +2,7 @@
 //   out = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q.k_j - m),   m near the running maximum (see Reference)
 // All query heads of a key / value head (and a sequence's new tokens) are rows of one product, so that the cache is read once:
 // its bytes bound these launches (32 heads over 8 of 128: one sequence of 131071 keys 97 us, 5.5 TB/s; 64 of up to 8192 195 us,
-// 5.5 TB/s; 16 of up to 4096 with five tokens each 46 us, 3.8 TB/s; a copy reaches 4.9 of read and write).  A wave takes 64 keys
+// 5.6 TB/s; 16 of up to 4096 with five tokens each 47 us, 3.6 TB/s; a plain read of gigabytes reaches 6.4).  A wave takes 64 keys
 // at a time, straight from the pages into the operands of the matrix
 // instruction: 16 rows of K (or of V^T, which is what the value pages hold) are 16 lanes, four lanes share a row's 32 columns.
 // The next tile's keys are asked for when the scores are done, its values after the second product, and its pages a tile ahead
@@ -63,7 +63,7 @@ struct Attend {
   // rounding alone (rounded once, the probabilities add as much again: 2.3e-3 of the norm in bf16, not 1.7e-3).  Up to 32 rows, single
   // and drafted tokens, the cache's bytes bound a launch, and this costs little: 16 sequences of up to 4096 keys with five tokens 46.5
   // us with and without, 64 of up to 2048 with eight and heads of 64 18.7 and 17.9.  Blocks of 64 rows are chunks, bound by their
-  // products and exponentials (a mixed step 17.3 and 15.0 us), and round once.
+  // products and exponentials (a mixed step 17.3 and 15.0 us), or groups of more than 32 heads, and round once.
   static constexpr bool PRECISE = MB <= 2;
   const PagedKV kv;
   const int* table;                // the sequence's

@@ -1,8 +1,9 @@
 // Attention of a step's new tokens over the paged cache, many rows of queries per key / value head (chunks of prompts).
 // Bound by the matrix pipe and, nearly as much, by the vector pipe's exponentials.  A block holds 32 rows a wave (tokens times
 // the query heads of one key / value head) and walks its keys in tiles of 64, fetched from the pages straight into LDS, one
-// tile ahead (4096 tokens over 8192 keys, 32 heads over 8 of 128: 395 us, 1.04 PFLOP/s; the library's plain bf16 product of 8192^3
-// reaches 1.20).  A page id is looked at a tile after it was asked for: looked at once it waited for the tile's fetches, too (523 us).
+// tile ahead (4096 tokens over 8192 keys, 32 heads over 8 of 128: 386 to 402 us by card, 1.02 to 1.07 PFLOP/s, once the chip has
+// settled, 26 ms into a burst, and up to 534 before; the library's plain bf16 product of 8192^3 reaches 1.20; the matrix pipe is at work
+// 49 % of the cycles, the vector pipe 48 %).  A page id is looked at a tile after it was asked for: looked at once it waited for the tile's fetches, too (523 us).
 // Forming the next tile's scores among this one's exponentials was worth under 1 % (393 us), forced interleaving of products,
 // reads and vector instructions cost 2 %, four waves a block instead of eight 4 %.  As where rows are few, the scores are formed transposed: a lane has one row, and the keys of a product's 32
 // rows are chosen so (row 16 s + 8 a + 4 h + c is key 16 s + 8 h + 4 a + c) that its scores are what the second product wants.
