@@ -404,6 +404,26 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
                                const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* workspace_dev,
                                size_t workspace_bytes, void* hip_stream);
 
+/* The same append where a token's position is not its slot's number, as in trees of drafted tokens: token t is rotated by
+ * positions_dev[t] * inv_freq (int32 [n_tokens]; NULL: by its slot's number).  Slots are as above. */
+sna_status sna_kv_append_at(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, const sna_rows* q,
+                            const sna_rows* k, const sna_rows* v, const sna_rows* q_out, const float* inv_freq_dev,
+                            int32_t rot_dim, int32_t interleaved, const float* q_norm_dev, const float* k_norm_dev, float eps,
+                            const int32_t* positions_dev, void* hip_stream);
+
+/* Attention of the tokens of drafted trees over the cache.  A sequence's tree begins behind its first prefix_dev[b] slots (int32
+ * [n_seqs], 0 .. lens[b]; NULL: all but the step's own tokens); a step may bring all of a tree, or a part of it after others.
+ * Token t sees the slots before the tree, and slot prefix + 64 w + j where bit j of masks_dev[t][w] is set (uint64
+ * [n_tokens][mask_words], 1 .. 64 words): its own and those it comes from, in a tree, but any mask will do.  Without a prefix
+ * max_new <= 64 * mask_words.  window (0: none): of the slots before the tree a token sees those of positions
+ * p - window + 1 and more, p being positions_dev[t] (int32 [n_tokens]; NULL: its slot's number), taken to lie in
+ * prefix .. prefix + 64 mask_words - 1; of the tree it sees what its mask says.  A token that sees nothing gives zeros.  All
+ * else is as for sna_paged_attention, and so are the errors. */
+int64_t sna_tree_attention_workspace_bytes(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, int32_t mask_words, int32_t window);
+sna_status sna_tree_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, const sna_rows* q, const sna_rows* out,
+                              const uint64_t* masks_dev, int32_t mask_words, const int32_t* prefix_dev, const int32_t* positions_dev, float scale,
+                              int32_t window, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
 /* Verification of drafted tokens: sequence b drafted tokens[b][0 .. n_draft[b] - 1] (n_draft_dev NULL: all n_steps).
  * target[b][i] (fp32 [vocab], dense) are the target's probabilities of the token at drafted place i, given those before it,
  * and target[b][n_draft[b]] of the one after the last; draft[b][i] are those that drafted token i was drawn from, or NULL
@@ -418,6 +438,58 @@ sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, 
                             int64_t draft_seq_stride, int64_t draft_row_stride, const void* tokens_dev, int32_t token_bytes,
                             const float* uniforms_dev, const int32_t* n_draft_dev, int32_t n_seqs, int32_t n_steps, int32_t vocab,
                             int32_t* out_dev, int32_t* accepted_dev, void* hip_stream);
+
+/* Which tokens of drafted trees stand.  A step's tokens of sequence b are its tree: the first is the root, which stands (the last
+ * token that is known); token i > 0 is a child of parents[i] (its number within the sequence, less than i; others are nobody's
+ * child).  sampled[i] is the token drawn behind token i (from the target's probabilities there), and of the children of a token
+ * that stands the first one with tokens[child] == sampled[i] stands, too; a sampled token below 0 matches none.  kept[b]
+ * (int32 [n_seqs][max_new]): the numbers of those that stand, rising, then -1; counts[b]: how many; next[b]: sampled behind the last
+ * of them, -1 where the sequence brings no tokens.  Tokens of 4 or 8 bytes; max_new is at most 4096.  Of the batch, starts,
+ * lens, the sizes and max_new are used.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_HIP. */
+sna_status sna_verify_tree(const sna_paged_batch* batch, const void* sampled_dev, int32_t sampled_bytes, const void* tokens_dev, int32_t token_bytes,
+                           const int32_t* parents_dev, int32_t* kept_dev, int32_t* counts_dev, int32_t* next_dev, void* hip_stream);
+
+/* Moves the kept ones of a step's tokens up behind the slots before them: of sequence b, whose step begins at slot
+ * base = lens[b] - (starts[b + 1] - starts[b]), slot base + kept[b][i] goes to slot base + i for i < counts[b], keys and values.
+ * kept (int32 [n_seqs][kept_width]) rises within a sequence from 0 or more; what does not, or is no token of the step, does not
+ * move, and what its slot then holds is unspecified.  lens_out_dev[b] (int32 [n_seqs], none of the arrays that are read): base + counts[b].
+ * Slots behind that keep what they held.  Of the batch, n_tokens and max_len are not used.  A cache of all layers at once, where the
+ * layers of a page lie next to each other, is one of layers * kv_heads heads.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_HIP. */
+sna_status sna_kv_compact(const sna_paged_cache* cache, const sna_paged_batch* batch, const int32_t* kept_dev, int32_t kept_width, const int32_t* counts_dev,
+                          int32_t* lens_out_dev, void* hip_stream);
+
+/* Copies page source[i] over page target[i] (int32 [n]), keys and values.  Pages outside the pool are left out; a target is no
+ * other pair's target or source.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_HIP. */
+sna_status sna_copy_pages(const sna_paged_cache* cache, const int32_t* source_dev, const int32_t* target_dev, int32_t n, void* hip_stream);
+
+/* Draws a token from each row of logits with a given random number.  With w_i = exp((l_i - max l) / temperature) and tokens in the
+ * order of falling logits, equal ones by number: of the first top_k (0: all) the fewest, and at least one, whose weights make
+ * top_p of theirs (1: all), and of these the ones with w_i >= min_p.  The token is the first, in the vocabulary's order, up to
+ * which the weights that are left make more than uniforms[r] (of [0, 1)) of all of them.  Temperature 0: the first of the largest.
+ * A logit that is no number counts as -inf, weight 0; where +inf is the largest, only those have weight.  A row without weight gives
+ * -1.  Weights are formed in 64 bits and held in steps of 2^-44 of the largest, or finer below 2^18 logits and up to
+ * 2^-42 at 2^20: one below half a step is never drawn.  probs (fp32 [n_rows][vocab], may be NULL): what is left, each weight over
+ * their sum.  The settings are one number for all rows or, where the pointer is given, fp32 (top_k: int32) [n_rows] in device
+ * memory; there a temperature that is not positive is 0, and a top_k below 1, a top_p of 1 or more and what is no number cut
+ * nothing.  Workspace as for attention.
+ * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_WORKSPACE, SNA_E_HIP. */
+typedef struct {
+  const void* logits_dev;         /* [n_rows][vocab] of any stride between rows; rows may overlap */
+  int64_t row_stride;             /* elements */
+  int32_t n_rows, vocab;          /* vocab: 1 .. 2^20 */
+  int32_t dtype;                  /* of the logits: SNA_DTYPE_FP32, SNA_DTYPE_BF16 or SNA_DTYPE_FP16 */
+  int32_t top_k;
+  float temperature, top_p, min_p;
+  const float* uniforms_dev;      /* [n_rows] */
+  const float *temperature_dev, *top_p_dev, *min_p_dev;
+  const int32_t* top_k_dev;
+} sna_sampling;
+int64_t sna_sample_tokens_workspace_bytes(const sna_sampling* sampling);
+sna_status sna_sample_tokens(const sna_sampling* sampling, int32_t* tokens_dev, float* probs_dev, int64_t probs_stride, void* workspace_dev,
+                             size_t workspace_bytes, void* hip_stream);
 
 const char* sna_last_error(void);
 

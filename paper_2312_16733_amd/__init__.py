@@ -13,7 +13,8 @@ __all__ = ["ArchDesc", "SubnetCfgC", "Supernet", "lib", "library_path", "arch_de
            "supernet_load", "subnet_forward", "SnaError"]
 
 # Autoregressive serving: needs torch, which the rest of the package does not, and so comes when it is asked for by name
-_SERVING = ("PagedCache", "PagedBatch", "kv_append", "paged_attention", "verify_draft")
+_SERVING = ("PagedCache", "PagedBatch", "PagePool", "kv_append", "paged_attention", "verify_draft", "sample_tokens", "tree_masks", "tree_attention",
+            "verify_tree", "kv_compact", "copy_pages")
 
 
 def __getattr__(name):

@@ -63,6 +63,12 @@ class PagedBatchC(C.Structure):
                 ("table_width", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32)]
 
 
+class SamplingC(C.Structure):
+    _fields_ = [("logits_dev", C.c_void_p), ("row_stride", C.c_int64), ("n_rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("top_k", C.c_int32),
+                ("temperature", C.c_float), ("top_p", C.c_float), ("min_p", C.c_float), ("uniforms_dev", C.c_void_p), ("temperature_dev", C.c_void_p),
+                ("top_p_dev", C.c_void_p), ("min_p_dev", C.c_void_p), ("top_k_dev", C.c_void_p)]
+
+
 class RowsC(C.Structure):
     _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
@@ -123,6 +129,16 @@ def lib():
     L.sna_paged_attention_workspace_bytes.argtypes = [cp, bp, i32, i32]; L.sna_paged_attention_workspace_bytes.restype = i64
     L.sna_verify_draft.argtypes = [vp, i64, i64, vp, i64, i64, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp]
     L.sna_verify_draft.restype = i32
+    L.sna_kv_append_at.argtypes = [cp, bp, i32, rp, rp, rp, rp, vp, i32, i32, vp, vp, C.c_float, vp, vp]
+    L.sna_kv_append_at.restype = i32
+    L.sna_tree_attention.argtypes = [cp, bp, i32, rp, rp, vp, i32, vp, vp, C.c_float, i32, vp, sz, vp]; L.sna_tree_attention.restype = i32
+    L.sna_tree_attention_workspace_bytes.argtypes = [cp, bp, i32, i32, i32]; L.sna_tree_attention_workspace_bytes.restype = i64
+    L.sna_verify_tree.argtypes = [bp, vp, i32, vp, i32, vp, vp, vp, vp, vp]; L.sna_verify_tree.restype = i32
+    L.sna_kv_compact.argtypes = [cp, bp, vp, i32, vp, vp, vp]; L.sna_kv_compact.restype = i32
+    L.sna_copy_pages.argtypes = [cp, vp, vp, i32, vp]; L.sna_copy_pages.restype = i32
+    mp = C.POINTER(SamplingC)
+    L.sna_sample_tokens.argtypes = [mp, vp, vp, i64, vp, sz, vp]; L.sna_sample_tokens.restype = i32
+    L.sna_sample_tokens_workspace_bytes.argtypes = [mp]; L.sna_sample_tokens_workspace_bytes.restype = i64
     _lib = L
     return L
 

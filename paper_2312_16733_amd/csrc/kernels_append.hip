@@ -120,7 +120,7 @@ __device__ __forceinline__ void append_qk(const AppendArgs& a, const bool is_k, 
   }
   for (int i = tid; i < cnt * half; i += nt) {
     const int tok = i / half;
-    double turns = (double)(first + tok) * (double)a.inv_freq[i - tok * half] * 0.15915494309189533577;
+    double turns = (double)(a.positions ? a.positions[row0 + tok] : first + tok) * (double)a.inv_freq[i - tok * half] * 0.15915494309189533577;
     turns -= rint(turns);
     float sn, co;
     sincospif(2.f * (float)turns, &sn, &co);

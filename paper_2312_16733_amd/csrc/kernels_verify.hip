@@ -8,6 +8,8 @@
 // the row, then the run that holds the draw (V / 16 values, cached by now) is shared out over the waves, and the run of that
 // over the lanes of one.  128 sequences of 131072: 19.2 us, 3.5 TB/s; 64 of 50257 with the draft's rows: 11.9 us, of which 4.5 are
 // the round trips that follow each other (drafts, their probabilities, the rows, the draw), and one CU a sequence reads 0.4 MB.
+#include <climits>
+
 #include "paged.h"
 
 namespace sna {
@@ -217,6 +219,50 @@ __global__ __launch_bounds__(64 * VD_W) void verify_kernel(const VerifyArgs a) {
     for (int i = lane; i <= K; i += 64) a.out[(long)b * (K + 1) + i] = i < acc ? (int)tokens[i] : i == acc ? token : -1;
     if (lane == 0) a.accepted[b] = acc;
   }
+}
+
+// Which tokens of a drafted tree stand, from the token drawn behind each of them: the root does, and behind one that stands its
+// first child whose token is the one drawn there.  Bound by round trips: every token finds out at once whether it is its parent's
+// choice, and the first of several in LDS by its number, so that the walk itself goes from one LDS word to the next.
+__device__ __forceinline__ long token_at(const void* p, int bytes, long i) { return bytes == 8 ? ((const long*)p)[i] : (long)((const int*)p)[i]; }
+__global__ __launch_bounds__(256) void verify_tree_kernel(const TreeWalkArgs a) {
+  extern __shared__ int following[];               // [max_new]: the child that stands, or none; then [max_new]: those that do
+  __shared__ int found;
+  const int b = blockIdx.x, tid = threadIdx.x, nt = blockDim.x;
+  const Seq q = uniform(sequence(a.s, b));
+  const int n = min(q.n, a.max_new);
+  int* path = following + a.max_new;
+  for (int i = tid; i < n; i += nt) following[i] = INT_MAX;
+  __syncthreads();
+  for (int j = 1 + tid; j < n; j += nt) {
+    const int p = a.parents[q.row0 + j];
+    if (p < 0 || p >= j) continue;                                   // nobody's child; so a walk rises, and ends
+    const long drawn = token_at(a.sampled, a.sampled_bytes, q.row0 + p);
+    if (drawn >= 0 && drawn == token_at(a.tokens, a.token_bytes, q.row0 + j)) atomicMin(&following[p], j);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int c = 0, count = 0;
+    while (c < n) {
+      path[count++] = c;
+      c = following[c];
+    }
+    found = count;
+  }
+  __syncthreads();
+  const int count = found;
+  for (int i = tid; i < a.max_new; i += nt) a.kept[(long)b * a.max_new + i] = i < count ? path[i] : -1;
+  if (tid == 0) {
+    a.counts[b] = count;
+    a.next[b] = count ? (int)token_at(a.sampled, a.sampled_bytes, q.row0 + path[count - 1]) : -1;
+  }
+}
+
+hipError_t launch_verify_tree(const TreeWalkArgs& a, hipStream_t s) {
+  const int threads = a.max_new <= 64 ? 64 : 256;
+  if (!fits_a_launch(a.s.B, threads)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(verify_tree_kernel, dim3(a.s.B), dim3(threads), 8 * a.max_new, s, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_verify(const VerifyArgs& a, int token_bytes, int n_seqs, hipStream_t s) {

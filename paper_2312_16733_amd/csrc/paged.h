@@ -86,6 +86,13 @@ __device__ __forceinline__ u32x4 ones_where_seen(int key, int low, int lim) {
   for (int w = 0; w < 4; ++w) v[w] = one(key + 2 * w) | one(key + 2 * w + 1) << 16;
   return v;
 }
+// Of the keys of those ones, the ones whose bit is set
+template <class T>
+__device__ __forceinline__ u32x4 ones_of_both(u32x4 v, unsigned bits) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v[w] &= (0u - (bits >> 2 * w & 1)) >> 16 | (0u - (bits >> (2 * w + 1) & 1)) << 16;
+  return v;
+}
 __device__ __forceinline__ float odd_sum(bool some, int kind) {      // what they add
   return some ? kind == ODD_NAN ? __builtin_nanf("") : kind == ODD_INF ? INFINITY : -INFINITY : 0.f;
 }
@@ -196,6 +203,7 @@ struct AppendArgs {
   const char *q, *k, *v;
   char* qo;
   const float *inv_freq, *q_norm, *k_norm;
+  const int* positions;                          // [T] or nullptr: a token's slot is its position
   long q_t, q_h, k_t, k_h, v_t, v_h, o_t, o_h;   // bytes between tokens / heads
   int Hq, half;                                  // half: rotated pairs of a head
   float eps;
@@ -222,11 +230,47 @@ struct PagedAttnArgs {
   FastDiv by_tpt;
   int rows_cap, least, blocks;                   // rows of a part; least tiles of a share; blocks that share
   int splits;                                    // many rows: shares of the keys
+  // of trees only
+  const unsigned long long* masks;               // [T][words]
+  const int* prefix;                             // [B] or nullptr: all but the step's own tokens
+  const int* positions;                          // [T] or nullptr: a token's slot is its position
+  int words;
 };
+
+// The keys of a sequence of which a tree's tokens see different ones.  All of them see keys 0 .. base - 1, as far as the window
+// goes, and of base .. last those whose bit is set: bit j of word w is key base + 64 w + j.
+struct TreeMask {
+  int base, last, words;
+  // Bits of key .. key + 7; ones for those before the tree
+  __device__ __forceinline__ unsigned seen8(const unsigned long long* mask, int key) const {
+    const int o = key - base, w = o >> 6, s = o & 63;
+    if (o <= -8) return 0xff;
+    const unsigned long long a = w < 0 ? ~0ull : w < words ? mask[w] : 0, b = s > 56 && w + 1 < words ? mask[w + 1] : 0;
+    return (unsigned)(a >> s | (s ? b << (64 - s) : 0)) & 0xff;
+  }
+  // The first key of those before the tree that a row sees.  Its position is taken to be one that its tree can have
+  __device__ __forceinline__ int low(const PagedAttnArgs& a, int row, int slot) const {
+    if (a.window == 0x7fffffff) return 0;
+    const int pos = clamped(a.positions ? a.positions[row] : slot, base, base + 64 * words - 1);
+    return min(a.window <= pos ? pos - a.window + 1 : 0, max(base, 0));
+  }
+};
+__device__ __forceinline__ int first_in_window(int window, int pos) { return window <= pos ? pos - window + 1 : 0; }
+__device__ __forceinline__ TreeMask tree_of(const PagedAttnArgs& a, const Seq& sq, int b) {
+  TreeMask m;
+  m.base = a.prefix ? clamped(a.prefix[b], 0, sq.len) : sq.len - sq.n;
+  m.words = a.words;
+  m.last = min(min(sq.len, m.base + 64 * a.words), a.s.width << a.kv.lps) - 1;
+  return m;
+}
+// A window that holds the keys of all of a tree's tokens, for the choice of a launch
+inline int tree_window(int window, int words) { return (int)std::min<long>((long)window + 64 * words, 1l << 30); }
 size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim);
 bool chunks_fit_a_launch(const PagedAttnArgs& a);
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
+hipError_t launch_tree_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_tree_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
 
 struct VerifyArgs {
   const float *target, *draft;                   // [seq][K + 1][V], [seq][K][V] or nullptr
@@ -239,5 +283,54 @@ struct VerifyArgs {
   int K, V;
 };
 hipError_t launch_verify(const VerifyArgs& a, int token_bytes, int n_seqs, hipStream_t s);
+
+constexpr int kTreeTokens = 4096;                // of a sequence, that a walk along a tree takes
+struct TreeWalkArgs {
+  PagedSeqs s;
+  const void *sampled, *tokens;                  // [T]
+  int sampled_bytes, token_bytes;
+  const int* parents;                            // [T]
+  int* kept;                                     // [B][max_new]
+  int *counts, *next;                            // [B]
+  int max_new;
+};
+hipError_t launch_verify_tree(const TreeWalkArgs& a, hipStream_t s);
+
+struct CompactArgs {
+  PagedSeqs s;
+  PagedKV kv;
+  const int* kept;                               // [B][width]
+  const int* counts;                             // [B]
+  int* lens;                                     // [B]
+  int width, max_new, dim;
+  int k_blocks, blocks;                          // of a sequence; filled by the launcher
+};
+hipError_t launch_compact(CompactArgs a, hipStream_t s);
+
+struct PageCopyArgs {
+  PagedKV kv;
+  const int *source, *target;
+  long bytes;                                    // of a page's keys, and of its values
+  int blocks;                                    // of a page; filled by the launcher
+};
+hipError_t launch_copy_pages(PageCopyArgs a, int n, hipStream_t s);
+
+struct SampleArgs {
+  const void* logits;
+  long stride;                                   // elements between rows
+  const float* u;                                // [n]
+  const float *temperature_of, *top_p_of, *min_p_of;                   // [n] or nullptr: the same for all rows
+  const int* top_k_of;
+  float temperature, top_p, min_p;
+  int top_k;
+  int V, n;
+  int* tokens;                                   // [n]
+  float* probs;                                  // [n][V] or nullptr
+  long p_stride;
+  void* work;
+  int scale_bits;                                // weights are held in steps of 2^-scale_bits of the largest
+};
+size_t sample_workspace(int n, int vocab, int dtype);
+hipError_t launch_sample(SampleArgs a, int dtype, hipStream_t s);
 
 }  // namespace sna

@@ -87,11 +87,19 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
                          const sna_rows* k, const sna_rows* v, const sna_rows* q_out, const float* inv_freq_dev,
                          int32_t rot_dim, int32_t interleaved, const float* q_norm_dev, const float* k_norm_dev, float eps,
                          void* hip_stream) {
+  return sna_kv_append_at(cache, batch, q_heads, q, k, v, q_out, inv_freq_dev, rot_dim, interleaved, q_norm_dev, k_norm_dev, eps, nullptr, hip_stream);
+}
+
+sna_status sna_kv_append_at(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, const sna_rows* q,
+                            const sna_rows* k, const sna_rows* v, const sna_rows* q_out, const float* inv_freq_dev,
+                            int32_t rot_dim, int32_t interleaved, const float* q_norm_dev, const float* k_norm_dev, float eps,
+                            const int32_t* positions_dev, void* hip_stream) {
   sna_status st;
   if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, batch, q_heads)) != SNA_OK) return st;
   if (rot_dim < 0 || rot_dim > cache->head_dim || rot_dim % 16) return fail(SNA_E_CFG_RANGE, "rot_dim %d (a multiple of 16 up to head_dim is supported)", rot_dim);
   if (rot_dim && !inv_freq_dev) return fail(SNA_E_NULL, "inv_freq is NULL");
   if (!q_norm_dev != !k_norm_dev) return fail(SNA_E_NULL, "one of q_norm and k_norm is NULL");
+  if ((uintptr_t)positions_dev & 3) return fail(SNA_E_CFG_ALIGN, "positions are not aligned to their elements");
   if (batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_rows(k, "k")) != SNA_OK || (st = check_rows(v, "v")) != SNA_OK ||
       (st = check_out(q_out, "q_out", batch->n_tokens, q_heads, cache->head_dim)) != SNA_OK) return st;
@@ -101,6 +109,7 @@ sna_status sna_kv_append(const sna_paged_cache* cache, const sna_paged_batch* ba
   a.kv = kv_of(cache);
   a.q = (const char*)q->dev; a.k = (const char*)k->dev; a.v = (const char*)v->dev; a.qo = (char*)q_out->dev;
   a.inv_freq = inv_freq_dev; a.q_norm = q_norm_dev; a.k_norm = k_norm_dev;
+  a.positions = positions_dev;
   a.q_t = 2 * q->token_stride; a.q_h = 2 * q->head_stride;
   a.k_t = 2 * k->token_stride; a.k_h = 2 * k->head_stride;
   a.v_t = 2 * v->token_stride; a.v_h = 2 * v->head_stride;
@@ -122,19 +131,16 @@ int64_t sna_paged_attention_workspace_bytes(const sna_paged_cache* cache, const 
   return (int64_t)paged_attention_workspace(batch->n_seqs, batch->n_tokens, cache->kv_heads, q_heads / cache->kv_heads, batch->max_new, batch->max_len, window, cache->head_dim);
 }
 
-sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
-                               const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* workspace_dev,
-                               size_t workspace_bytes, void* hip_stream) {
+static sna_status attend(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, const sna_rows* q, const sna_rows* out, float scale, int32_t window,
+                         int64_t need, void* workspace_dev, size_t workspace_bytes, PagedAttnArgs a, void* hip_stream, const char* name) {
   sna_status st;
-  const int64_t need = sna_paged_attention_workspace_bytes(cache, batch, q_heads, window);
   if (need < 0) return (sna_status)need;
   const float scale2 = scale * 1.44269504088896340736f;              // of powers of two
   if (!(scale > 0.f && scale2 < INFINITY)) return fail(SNA_E_CFG_RANGE, "scale %g (a positive number is needed)", (double)scale);
   if (batch->n_tokens == 0) return SNA_OK;
   if ((st = check_rows(q, "q")) != SNA_OK || (st = check_out(out, "out", batch->n_tokens, q_heads, cache->head_dim)) != SNA_OK) return st;
   if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))
-    return fail(SNA_E_WORKSPACE, "paged_attention: a workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
-  PagedAttnArgs a = {};
+    return fail(SNA_E_WORKSPACE, "%s: a workspace of %lld bytes, 16-byte aligned, is needed", name, (long long)need);
   a.s = seqs_of(batch);
   a.kv = kv_of(cache);
   a.q = (const char*)q->dev; a.o = (char*)out->dev;
@@ -144,8 +150,38 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
   a.window = window ? window : INT32_MAX;
   a.scale2 = scale2;
   a.max_new = batch->max_new;
-  const hipError_t e = launch_paged_attention(a, cache->dtype, cache->head_dim, batch->max_len, workspace_dev, (hipStream_t)hip_stream);
-  return launched(e, "paged_attention");
+  const hipError_t e = (a.masks ? launch_tree_attention : launch_paged_attention)(a, cache->dtype, cache->head_dim, batch->max_len, workspace_dev, (hipStream_t)hip_stream);
+  return launched(e, name);
+}
+
+sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads,
+                               const sna_rows* q, const sna_rows* out, float scale, int32_t window, void* workspace_dev,
+                               size_t workspace_bytes, void* hip_stream) {
+  const int64_t need = sna_paged_attention_workspace_bytes(cache, batch, q_heads, window);
+  return attend(cache, batch, q_heads, q, out, scale, window, need, workspace_dev, workspace_bytes, PagedAttnArgs{}, hip_stream, "paged_attention");
+}
+
+int64_t sna_tree_attention_workspace_bytes(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, int32_t mask_words, int32_t window) {
+  if (mask_words < 1 || mask_words > 64) return fail(SNA_E_CFG_RANGE, "masks of %d words (1 to 64 are supported)", mask_words);
+  if (window < 0) return fail(SNA_E_CFG_RANGE, "window %d", window);
+  return sna_paged_attention_workspace_bytes(cache, batch, q_heads, window ? tree_window(window, mask_words) : 0);
+}
+
+sna_status sna_tree_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, const sna_rows* q, const sna_rows* out,
+                              const uint64_t* masks_dev, int32_t mask_words, const int32_t* prefix_dev, const int32_t* positions_dev, float scale,
+                              int32_t window, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  const int64_t need = sna_tree_attention_workspace_bytes(cache, batch, q_heads, mask_words, window);
+  if (need < 0) return (sna_status)need;
+  if (batch->n_tokens > 0 && !masks_dev) return fail(SNA_E_NULL, "masks are NULL");
+  if (batch->n_tokens > 0 && !prefix_dev && batch->max_new > 64 * mask_words)
+    return fail(SNA_E_CFG_RANGE, "masks of %d words do not reach the last of %d tokens", mask_words, batch->max_new);
+  if ((uintptr_t)masks_dev & 7 || ((uintptr_t)prefix_dev | (uintptr_t)positions_dev) & 3) return fail(SNA_E_CFG_ALIGN, "masks, prefix or positions are not aligned to their elements");
+  PagedAttnArgs a = {};
+  a.masks = (const unsigned long long*)masks_dev;
+  a.words = mask_words;
+  a.prefix = prefix_dev;
+  a.positions = positions_dev;
+  return attend(cache, batch, q_heads, q, out, scale, window, need, workspace_dev, workspace_bytes, a, hip_stream, "tree_attention");
 }
 
 sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, int64_t target_row_stride, const float* draft_dev,
@@ -165,6 +201,102 @@ sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, 
                         n_draft_dev, out_dev, accepted_dev, n_steps, vocab};
   const hipError_t e = launch_verify(a, token_bytes, n_seqs, (hipStream_t)hip_stream);
   return launched(e, "verify_draft");
+}
+
+sna_status sna_verify_tree(const sna_paged_batch* batch, const void* sampled_dev, int32_t sampled_bytes, const void* tokens_dev, int32_t token_bytes,
+                           const int32_t* parents_dev, int32_t* kept_dev, int32_t* counts_dev, int32_t* next_dev, void* hip_stream) {
+  if (!batch) return fail(SNA_E_NULL, "paged batch: NULL");
+  if (batch->n_seqs < 0 || batch->n_seqs > (1 << 20) || batch->n_tokens < 0 || batch->n_tokens > (1 << 26) || batch->max_new < 0 || batch->max_new > kTreeTokens)
+    return fail(SNA_E_CFG_RANGE, "verify_tree: %d sequences, %d tokens, trees of %d (up to %d are supported)", batch->n_seqs, batch->n_tokens, batch->max_new, kTreeTokens);
+  for (const int32_t bytes : {sampled_bytes, token_bytes})
+    if (bytes != 4 && bytes != 8) return fail(SNA_E_CFG_RANGE, "verify_tree: tokens of %d bytes (4 and 8 are supported)", bytes);
+  if (batch->n_seqs == 0) return batch->n_tokens ? fail(SNA_E_CFG_RANGE, "paged batch: %d tokens of no sequence", batch->n_tokens) : SNA_OK;
+  if (!batch->starts_dev || !batch->lens_dev || (batch->n_tokens && (!sampled_dev || !tokens_dev || !parents_dev)) || (batch->max_new && !kept_dev) || !counts_dev || !next_dev)
+    return fail(SNA_E_NULL, "verify_tree: a required pointer is NULL");
+  if (((uintptr_t)parents_dev | (uintptr_t)kept_dev | (uintptr_t)counts_dev | (uintptr_t)next_dev) & 3 || (uintptr_t)sampled_dev & (sampled_bytes - 1) || (uintptr_t)tokens_dev & (token_bytes - 1))
+    return fail(SNA_E_CFG_ALIGN, "verify_tree: a pointer is not aligned to its elements");
+  const TreeWalkArgs a = {seqs_of(batch), sampled_dev, tokens_dev, sampled_bytes, token_bytes, parents_dev, kept_dev, counts_dev, next_dev, batch->max_new};
+  return launched(launch_verify_tree(a, (hipStream_t)hip_stream), "verify_tree");
+}
+
+sna_status sna_kv_compact(const sna_paged_cache* cache, const sna_paged_batch* batch, const int32_t* kept_dev, int32_t kept_width, const int32_t* counts_dev,
+                          int32_t* lens_dev, void* hip_stream) {
+  sna_status st;
+  if ((st = check_cache(cache)) != SNA_OK) return st;
+  if (!batch) return fail(SNA_E_NULL, "paged batch: NULL");
+  if (batch->n_seqs < 0 || batch->n_seqs > (1 << 20) || batch->max_new < 0 || batch->max_new > (1 << 26) || kept_width < 0 || kept_width > (1 << 26))
+    return fail(SNA_E_CFG_RANGE, "kv_compact: %d sequences, %d new tokens, %d kept", batch->n_seqs, batch->max_new, kept_width);
+  if (batch->n_seqs == 0) return SNA_OK;
+  if (!batch->starts_dev || !batch->lens_dev || !batch->page_table_dev || (kept_width && !kept_dev) || !counts_dev || !lens_dev)
+    return fail(SNA_E_NULL, "kv_compact: a required pointer is NULL");
+  if (batch->table_width < 1 || batch->table_stride < 0 || batch->table_stride > INT32_MAX) return fail(SNA_E_CFG_RANGE, "paged batch: page table of %d columns", batch->table_width);
+  if (lens_dev == batch->lens_dev || lens_dev == batch->starts_dev || lens_dev == counts_dev || lens_dev == kept_dev)
+    return fail(SNA_E_CFG_RANGE, "kv_compact: the new lengths are written over what is read");
+  if (((uintptr_t)kept_dev | (uintptr_t)counts_dev | (uintptr_t)lens_dev) & 3) return fail(SNA_E_CFG_ALIGN, "kv_compact: a pointer is not aligned to its elements");
+  CompactArgs a = {};
+  a.s = seqs_of(batch);
+  a.s.T = INT32_MAX / 2;                                             // rows are not looked at
+  a.s.max_len = 1 << 30;
+  a.kv = kv_of(cache);
+  a.kept = kept_dev; a.counts = counts_dev; a.lens = lens_dev;
+  a.width = kept_width;
+  a.max_new = batch->max_new;
+  a.dim = cache->head_dim;
+  return launched(launch_compact(a, (hipStream_t)hip_stream), "kv_compact");
+}
+
+sna_status sna_copy_pages(const sna_paged_cache* cache, const int32_t* source_dev, const int32_t* target_dev, int32_t n, void* hip_stream) {
+  sna_status st;
+  if ((st = check_cache(cache)) != SNA_OK) return st;
+  if (n < 0) return fail(SNA_E_CFG_RANGE, "copy_pages: %d pages", n);
+  if (n == 0) return SNA_OK;
+  if (!source_dev || !target_dev) return fail(SNA_E_NULL, "copy_pages: a required pointer is NULL");
+  if (((uintptr_t)source_dev | (uintptr_t)target_dev) & 3) return fail(SNA_E_CFG_ALIGN, "copy_pages: a pointer is not aligned to its elements");
+  PageCopyArgs a = {};
+  a.kv = kv_of(cache);
+  a.source = source_dev; a.target = target_dev;
+  a.bytes = 2l * cache->kv_heads * cache->page_size * cache->head_dim;
+  return launched(launch_copy_pages(a, n, (hipStream_t)hip_stream), "copy_pages");
+}
+
+static sna_status check_sampling(const sna_sampling* s) {
+  if (!s) return fail(SNA_E_NULL, "sampling: NULL");
+  if (s->n_rows < 0 || s->n_rows > (1 << 24) || s->vocab < 1 || s->vocab > (1 << 20) || s->row_stride < 0)
+    return fail(SNA_E_CFG_RANGE, "sample_tokens: %d rows, vocabulary of %d (up to 2^20 is supported)", s->n_rows, s->vocab);
+  if (s->dtype < SNA_DTYPE_FP32 || s->dtype > SNA_DTYPE_FP16) return fail(SNA_E_CFG_RANGE, "sample_tokens: dtype %d", s->dtype);
+  if (!s->temperature_dev && !(s->temperature >= 0.f && s->temperature < INFINITY)) return fail(SNA_E_CFG_RANGE, "sample_tokens: temperature %g", (double)s->temperature);
+  if (!s->top_k_dev && s->top_k < 0) return fail(SNA_E_CFG_RANGE, "sample_tokens: top_k %d", s->top_k);
+  if (!s->top_p_dev && !(s->top_p >= 0.f && s->top_p <= 1.f)) return fail(SNA_E_CFG_RANGE, "sample_tokens: top_p %g", (double)s->top_p);
+  if (!s->min_p_dev && !(s->min_p >= 0.f && s->min_p <= 1.f)) return fail(SNA_E_CFG_RANGE, "sample_tokens: min_p %g", (double)s->min_p);
+  return SNA_OK;
+}
+
+int64_t sna_sample_tokens_workspace_bytes(const sna_sampling* s) {
+  const sna_status st = check_sampling(s);
+  return st != SNA_OK ? st : s->n_rows ? (int64_t)sample_workspace(s->n_rows, s->vocab, s->dtype) : 0;
+}
+
+sna_status sna_sample_tokens(const sna_sampling* s, int32_t* tokens_dev, float* probs_dev, int64_t probs_stride, void* workspace_dev, size_t workspace_bytes,
+                             void* hip_stream) {
+  const int64_t need = sna_sample_tokens_workspace_bytes(s);
+  if (need < 0) return (sna_status)need;
+  if (s->n_rows == 0) return SNA_OK;
+  if (!s->logits_dev || !s->uniforms_dev || !tokens_dev) return fail(SNA_E_NULL, "sample_tokens: a required pointer is NULL");
+  if (probs_dev && s->n_rows > 1 && probs_stride < s->vocab) return fail(SNA_E_CFG_RANGE, "sample_tokens: rows of probabilities overlap");
+  if (((uintptr_t)s->uniforms_dev | (uintptr_t)s->temperature_dev | (uintptr_t)s->top_k_dev | (uintptr_t)s->top_p_dev | (uintptr_t)s->min_p_dev | (uintptr_t)tokens_dev | (uintptr_t)probs_dev) & 3 ||
+      (uintptr_t)s->logits_dev & (s->dtype == SNA_DTYPE_FP32 ? 3 : 1))
+    return fail(SNA_E_CFG_ALIGN, "sample_tokens: a pointer is not aligned to its elements");
+  if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))
+    return fail(SNA_E_WORKSPACE, "sample_tokens: a workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
+  SampleArgs a = {};
+  a.logits = s->logits_dev; a.stride = s->row_stride;
+  a.u = s->uniforms_dev;
+  a.temperature_of = s->temperature_dev; a.top_k_of = s->top_k_dev; a.top_p_of = s->top_p_dev; a.min_p_of = s->min_p_dev;
+  a.temperature = s->temperature; a.top_k = s->top_k; a.top_p = s->top_p; a.min_p = s->min_p;
+  a.V = s->vocab; a.n = s->n_rows;
+  a.tokens = tokens_dev; a.probs = probs_dev; a.p_stride = probs_stride;
+  a.work = workspace_dev;
+  return launched(launch_sample(a, s->dtype, (hipStream_t)hip_stream), "sample_tokens");
 }
 
 }

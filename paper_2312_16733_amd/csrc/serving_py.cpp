@@ -332,10 +332,22 @@ int vector_of(PyObject* o, const char* name, int64_t n, const Cache* c, const fl
   return 1;
 }
 
+// A dense int32 vector of n, or none
+int ints_of(PyObject* o, const char* name, int64_t n, c10::Device device, const int32_t** p) {
+  *p = nullptr;
+  if (none(o)) return 1;
+  const at::Tensor* t = tensor_of(o, name);
+  if (!t) return 0;
+  NEED(t->scalar_type() == at::kInt && t->device() == device && t->dim() == 1 && t->size(0) == n && (n <= 1 || t->stride(0) == 1), "%s: dense int32 [%lld] on %s is needed, got %s", name,
+       (long long)n, device.str().c_str(), shape_of(*t).c_str());
+  *p = (const int32_t*)t->data_ptr();
+  return 1;
+}
+
 PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
   HANDLE_TH_ERRORS
-  static const char* const names[] = {"cache", "batch", "q", "k", "v", "inv_freq", "interleaved", "q_norm", "k_norm", "eps", "out", "stream"};
-  PyObject* a[12];
+  static const char* const names[] = {"cache", "batch", "q", "k", "v", "inv_freq", "interleaved", "q_norm", "k_norm", "eps", "out", "stream", "positions"};
+  PyObject* a[13];
   if (!arguments("kv_append", names, 5, args, n, kw, a)) return nullptr;
   Step s;
   if (!step_of(&s, a[0], a[1], a[2], a[10])) return nullptr;
@@ -347,6 +359,8 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw
   int64_t pairs = 0, dim = s.cache->c.head_dim, ignored;
   if (!vector_of(a[5], "inv_freq", -1, s.cache, &inv, &pairs) || !vector_of(a[7], "q_norm", dim, s.cache, &qn, &ignored) || !vector_of(a[8], "k_norm", dim, s.cache, &kn, &ignored)) return nullptr;
   NEED(pairs <= dim, "inv_freq: %lld pairs of a head of %lld", (long long)pairs, (long long)dim);
+  const int32_t* positions;
+  if (!ints_of(a[12], "positions", s.q->size(0), *s.cache->device, &positions)) return nullptr;
   const int interleaved = none(a[6]) ? 0 : PyObject_IsTrue(a[6]);
   double eps = 1e-6;
   if (interleaved < 0 || !real_number(a[9], &eps)) return nullptr;
@@ -354,11 +368,51 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw
   if (!on.begin(a[11], s.cache->device->index()) || !out_of(&s)) return nullptr;
   sna_status st;
   Py_BEGIN_ALLOW_THREADS
-  st = sna_kv_append(&s.cache->c, &s.batch, (int32_t)s.q->size(1), &s.q_rows, &k, &v, &s.out_rows, inv, (int32_t)(2 * pairs), interleaved, qn, kn, (float)eps, on.raw());
+  st = sna_kv_append_at(&s.cache->c, &s.batch, (int32_t)s.q->size(1), &s.q_rows, &k, &v, &s.out_rows, inv, (int32_t)(2 * pairs), interleaved, qn, kn, (float)eps, positions, on.raw());
   Py_END_ALLOW_THREADS
   if (!status(st)) return nullptr;
   return none(a[10]) ? THPVariable_Wrap(std::move(s.out)) : Py_NewRef(a[10]);
   END_HANDLE_TH_ERRORS
+}
+
+// What the caller brought, where it is large enough, or the allocator's, on the call's stream
+int workspace_of(PyObject* o, int64_t need, const at::Tensor& like, at::Tensor* workspace) {
+  if (need <= 0) return 1;
+  const at::Tensor* given = none(o) ? nullptr : tensor_of(o, "workspace");
+  if (!none(o) && !given) return 0;
+  NEED(!given || (given->scalar_type() == at::kByte && given->device() == like.device() && given->is_contiguous()), "workspace: dense uint8 on %s is needed, got %s",
+       like.device().str().c_str(), shape_of(*given).c_str());
+  *workspace = given && given->numel() >= need ? *given : at::empty({need}, like.options().dtype(at::kByte));
+  return 1;
+}
+
+// What both forms of attention share behind their own arguments.  No words: causal
+struct Masks {
+  const uint64_t* masks;
+  int32_t words;
+  const int32_t *prefix, *positions;
+};
+PyObject* attend(Step& s, const Masks& m, PyObject* scale_o, PyObject* window_o, PyObject* out_o, PyObject* workspace_o, PyObject* stream_o) {
+  double scale = 1.0 / std::sqrt((double)s.cache->c.head_dim);
+  int64_t window = 0;
+  if (!real_number(scale_o, &scale) || !whole_number(window_o, &window)) return nullptr;
+  NEED(window >= 0 && window <= INT32_MAX, "window: %lld is out of range", (long long)window);
+  const int32_t heads = (int32_t)s.q->size(1);
+  const int64_t need = m.words ? sna_tree_attention_workspace_bytes(&s.cache->c, &s.batch, heads, m.words, (int32_t)window)
+                               : sna_paged_attention_workspace_bytes(&s.cache->c, &s.batch, heads, (int32_t)window);
+  if (!status(need)) return nullptr;
+  On on;
+  if (!on.begin(stream_o, s.cache->device->index()) || !out_of(&s)) return nullptr;
+  at::Tensor workspace;
+  if (!workspace_of(workspace_o, need, *s.q, &workspace)) return nullptr;
+  void* ws = need > 0 ? workspace.data_ptr() : nullptr;
+  sna_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = m.words ? sna_tree_attention(&s.cache->c, &s.batch, heads, &s.q_rows, &s.out_rows, m.masks, m.words, m.prefix, m.positions, (float)scale, (int32_t)window, ws, (size_t)need, on.raw())
+               : sna_paged_attention(&s.cache->c, &s.batch, heads, &s.q_rows, &s.out_rows, (float)scale, (int32_t)window, ws, (size_t)need, on.raw());
+  Py_END_ALLOW_THREADS
+  if (!status(st)) return nullptr;
+  return none(out_o) ? THPVariable_Wrap(std::move(s.out)) : Py_NewRef(out_o);
 }
 
 PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
@@ -368,29 +422,26 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObje
   if (!arguments("paged_attention", names, 3, args, n, kw, a)) return nullptr;
   Step s;
   if (!step_of(&s, a[0], a[1], a[2], a[5])) return nullptr;
-  double scale = 1.0 / std::sqrt((double)s.cache->c.head_dim);
-  int64_t window = 0;
-  if (!real_number(a[3], &scale) || !whole_number(a[4], &window)) return nullptr;
-  NEED(window >= 0 && window <= INT32_MAX, "window: %lld is out of range", (long long)window);
-  const int32_t heads = (int32_t)s.q->size(1);
-  const int64_t need = sna_paged_attention_workspace_bytes(&s.cache->c, &s.batch, heads, (int32_t)window);
-  if (!status(need)) return nullptr;
-  On on;
-  if (!on.begin(a[7], s.cache->device->index()) || !out_of(&s)) return nullptr;
-  at::Tensor workspace;
-  if (need > 0) {
-    const at::Tensor* given = none(a[6]) ? nullptr : tensor_of(a[6], "workspace");
-    if (!none(a[6]) && !given) return nullptr;
-    NEED(!given || (given->scalar_type() == at::kByte && given->device() == *s.cache->device && given->is_contiguous()), "workspace: dense uint8 on %s is needed, got %s",
-         s.cache->device->str().c_str(), shape_of(*given).c_str());
-    workspace = given && given->numel() >= need ? *given : at::empty({need}, s.q->options().dtype(at::kByte));
-  }
-  sna_status st;
-  Py_BEGIN_ALLOW_THREADS
-  st = sna_paged_attention(&s.cache->c, &s.batch, heads, &s.q_rows, &s.out_rows, (float)scale, (int32_t)window, need > 0 ? workspace.data_ptr() : nullptr, (size_t)need, on.raw());
-  Py_END_ALLOW_THREADS
-  if (!status(st)) return nullptr;
-  return none(a[5]) ? THPVariable_Wrap(std::move(s.out)) : Py_NewRef(a[5]);
+  return attend(s, Masks{}, a[3], a[4], a[5], a[6], a[7]);
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* tree_attention(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"cache", "batch", "q", "masks", "prefix", "positions", "scale", "window", "out", "workspace", "stream"};
+  PyObject* a[11];
+  if (!arguments("tree_attention", names, 4, args, n, kw, a)) return nullptr;
+  Step s;
+  if (!step_of(&s, a[0], a[1], a[2], a[8])) return nullptr;
+  const at::Tensor* t = tensor_of(a[3], "masks");
+  if (!t) return nullptr;
+  NEED(t->dim() == 2 && t->size(0) == s.q->size(0) && t->size(1) >= 1 && t->size(1) <= 64 && t->scalar_type() == at::kLong && t->device() == *s.cache->device && t->is_contiguous(),
+       "masks: dense int64 [%lld][words], 1 to 64 words, on %s is needed, got %s", (long long)s.q->size(0), s.cache->device->str().c_str(), shape_of(*t).c_str());
+  Masks m = {};
+  m.words = (int32_t)t->size(1);
+  m.masks = (const uint64_t*)t->data_ptr();
+  if (!ints_of(a[4], "prefix", s.batch.n_seqs, *s.cache->device, &m.prefix) || !ints_of(a[5], "positions", s.q->size(0), *s.cache->device, &m.positions)) return nullptr;
+  return attend(s, m, a[6], a[7], a[8], a[9], a[10]);
   END_HANDLE_TH_ERRORS
 }
 
@@ -439,12 +490,199 @@ PyObject* verify_draft(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObj
   END_HANDLE_TH_ERRORS
 }
 
+PyObject* wrapped(std::initializer_list<at::Tensor> tensors) {
+  PyObject* r = PyTuple_New((Py_ssize_t)tensors.size());
+  Py_ssize_t i = 0;
+  for (const at::Tensor& t : tensors) {
+    PyObject* x = r ? THPVariable_Wrap(t) : nullptr;
+    if (!x) {
+      Py_XDECREF(r);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(r, i++, x);
+  }
+  return r;
+}
+const Batch* batch_of(PyObject* o) {
+  if (!PyObject_TypeCheck(o, batch_type)) {
+    PyErr_SetString(PyExc_TypeError, "a PagedBatch is needed");
+    return nullptr;
+  }
+  return is_current((Batch*)o) ? (Batch*)o : nullptr;
+}
+const Cache* cache_of(PyObject* o) {
+  if (!PyObject_TypeCheck(o, cache_type)) {
+    PyErr_SetString(PyExc_TypeError, "a PagedCache is needed");
+    return nullptr;
+  }
+  return is_current((Cache*)o) ? (Cache*)o : nullptr;
+}
+
+// Dense tokens [n], int32 or int64
+const at::Tensor* tokens_of(PyObject* o, const char* name, int64_t n, c10::Device device) {
+  const at::Tensor* t = tensor_of(o, name);
+  if (!t) return nullptr;
+  NEED(t->dim() == 1 && (n < 0 || t->size(0) == n) && (t->scalar_type() == at::kInt || t->scalar_type() == at::kLong) && t->device() == device && t->is_contiguous(),
+       "%s: dense int32 or int64 [%s] on %s is needed, got %s", name, n < 0 ? "tokens" : std::to_string(n).c_str(), device.str().c_str(), shape_of(*t).c_str());
+  return t;
+}
+
+PyObject* verify_tree(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"batch", "sampled", "tokens", "parents", "stream"};
+  PyObject* a[5];
+  if (!arguments("verify_tree", names, 4, args, nargs, kw, a)) return nullptr;
+  const Batch* b = batch_of(a[0]);
+  if (!b) return nullptr;
+  const c10::Device device = *b->device;
+  const at::Tensor *sampled = tokens_of(a[1], "sampled", -1, device), *tokens = sampled ? tokens_of(a[2], "tokens", sampled->size(0), device) : nullptr;
+  if (!tokens) return nullptr;
+  const int64_t n = tokens->size(0);
+  NEED(n <= INT32_MAX, "tokens: %s is out of range", shape_of(*tokens).c_str());
+  const at::Tensor* p = tensor_of(a[3], "parents");
+  const int32_t* parents;
+  if (!p || !ints_of(a[3], "parents", n, device, &parents)) return nullptr;
+  sna_paged_batch c = b->c;
+  c.n_tokens = (int32_t)n;
+  On on;
+  if (!on.begin(a[4], device.index())) return nullptr;
+  const auto options = THPVariable_Unpack(b->lens).options();
+  at::Tensor kept = at::empty({c.n_seqs, c.max_new}, options), counts = at::empty({c.n_seqs}, options), next = at::empty({c.n_seqs}, options);
+  sna_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sna_verify_tree(&c, sampled->data_ptr(), (int32_t)sampled->element_size(), tokens->data_ptr(), (int32_t)tokens->element_size(), parents, (int32_t*)kept.data_ptr(), (int32_t*)counts.data_ptr(),
+                       (int32_t*)next.data_ptr(), on.raw());
+  Py_END_ALLOW_THREADS
+  return status(st) ? wrapped({kept, counts, next}) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* kv_compact(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"cache", "batch", "kept", "counts", "stream"};
+  PyObject* a[5];
+  if (!arguments("kv_compact", names, 4, args, nargs, kw, a)) return nullptr;
+  const Cache* c = cache_of(a[0]);
+  const Batch* b = c ? batch_of(a[1]) : nullptr;
+  if (!b) return nullptr;
+  NEED(*b->device == *c->device, "the batch is on %s, the cache on %s", b->device->str().c_str(), c->device->str().c_str());
+  const at::Tensor* kept = tensor_of(a[2], "kept");
+  if (!kept) return nullptr;
+  NEED(kept->dim() == 2 && kept->size(0) == b->c.n_seqs && kept->size(1) <= INT32_MAX && kept->scalar_type() == at::kInt && kept->device() == *c->device && kept->is_contiguous(),
+       "kept: dense int32 [%d][tokens] on %s is needed, got %s", b->c.n_seqs, c->device->str().c_str(), shape_of(*kept).c_str());
+  const int32_t* counts;
+  if (!tensor_of(a[3], "counts") || !ints_of(a[3], "counts", b->c.n_seqs, *c->device, &counts)) return nullptr;
+  On on;
+  if (!on.begin(a[4], c->device->index())) return nullptr;
+  at::Tensor lens = at::empty({b->c.n_seqs}, THPVariable_Unpack(b->lens).options());
+  sna_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sna_kv_compact(&c->c, &b->c, (const int32_t*)kept->data_ptr(), (int32_t)kept->size(1), counts, (int32_t*)lens.data_ptr(), on.raw());
+  Py_END_ALLOW_THREADS
+  return status(st) ? THPVariable_Wrap(std::move(lens)) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* copy_pages(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"cache", "source", "target", "stream"};
+  PyObject* a[4];
+  if (!arguments("copy_pages", names, 3, args, nargs, kw, a)) return nullptr;
+  const Cache* c = cache_of(a[0]);
+  const at::Tensor* from = c ? tensor_of(a[1], "source") : nullptr;
+  if (!from || !tensor_of(a[2], "target")) return nullptr;
+  const int64_t n = from->dim() == 1 ? from->size(0) : 0;
+  const int32_t *source, *target;
+  if (!ints_of(a[1], "source", n, *c->device, &source) || !ints_of(a[2], "target", n, *c->device, &target)) return nullptr;
+  NEED(n <= INT32_MAX, "source: %s is out of range", shape_of(*from).c_str());
+  On on;
+  if (!on.begin(a[3], c->device->index())) return nullptr;
+  sna_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sna_copy_pages(&c->c, source, target, (int32_t)n, on.raw());
+  Py_END_ALLOW_THREADS
+  if (!status(st)) return nullptr;
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// A number for all rows, or a dense vector of one for each
+int setting(PyObject* o, const char* name, int64_t n, at::ScalarType type, c10::Device device, const void** of, double* all) {
+  *of = nullptr;
+  if (none(o)) return 1;
+  if (!THPVariable_Check(o)) return real_number(o, all);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  NEED(t.dim() == 1 && t.size(0) == n && t.scalar_type() == type && t.device() == device && (n <= 1 || t.stride(0) == 1), "%s: a number or dense %s [%lld] on %s is needed, got %s", name,
+       c10::toString(type), (long long)n, device.str().c_str(), shape_of(t).c_str());
+  *of = t.data_ptr();
+  return 1;
+}
+
+PyObject* sample_tokens(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+  HANDLE_TH_ERRORS
+  static const char* const names[] = {"logits", "uniforms", "temperature", "top_k", "top_p", "min_p", "probs", "out", "workspace", "stream"};
+  PyObject* a[10];
+  if (!arguments("sample_tokens", names, 2, args, nargs, kw, a)) return nullptr;
+  const at::Tensor *l = tensor_of(a[0], "logits"), *u = l ? tensor_of(a[1], "uniforms") : nullptr;
+  if (!u) return nullptr;
+  const at::ScalarType type = l->scalar_type();
+  NEED(l->dim() == 2 && (type == at::kFloat || type == at::kBFloat16 || type == at::kHalf) && l->is_cuda() && l->size(1) >= 1 && (l->size(1) == 1 || l->stride(1) == 1),
+       "logits: fp32, bf16 or fp16 [rows][vocabulary], dense rows on a GPU are needed, got %s", shape_of(*l).c_str());
+  const int64_t n = l->size(0), V = l->size(1);
+  const c10::Device device = l->device();
+  NEED(n <= INT32_MAX && V <= INT32_MAX, "logits: %s is out of range", shape_of(*l).c_str());
+  NEED(u->dim() == 1 && u->size(0) == n && u->scalar_type() == at::kFloat && u->device() == device && (n <= 1 || u->stride(0) == 1), "uniforms: dense fp32 [%lld] on %s is needed, got %s", (long long)n,
+       device.str().c_str(), shape_of(*u).c_str());
+  double temperature = 1.0, top_k = 0.0, top_p = 1.0, min_p = 0.0;
+  sna_sampling s = {};
+  if (!setting(a[2], "temperature", n, at::kFloat, device, (const void**)&s.temperature_dev, &temperature) || !setting(a[3], "top_k", n, at::kInt, device, (const void**)&s.top_k_dev, &top_k) ||
+      !setting(a[4], "top_p", n, at::kFloat, device, (const void**)&s.top_p_dev, &top_p) || !setting(a[5], "min_p", n, at::kFloat, device, (const void**)&s.min_p_dev, &min_p))
+    return nullptr;
+  NEED(top_k >= 0.0 && top_k <= INT32_MAX && top_k == std::floor(top_k), "top_k: %s is no count", std::to_string(top_k).c_str());
+  s.logits_dev = l->data_ptr();
+  s.row_stride = n > 1 ? l->stride(0) : 0;
+  s.n_rows = (int32_t)n;
+  s.vocab = (int32_t)V;
+  s.dtype = type == at::kFloat ? SNA_DTYPE_FP32 : type == at::kHalf ? SNA_DTYPE_FP16 : SNA_DTYPE_BF16;
+  s.top_k = (int32_t)top_k;
+  s.temperature = (float)temperature;
+  s.top_p = (float)top_p;
+  s.min_p = (float)min_p;
+  s.uniforms_dev = (const float*)u->data_ptr();
+  const int64_t need = sna_sample_tokens_workspace_bytes(&s);
+  if (!status(need)) return nullptr;
+  const at::Tensor *given_probs = !none(a[6]) && THPVariable_Check(a[6]) ? &THPVariable_Unpack(a[6]) : nullptr, *given_out = none(a[7]) ? nullptr : tensor_of(a[7], "out");
+  if (!none(a[7]) && !given_out) return nullptr;
+  NEED(!given_probs || (given_probs->dim() == 2 && given_probs->sizes() == l->sizes() && given_probs->scalar_type() == at::kFloat && given_probs->device() == device &&
+                        (V == 1 || given_probs->stride(1) == 1)),
+       "probs: fp32 (%lld, %lld), dense rows on %s are needed, got %s", (long long)n, (long long)V, device.str().c_str(), shape_of(*given_probs).c_str());
+  NEED(!given_out || (given_out->dim() == 1 && given_out->size(0) == n && given_out->scalar_type() == at::kInt && given_out->device() == device && (n <= 1 || given_out->stride(0) == 1)),
+       "out: dense int32 [%lld] on %s is needed, got %s", (long long)n, device.str().c_str(), shape_of(*given_out).c_str());
+  const int want_probs = given_probs ? 1 : none(a[6]) ? 0 : PyObject_IsTrue(a[6]);
+  if (want_probs < 0) return nullptr;
+  On on;
+  if (!on.begin(a[9], device.index())) return nullptr;
+  at::Tensor workspace, tokens = given_out ? *given_out : at::empty({n}, l->options().dtype(at::kInt)), probs;
+  if (want_probs) probs = given_probs ? *given_probs : at::empty({n, V}, l->options().dtype(at::kFloat));
+  if (!workspace_of(a[8], need, *l, &workspace)) return nullptr;
+  void* ws = need > 0 ? workspace.data_ptr() : nullptr;
+  float* p = want_probs && n ? (float*)probs.data_ptr() : nullptr;
+  sna_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sna_sample_tokens(&s, (int32_t*)tokens.data_ptr(), p, p && n > 1 ? probs.stride(0) : V, ws, (size_t)need, on.raw());
+  Py_END_ALLOW_THREADS
+  if (!status(st)) return nullptr;
+  return want_probs ? wrapped({tokens, probs}) : THPVariable_Wrap(std::move(tokens));
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"kv_append", (PyCFunction)(void*)kv_append, METH_FASTCALL | METH_KEYWORDS,
-     "kv_append(cache, batch, q, k, v, inv_freq=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6, out=None, stream=None)\n\n"
+     "kv_append(cache, batch, q, k, v, inv_freq=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6, out=None, stream=None, positions=None)\n\n"
      "Stores the step's k and v [tokens][kv_heads][head_dim] in the cache and returns its q [tokens][heads][head_dim], q and k\n"
      "normalised per head (fp32 q_norm and k_norm [head_dim], both or neither) and rotated (fp32 inv_freq [rot_dim / 2]; pairs\n"
-     "i and i + rot_dim / 2, or 2 i and 2 i + 1 where `interleaved`).  Strided q, k and v are read in place.  `out` may be q."},
+     "i and i + rot_dim / 2, or 2 i and 2 i + 1 where `interleaved`).  Strided q, k and v are read in place.  `out` may be q.\n"
+     "positions int32 [tokens]: what the rotation goes by where it is not the slot's number, as in trees."},
     {"paged_attention", (PyCFunction)(void*)paged_attention, METH_FASTCALL | METH_KEYWORDS,
      "paged_attention(cache, batch, q, scale=None, window=0, out=None, workspace=None, stream=None)\n\n"
      "Causal attention of the step's q [tokens][heads][head_dim] over the cached keys and values, these tokens' own among them\n"
@@ -457,6 +695,34 @@ PyMethodDef methods[] = {
      "each draft, the last for the draw; draft_probs fp32 [n][K][V] that the drafts were drawn from, or None where they were\n"
      "chosen without chance; n_draft int32 [n]: how many of the K each sequence has (all).  Returns (out int32 [n][K + 1],\n"
      "accepted int32 [n]): the accepted drafts, the drawn token, -1 behind it."},
+    {"tree_attention", (PyCFunction)(void*)tree_attention, METH_FASTCALL | METH_KEYWORDS,
+     "tree_attention(cache, batch, q, masks, prefix=None, positions=None, scale=None, window=0, out=None, workspace=None, stream=None)\n\n"
+     "Attention of the tokens of drafted trees q [tokens][heads][head_dim] over the cached keys and values, theirs among them (after\n"
+     "kv_append).  A sequence's tree begins behind its first prefix[b] slots (int32 [n]; None: all but the step's own tokens).  A token\n"
+     "sees what lies before the tree, and slot prefix + 64 w + j where bit j of masks[token][w] is set (int64 [tokens][words], up\n"
+     "to 64 words; see tree_masks).  window: how far back it sees before the tree, from its position (int32 [tokens]; None: its\n"
+     "slot); 0: all.  The rest is as for paged_attention."},
+    {"verify_tree", (PyCFunction)(void*)verify_tree, METH_FASTCALL | METH_KEYWORDS,
+     "verify_tree(batch, sampled, tokens, parents, stream=None)\n\n"
+     "Which tokens of the step's trees stand.  A sequence's first token is its root and stands; behind one that stands its first child\n"
+     "(parents int32 [tokens]: a number within the sequence) whose token is sampled[parent] does, too.  sampled, tokens [tokens]\n"
+     "int32 or int64.  Returns (kept int32 [n][max_new]: their numbers within the sequence, then -1; counts int32 [n]; next int32\n"
+     "[n]: the token sampled behind the last)."},
+    {"kv_compact", (PyCFunction)(void*)kv_compact, METH_FASTCALL | METH_KEYWORDS,
+     "kv_compact(cache, batch, kept, counts, stream=None)\n\n"
+     "Moves the keys and values of the kept ones of the step's tokens (kept int32 [n][any], rising, counts[b] of them) up to the first\n"
+     "slots of the step, and returns the new lengths int32 [n].  A pool whose layers lie next to each other within a page goes in\n"
+     "one call, as a PagedCache of layers * kv_heads heads."},
+    {"copy_pages", (PyCFunction)(void*)copy_pages, METH_FASTCALL | METH_KEYWORDS,
+     "copy_pages(cache, source, target, stream=None)\n\n"
+     "Copies page source[i] over page target[i] (int32 [n]), keys and values.  No target is another's target or source."},
+    {"sample_tokens", (PyCFunction)(void*)sample_tokens, METH_FASTCALL | METH_KEYWORDS,
+     "sample_tokens(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, probs=False, out=None, workspace=None, stream=None)\n\n"
+     "A token int32 [n] of each row of logits [n][V] (fp32, bf16 or fp16) by uniforms fp32 [n] from [0, 1): of the top_k largest (0:\n"
+     "all; ties go to the lower token) the fewest that make top_p of their weights exp(logit / temperature), of these the ones with\n"
+     "at least min_p of the largest's; drawn by running sums in token order.  Temperature 0: the largest.  -1 where no logit is more\n"
+     "than -inf (NaN counts as that).  Each setting is a number or a tensor [n] (top_k int32, the others fp32).  probs: True, or an\n"
+     "fp32 [n][V] to write to: (tokens, probs) is returned, the probabilities that the token was drawn by."},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
