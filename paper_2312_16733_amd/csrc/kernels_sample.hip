@@ -10,6 +10,7 @@
 // many blocks as fill the chip: for the largest; for counts or weights by distance from it (where a row is cut); and for what lies at
 // the cut, a short list, and the sums of what is kept for certain, by runs of 512.  Then one block a row has the list and the sums.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -27,66 +28,137 @@ constexpr int SM_FINAL = 1024;     // of the one that ends it
 __device__ __forceinline__ float logit(const float* p, long i) { return p[i]; }
 __device__ __forceinline__ float logit(const __bf16* p, long i) { return (float)p[i]; }
 __device__ __forceinline__ float logit(const _Float16* p, long i) { return (float)p[i]; }
-// What a row's logit counts as: no number as none, both zeros as one
-__device__ __forceinline__ float taken(float x) { return x == x ? x + 0.f : -INFINITY; }
-// Rises as the logit falls; an order of all floats
+// What a row's logit counts as: no number as none
+__device__ __forceinline__ float taken(float x) { return x == x ? x : -INFINITY; }
+// Rises as the logit falls; an order of all floats, both zeros as one
 __device__ __forceinline__ unsigned falling(float x) {
-  const unsigned u = __float_as_uint(x);
+  const unsigned u = __float_as_uint(x + 0.f);
   return ~(u ^ (unsigned)((int)u >> 31 | (int)0x80000000));
 }
-__device__ __forceinline__ float of_falling(unsigned f) {
-  const unsigned u = ~f;
-  return __uint_as_float(u ^ (u >> 31 ? 0x80000000u : ~0u));
-}
-__device__ __forceinline__ u64 place(float x, int i) { return (u64)falling(x) << 32 | (unsigned)i; }
+// Bits that are the same for all logits of a type and sign: below the last place of its numbers, as fp32
+template <class X> constexpr int kSpare = 0;
+template <> constexpr int kSpare<__bf16> = 16;
+template <> constexpr int kSpare<_Float16> = 13;
 
-struct Row {                       // of logits, and what is wanted of it
-  float top;
-  double inv_t, magic, min_p;
-  u64 cut;                         // place of the last one kept
-  float top_p;
-  int top_k;                       // 0: all
-  __device__ __forceinline__ double weight(float x) const { return x == top ? 1.0 : exp(((double)x - (double)top) * inv_t); }
-  // In steps: the sum with a power of two whose last place is a step
-  __device__ __forceinline__ u64 steps(double w) const { return (u64)__double_as_longlong(w + magic) & 0xfffffffffffffull; }
-  __device__ __forceinline__ u64 weight_of(float x) const { return x > -INFINITY ? steps(weight(x)) : 0; }
-  __device__ __forceinline__ double kept(float x, int i) const {       // the weight of one that is left
-    if (!(x > -INFINITY && place(x, i) <= cut)) return 0.0;
-    const double w = weight(x);
-    return w >= min_p ? w : 0.0;
+// 2^y for -1000 <= y <= 0, off by 7e-16 of itself: y's fraction f within 1/2, and 1 + f times the polynomial through (2^f - 1) / f at
+// ten Chebyshev points, so that 2^0 is 1.  The whole number comes off by adding a power of two whose last place is 1, and goes into
+// the exponent as it is.  Two thirds of the time of the library's, which takes any argument
+struct Power {
+  double c[10];
+  __device__ __forceinline__ void begin() {
+    const double v[10] = {0x1.62e42fefa39f7p-1, 0x1.ebfbdff82c590p-3, 0x1.c6b08d7044119p-5, 0x1.3b2ab6fba385fp-7, 0x1.5d87fe908f88ap-10,
+                              0x1.4309130378460p-13, 0x1.ffcb76789860fp-17, 0x1.62bfe46117445p-20, 0x1.b6571de2f2351p-24, 0x1.e5e9f548e5725p-28};
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+      c[i] = v[i];
+#if defined(__HIP_DEVICE_COMPILE__)
+      asm("" : "+s"(c[i]));                                          // in scalar registers: moved into vector ones, they took as long as the products
+#endif
+    }
+  }
+  __device__ __forceinline__ double of_2(double y) const {
+    const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
+    double p = c[9];
+#pragma unroll
+    for (int i = 8; i >= 0; --i) p = fma(p, f, c[i]);
+    p = fma(p, f, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
   }
 };
+
+struct Row {                       // of logits, and what is wanted of it
+  Power power;
+  double top, per, magic, min_p;   // per: powers of two to one of a logit
+  u64 cut;                         // place of the last one kept
+  float top_p, top32, near;        // near: see distance()
+  int top_k;                       // 0: all
+  int spare, bits;                 // of a logit's order, of an index
+  bool infinite;                   // the largest is +inf: only such have weight
+  __device__ __forceinline__ bool begin(float x) {                   // with the largest; false: nothing to draw from
+    infinite = x == INFINITY;
+    top32 = infinite ? 0.f : x;
+    top = top32;
+    return x > -INFINITY;
+  }
+  __device__ __forceinline__ float seen(float x) const { return infinite ? x == INFINITY ? 0.f : -INFINITY : taken(x); }
+  // Where it stands among the row's
+  __device__ __forceinline__ u64 place(float x, int i) const { return (u64)(falling(x) >> spare) << bits | (unsigned)i; }
+  __device__ __forceinline__ double weight(float x) const { return power.of_2(fmax(((double)x - top) * per, -1000.0)); }      // NaN has none
+  // In steps: the sum with a power of two whose last place is a step
+  __device__ __forceinline__ u64 steps(double w) const { return (u64)__double_as_longlong(w + magic) & 0xfffffffffffffull; }
+  __device__ __forceinline__ double left(double w) const { return w >= min_p ? w : 0.0; }
+  __device__ __forceinline__ double kept(float x, int i) const {       // the weight of one that is left
+    return x > -INFINITY && place(x, i) <= cut ? left(weight(x)) : 0.0;
+  }
+  // Rises as x falls, in SM_BINS steps: 256 even ones of 1 / 64 of the temperature, then twice as wide from 4 temperatures on, and
+  // again from 12, 28, .. on: what 1 and more has of bits behind the leading ones
+  __device__ __forceinline__ int distance(float x) const {
+    return (int)min((__float_as_uint(fmaf(top32 - x, near, 1.f)) >> 15) - (0x3f800000u >> 15), (unsigned)SM_BINS - 1);
+  }
+};
+template <class X>
 __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
   Row r;
+  r.power.begin();
   const float t = a.temperature_of ? a.temperature_of[row] : a.temperature;
   const int k = a.top_k_of ? a.top_k_of[row] : a.top_k;
-  r.inv_t = t > 0.f ? 1.0 / (double)fminf(t, 3.4028235e38f) : 0.0;
+  const double inv = t > 0.f ? 1.0 / (double)fminf(t, 1e33f) : 1.0;
+  r.per = inv * 1.44269504088896340736;
+  r.near = fmaxf((float)fmin(inv * 0.25, 1e38), 1e-38f);
   r.min_p = fmin(fmax((double)(a.min_p_of ? a.min_p_of[row] : a.min_p), 0.0), 1.0);       // what is no number cuts nothing, and the largest stays
   r.magic = __longlong_as_double((long long)(1023 + 52 - a.scale_bits) << 52);
   r.top_p = a.top_p_of ? a.top_p_of[row] : a.top_p;
   r.top_k = t > 0.f ? k > 0 && k < a.V ? k : 0 : 1;
   r.cut = ~0ull;
+  r.spare = kSpare<X>;
+  r.bits = 32 - __builtin_clz(a.V);
+  r.infinite = false;
   return r;
 }
 
-__device__ __forceinline__ u64 scan_up(u64 v) {                      // inclusive, of a wave
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const u64 x = __shfl_up(v, m, 64);
-    if (lane >= m) v += x;
-  }
+// Over a wave, in vector registers: a shuffle through LDS takes 50 cycles and more a step
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned moved(unsigned none, unsigned v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return (unsigned)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false);
+#else
+  return v + none;
+#endif
+}
+template <class F>
+__device__ __forceinline__ u64 scan_of(u64 v, u64 none, const F& f) {                  // inclusive; lanes without a neighbour get `none`
+  const auto step = [&](auto ctrl, auto rows) {
+    const unsigned lo = moved<decltype(ctrl)::value, decltype(rows)::value>((unsigned)none, (unsigned)v), hi = moved<decltype(ctrl)::value, decltype(rows)::value>((unsigned)(none >> 32), (unsigned)(v >> 32));
+    v = f(v, (u64)hi << 32 | lo);
+  };
+  step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());      // within 16 lanes: 1, 2, 4, 8 to the right
+  step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());      // the last of 16 to the 16 behind, in rows 1 and 3
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());      // the last of 32 to the 32 behind
   return v;
 }
-__device__ __forceinline__ u64 sum_of_wave(u64 v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
+__device__ __forceinline__ u64 last_lane(u64 v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  v = (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+#endif
   return v;
 }
+struct Add { __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a + b; } };
+struct Or { __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a | b; } };
+struct And { __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a & b; } };
+__device__ __forceinline__ u64 scan_up(u64 v) { return scan_of(v, 0, Add()); }
+__device__ __forceinline__ u64 sum_of_wave(u64 v) { return last_lane(scan_up(v)); }
 __device__ __forceinline__ float max_of_wave(float v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, 64));
-  return v;
+  const auto step = [&](auto ctrl, auto rows) { v = fmaxf(v, __uint_as_float(moved<decltype(ctrl)::value, decltype(rows)::value>(0xff800000u, __float_as_uint(v)))); };
+  step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());
+  step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());
+  return __uint_as_float((unsigned)last_lane(__float_as_uint(v)));
 }
 
 template <int NT>
@@ -117,17 +189,21 @@ __device__ __forceinline__ float max_of_block(SampleLds<NT>& lds, float v) {
 }
 
 // The bin of lds.sums at which their running sum reaches `want` (1 or more, at most the sum of all), and what comes before it.
-// All threads get both; the sums are complete when it is called, and may be overwritten when it returns.
+// All threads get both; the sums are complete when it is called, and zero when it returns.
 template <int NT>
 __device__ __forceinline__ int crossing(SampleLds<NT>& lds, u64 want, u64& before) {
   constexpr int N = SM_BINS / NT;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   u64 v[N], mine = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) mine += v[i] = lds.sums[N * tid + i];
+  for (int i = 0; i < N; ++i) {
+    mine += v[i] = lds.sums[N * tid + i];
+    lds.sums[N * tid + i] = 0;
+  }
   const u64 up = scan_up(mine);
   if (lane == 63) lds.ups[wave] = up;
   __syncthreads();
+  if (tid == 0) lds.n = 0;
   u64 at = up - mine;
 #pragma unroll
   for (int w = 0; w < NT / 64; ++w) at += w < wave ? lds.ups[w] : 0;
@@ -143,48 +219,53 @@ __device__ __forceinline__ int crossing(SampleLds<NT>& lds, u64 want, u64& befor
 }
 
 // Of all (order, weight) that `each` visits, in rising order: the order at which the running sum of weights reaches `want`, which is
-// 1 .. the sum of all.  Orders differ in their last `bits` bits only.  All threads.
+// 1 .. the sum of all.  Orders differ in their last `bits` bits only.  All threads; lds.sums is zero before and after.
 template <int NT, class Each>
 __device__ __forceinline__ u64 select(SampleLds<NT>& lds, int bits, u64 want, const Each& each) {
-  u64 lo = 0;
-  bool first = true;
-  for (int left = bits; left > 0; first = false) {
-    const int width = min(left, 11), shift = left - width;
-    const u64 mask = left == 64 ? ~0ull : (1ull << left) - 1, same = lo >> shift >> width;      // left == 64: no bits above
-    __syncthreads();
-    for (int i = threadIdx.x; i < SM_BINS; i += NT) lds.sums[i] = 0;
-    if (threadIdx.x == 0) lds.n = 0;
-    __syncthreads();
+  u64 lo = 0, known = 0;                                             // of the order's bits, those found so far
+  for (int left = bits; left > 0;) {
+    const int shift = max(left - 11, 0);
+    const u64 mask = (left == 64 ? ~0ull : (1ull << left) - 1);
     each([&](u64 order, u64 w) {
-      if (w && (first || order >> shift >> width == same)) atomicAdd(&lds.sums[(order & mask) >> shift], w);
+      if (w && ((order ^ lo) & known) == 0) atomicAdd(&lds.sums[(order & mask) >> shift], w);
     });
     __syncthreads();
     u64 before;
     const u64 digit = crossing(lds, want, before);
     want -= before;
-    if (first) {                                                     // the bits that all share
-      each([&](u64 order, u64 w) {
-        if (w && (order & mask) >> shift == digit) {
-          atomicAdd(&lds.n, 1);
-          lds.found = order;
-        }
-      });
-      __syncthreads();
-      lo = (lds.found & ~mask) | digit << shift;
-    } else {
-      lo |= digit << shift;
-      each([&](u64 order, u64 w) {
-        if (w && order >> shift == lo >> shift) {
-          atomicAdd(&lds.n, 1);
-          lds.found = order;
-        }
-      });
-      __syncthreads();
-    }
-    if (lds.n == 1) return lds.found;
+    known |= mask & ~((1ull << shift) - 1);
+    lo |= digit << shift;
+    each([&](u64 order, u64 w) {
+      if (w && ((order ^ lo) & known) == 0) {
+        atomicAdd(&lds.n, 1);
+        lds.found = order;
+      }
+    });
+    __syncthreads();
+    if (lds.n == 1 || shift == 0) break;
     left = shift;
   }
-  return lo;
+  return lds.found;
+}
+// The same for what the threads have in registers; the bits that all of them share are left out
+template <int NT, int N>
+__device__ __forceinline__ u64 select_held(SampleLds<NT>& lds, u64 want, const u64 (&order)[N], const u64 (&w)[N]) {
+  u64 any = 0, all = ~0ull;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (w[j]) { any |= order[j]; all &= order[j]; }
+  any = last_lane(scan_of(any, 0, Or()));
+  all = last_lane(scan_of(all, ~0ull, And()));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) { lds.waves[threadIdx.x >> 6] = any; lds.ups[threadIdx.x >> 6] = all; }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) { any |= lds.waves[i]; all &= lds.ups[i]; }
+  if (any == all) return any;
+  return select(lds, 64 - __builtin_clzll(any ^ all), want, [&](const auto& f) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f(order[j], w[j]);
+  });
 }
 // A fraction f of a sum of s steps, upwards, as a sum that can be reached
 __device__ __forceinline__ u64 part_of(double f, u64 s) {
@@ -198,24 +279,24 @@ __device__ __forceinline__ u64 drawn_at(const SampleArgs& a, int row, u64 total)
 }
 // 1 over the sum of what is left
 __device__ __forceinline__ double share_of(const SampleArgs& a, u64 total) { return 1.0 / ((double)total * __longlong_as_double((long long)(1023 - a.scale_bits) << 52)); }
-__device__ __forceinline__ int index_bits(int V) { return 32 - __builtin_clz(V); }
 
 // The cuts of logits that `each` visits (logit, index) into r.cut, top_k and then top_p
 template <int NT, class Each>
 __device__ __forceinline__ void cut_row(SampleLds<NT>& lds, Row& r, const Each& each) {
+  const int bits = 32 - r.spare + r.bits;
   if (r.top_k) {
     u64 n = 0;
     each([&](float x, int) { n += x > -INFINITY; });
     n = sum_of_block(lds, n);
-    if (n >= (u64)r.top_k)                                           // also of a list that holds no more than these
-      r.cut = select(lds, 64, (u64)r.top_k, [&](const auto& f) { each([&](float x, int i) { f(place(x, i), x > -INFINITY ? 1 : 0); }); });
+    if (n >= (u64)r.top_k) r.cut = select(lds, bits, (u64)r.top_k, [&](const auto& f) { each([&](float x, int i) { f(r.place(x, i), x > -INFINITY ? 1 : 0); }); });
   }
   if (r.top_p < 1.f) {
     const u64 cut = r.cut;
+    const auto weight = [&](float x, int i) { return x > -INFINITY && r.place(x, i) <= cut ? r.steps(r.weight(x)) : 0; };
     u64 n = 0;
-    each([&](float x, int i) { if (place(x, i) <= cut) n += r.weight_of(x); });
+    each([&](float x, int i) { n += weight(x, i); });
     n = sum_of_block(lds, n);
-    r.cut = select(lds, 64, part_of(r.top_p, n), [&](const auto& f) { each([&](float x, int i) { f(place(x, i), place(x, i) <= cut ? r.weight_of(x) : 0); }); });
+    r.cut = select(lds, bits, part_of(r.top_p, n), [&](const auto& f) { each([&](float x, int i) { f(r.place(x, i), weight(x, i)); }); });
   }
 }
 // The draw among those of them that are left, and the sum of these
@@ -224,7 +305,42 @@ __device__ __forceinline__ int draw_row(SampleLds<NT>& lds, const SampleArgs& a,
   total = 0;
   each([&](float x, int i) { total += r.steps(r.kept(x, i)); });
   total = sum_of_block(lds, total);
-  return (int)select(lds, index_bits(a.V), drawn_at(a, row, total), [&](const auto& f) { each([&](float x, int i) { f((u64)i, r.steps(r.kept(x, i))); }); });
+  return (int)select(lds, r.bits, drawn_at(a, row, total), [&](const auto& f) { each([&](float x, int i) { f((u64)i, r.steps(r.kept(x, i))); }); });
+}
+
+// Both for what the threads have in registers: logits, their numbers, and which of them there are by x > -inf.  What is left of each
+// comes back in w
+template <int NT, int N>
+__device__ __forceinline__ int draw_held(SampleLds<NT>& lds, const SampleArgs& a, int row, Row& r, u64& total, const float (&x)[N], const int (&at)[N], double (&w)[N]) {
+  u64 p[N], s[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) p[j] = r.place(x[j], at[j]);
+  if (r.top_k) {
+    u64 n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) n += s[j] = x[j] > -INFINITY;
+    n = sum_of_block(lds, n);
+    if (n >= (u64)r.top_k) r.cut = select_held(lds, (u64)r.top_k, p, s);               // also where there are no more than these
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) w[j] = x[j] > -INFINITY && p[j] <= r.cut ? r.weight(x[j]) : 0.0;
+  if (r.top_p < 1.f) {
+    u64 n = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) n += s[j] = r.steps(w[j]);
+    n = sum_of_block(lds, n);
+    r.cut = select_held(lds, part_of(r.top_p, n), p, s);
+  }
+  total = 0;
+  u64 i[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    w[j] = p[j] <= r.cut ? r.left(w[j]) : 0.0;
+    total += s[j] = r.steps(w[j]);
+    i[j] = (unsigned)at[j];
+  }
+  total = sum_of_block(lds, total);
+  return (int)select_held(lds, drawn_at(a, row, total), i, s);
 }
 
 // ---- rows of a block -----------------------------------------------------------------------------------------------------------
@@ -234,34 +350,32 @@ __global__ __launch_bounds__(NT) void sample_small_kernel(const SampleArgs a) {
   __shared__ SampleLds<NT> lds;
   const int tid = threadIdx.x, row = blockIdx.x, V = a.V;
   const X* logits = (const X*)a.logits + row * a.stride;
+  for (int i = tid; i < SM_BINS; i += NT) lds.sums[i] = 0;
   float x[N], top = -INFINITY;
+  int at[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const int i = j * NT + tid;
-    x[j] = i < V ? taken(logit(logits, i)) : -INFINITY;
+    at[j] = j * NT + tid;
+    x[j] = at[j] < V ? taken(logit(logits, at[j])) : -INFINITY;
   }
-  Row r = row_of(a, row);
+  Row r = row_of<X>(a, row);
 #pragma unroll
   for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
-  r.top = max_of_block(lds, top);
+  const bool some = r.begin(max_of_block(lds, top));
   u64 total = 0;
-  const bool some = r.top > -INFINITY;
+  double w[N] = {};
+  int token = -1;                                                    // nothing to draw from
   if (some) {
-    const auto each = [&](const auto& f) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) f(x[j], j * NT + tid);
-    };
-    cut_row(lds, r, each);
-    const int token = draw_row(lds, a, row, r, total, each);
-    if (tid == 0) a.tokens[row] = token;
-  } else if (tid == 0) {
-    a.tokens[row] = -1;                                              // nothing to draw from
+    for (int j = 0; j < N; ++j) x[j] = r.seen(x[j]);
+    token = draw_held(lds, a, row, r, total, x, at, w);
   }
+  if (tid == 0) a.tokens[row] = token;
   if (a.probs) {
     const double f = some ? share_of(a, total) : 0.0;
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (j * NT + tid < V) a.probs[row * a.p_stride + j * NT + tid] = some ? (float)(r.kept(x[j], j * NT + tid) * f) : 0.f;
+      if (at[j] < V) a.probs[row * a.p_stride + at[j]] = (float)(w[j] * f);
   }
 }
 
@@ -270,7 +384,7 @@ __global__ __launch_bounds__(NT) void sample_small_kernel(const SampleArgs a) {
 struct RowWork {
   u64 weights[SM_BINS];            // by distance from the largest
   unsigned counts[SM_BINS];
-  u64 list[SM_LIST];               // places
+  u64 list[SM_LIST];               // logits and, behind them, their indexes
   unsigned listed, pad;            // more than SM_LIST: not all of them are there
   u64 cut;                         // what the row comes to
   double share;
@@ -288,55 +402,35 @@ struct Work {                      // of a call
   int parts, len, n_runs;          // blocks of a row, logits of one, sums of a row
 };
 
-// Rises as x falls.  Even steps of 1 / 64 of the temperature for 16 of it, then 64 to an octave
-__device__ __forceinline__ int distance(const Row& r, float x) {
-  const float d = x == r.top ? 0.f : (r.top - x) * (r.inv_t > 0.0 ? (float)(r.inv_t * (1.0 / 16)) : 1.f);
-  return d < 1.f ? (int)(d * (SM_BINS / 2)) : min(SM_BINS / 2 + (int)((__float_as_uint(d) - 0x3f800000u) >> 17), SM_BINS - 1);
-}
-
-// Runs of the block's part of a row, a wave's turn each: eight logits a lane
-template <class X>
-struct Eight;
-template <>
-struct Eight<float> {
-  typedef __attribute__((ext_vector_type(4), aligned(4))) float v4;
-  static __device__ __forceinline__ void load(const float* p, float (&x)[8]) {
-    const v4 a = *(const v4*)p, b = *(const v4*)(p + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
-  }
-};
-template <class H>
-struct EightHalves {
-  typedef __attribute__((ext_vector_type(8), aligned(2))) H v8;
-  static __device__ __forceinline__ void load(const H* p, float (&x)[8]) {
-    const v8 a = *(const v8*)p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)a[e];
-  }
-};
-template <>
-struct Eight<__bf16> : EightHalves<__bf16> {};
-template <>
-struct Eight<_Float16> : EightHalves<_Float16> {};
-
-// f(logits, index of the first, run), run by run; what lies behind the row is -inf
+// f(logits, which may be NaN, index of the first, run) for a block's part of a row, run by run, eight logits a lane, the next run's on their way; what
+// lies behind the row is -inf
 template <class X, class F>
-__device__ __forceinline__ void each_run(const SampleArgs& a, const Work& w, int row, int part, const F& f) {
+__device__ __forceinline__ void each_run(const SampleArgs& a, const Work& w, int row, int part, const Row& r, const F& f) {
+  typedef __attribute__((ext_vector_type(8), aligned(sizeof(X)))) X X8;                // rows of odd vocabularies start anywhere
   const X* logits = (const X*)a.logits + row * a.stride;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, end = min((part + 1) * w.len, a.V);
-  for (int i0 = part * w.len + wave * SM_RUN; i0 < end; i0 += SM_T / 64 * SM_RUN) {
-    const int i = i0 + 8 * lane;
+  const auto load = [&](int i) {
+    X8 x;
+    if (i + 8 <= a.V) return *(const X8*)(logits + i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = i + e < a.V ? logits[i + e] : (X)-INFINITY;
+    return x;
+  };
+  const int first = part * w.len + wave * SM_RUN;
+  X8 now = {};
+  if (first < end) now = load(first + 8 * lane);
+  for (int i0 = first; i0 < end;) {
+    const X8 this_one = now;
+    const int i1 = i0 + SM_T / 64 * SM_RUN;
+    if (i1 < end) now = load(i1 + 8 * lane);
     float x[8];
-    if (i + 8 <= a.V) {
-      Eight<X>::load(logits + i, x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = taken(x[e]);
-    } else {
+    for (int e = 0; e < 8; ++e) x[e] = (float)this_one[e];
+    if (r.infinite)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = i + e < a.V ? taken(logit(logits, i + e)) : -INFINITY;
-    }
-    f(x, i, i0 / SM_RUN);
+      for (int e = 0; e < 8; ++e) x[e] = r.seen(x[e]);
+    f(x, i0 + 8 * lane, i0 / SM_RUN);
+    i0 = i1;
   }
 }
 __device__ __forceinline__ float top_of(const Work& w, int row) {
@@ -357,7 +451,9 @@ __global__ __launch_bounds__(SM_T) void sample_top_kernel(const SampleArgs a, co
     }
   if (part == 0 && threadIdx.x == 0) rw.listed = 0;
   float top = -INFINITY;
-  each_run<X>(a, w, row, part, [&](const float (&x)[8], int, int) {
+  Row r;
+  r.infinite = false;
+  each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
   });
@@ -370,11 +466,10 @@ __global__ __launch_bounds__(SM_T) void sample_sums_kernel(const SampleArgs a, c
   __shared__ u64 weights[SM_BINS];
   __shared__ unsigned counts[SM_BINS];
   const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts;
-  Row r = row_of(a, row);
+  Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
   if (kind != CUT_COUNT && kind != CUT_WEIGHT) return;
-  r.top = top_of(w, row);
-  if (r.top == -INFINITY) return;
+  if (!r.begin(top_of(w, row))) return;
   RowWork& rw = w.rows[row];
   for (int i = threadIdx.x; i < SM_BINS; i += SM_T) {
     if (kind == CUT_COUNT) counts[i] = 0;
@@ -382,17 +477,17 @@ __global__ __launch_bounds__(SM_T) void sample_sums_kernel(const SampleArgs a, c
   }
   __syncthreads();
   if (kind == CUT_COUNT)
-    each_run<X>(a, w, row, part, [&](const float (&x)[8], int, int) {
+    each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (x[e] > -INFINITY) atomicAdd(&counts[distance(r, x[e])], 1u);
+        if (x[e] > -INFINITY) atomicAdd(&counts[r.distance(x[e])], 1u);
     });
   else
-    each_run<X>(a, w, row, part, [&](const float (&x)[8], int, int) {
+    each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const u64 s = r.weight_of(x[e]);
-        if (s) atomicAdd(&weights[distance(r, x[e])], s);
+        const u64 s = r.steps(r.weight(x[e]));
+        if (s) atomicAdd(&weights[r.distance(x[e])], s);
       }
     });
   __syncthreads();
@@ -425,33 +520,48 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
   __shared__ u64 list[SM_LIST];
   __shared__ unsigned listed, first;
   const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts, tid = threadIdx.x;
-  Row r = row_of(a, row);
+  Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
   if (kind == CUT_SLOWLY) return;
-  r.top = top_of(w, row);
-  if (r.top == -INFINITY) return;
+  if (!r.begin(top_of(w, row))) return;
   RowWork& rw = w.rows[row];
   int at = SM_BINS;
   u64 want;
   if (tid == 0) listed = 0;
   if (kind != CUT_NONE) at = cut_at(lds, r, kind, rw, want);
   __syncthreads();
-  each_run<X>(a, w, row, part, [&](const float (&x)[8], int i, int run) {
-    u64 sum = 0;
+  const auto add = [&](float x, int i) {
+    const unsigned n = atomicAdd(&listed, 1u);
+    if (n < SM_LIST) list[n] = (u64)__float_as_uint(x) << 32 | (unsigned)i;
+  };
+  const auto end_run = [&](u64 sum, int run) {
+    sum = sum_of_wave(sum);
+    if ((tid & 63) == 0) w.runs[(long)row * w.n_runs + run] = sum;
+  };
+  if (kind == CUT_COUNT)
+    each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int d = kind == CUT_NONE ? 0 : distance(r, x[e]);
-      if (kind == CUT_COUNT ? d <= at && x[e] > -INFINITY : kind == CUT_WEIGHT && d == at && x[e] > -INFINITY) {
-        const unsigned n = atomicAdd(&listed, 1u);
-        if (n < SM_LIST) list[n] = place(x[e], i + e);
+      for (int e = 0; e < 8; ++e)
+        if (r.distance(x[e]) <= at && x[e] > -INFINITY) add(x[e], i + e);
+    });
+  else if (kind == CUT_WEIGHT)
+    each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int run) {
+      u64 sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int d = r.distance(x[e]);
+        if (d < at) sum += r.steps(r.left(r.weight(x[e])));
+        if (d == at && x[e] > -INFINITY) add(x[e], i + e);
       }
-      if (kind != CUT_COUNT && d < at) sum += r.steps(r.kept(x[e], i + e));
-    }
-    if (kind != CUT_COUNT) {
-      sum = sum_of_wave(sum);
-      if ((tid & 63) == 0) w.runs[(long)row * w.n_runs + run] = sum;
-    }
-  });
+      end_run(sum, run);
+    });
+  else
+    each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int run) {
+      u64 sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += r.steps(r.left(r.weight(x[e])));
+      end_run(sum, run);
+    });
   __syncthreads();
   if (tid == 0 && listed) first = atomicAdd(&rw.listed, listed);
   __syncthreads();
@@ -466,10 +576,11 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   const int tid = threadIdx.x, row = blockIdx.x;
   const X* logits = (const X*)a.logits + row * a.stride;
   RowWork& rw = w.rows[row];
-  Row r = row_of(a, row);
+  Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
-  r.top = top_of(w, row);
-  if (r.top == -INFINITY) {                                          // nothing to draw from
+  for (int i = tid; i < SM_BINS; i += SM_FINAL) lds.sums[i] = 0;
+  __syncthreads();
+  if (!r.begin(top_of(w, row))) {                                    // nothing to draw from
     if (tid == 0) {
       a.tokens[row] = -1;
       rw.cut = 0;
@@ -482,7 +593,7 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   const unsigned m = kind == CUT_COUNT || kind == CUT_WEIGHT ? rw.listed : 0;
   if (kind == CUT_SLOWLY || m > SM_LIST) {
     const auto each = [&](const auto& f) {
-      for (int i = tid; i < a.V; i += SM_FINAL) f(taken(logit(logits, i)), i);
+      for (int i = tid; i < a.V; i += SM_FINAL) f(r.seen(logit(logits, i)), i);
     };
     cut_row(lds, r, each);
     token = draw_row(lds, a, row, r, total, each);
@@ -493,30 +604,32 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
     for (int j = 0; j < N; ++j) {
       const bool is = j * SM_FINAL + tid < m;
       const u64 p = is ? rw.list[j * SM_FINAL + tid] : 0;
-      x[j] = is ? of_falling((unsigned)(p >> 32)) : -INFINITY;
+      x[j] = is ? __uint_as_float((unsigned)(p >> 32)) : -INFINITY;
       at[j] = (int)p;
     }
-    const auto each = [&](const auto& f) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) f(x[j], at[j]);
-    };
     if (kind == CUT_COUNT) {
-      cut_row(lds, r, each);
-      token = draw_row(lds, a, row, r, total, each);
+      double left[N];
+      token = draw_held(lds, a, row, r, total, x, at, left);
     } else {
       if (kind == CUT_WEIGHT) {
-        u64 want;
+        u64 want, p[N], s[N];
         cut_at(lds, r, kind, rw, want);
-        r.cut = select(lds, 64, want, [&](const auto& f) { each([&](float y, int i) { f(place(y, i), r.weight_of(y)); }); });
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          p[j] = r.place(x[j], at[j]);
+          s[j] = x[j] > -INFINITY ? r.steps(r.weight(x[j])) : 0;
+        }
+        r.cut = select_held(lds, want, p, s);
       }
       // the runs' sums with what is kept of the list; then the run that the draw falls into
       __syncthreads();
       for (int i = tid; i < SM_BINS; i += SM_FINAL) lds.sums[i] = i < w.n_runs ? w.runs[(long)row * w.n_runs + i] : 0;
       __syncthreads();
-      each([&](float y, int i) {
-        const u64 s = r.steps(r.kept(y, i));
-        if (s) atomicAdd(&lds.sums[i / SM_RUN], s);
-      });
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const u64 s = r.steps(r.kept(x[j], at[j]));
+        if (s) atomicAdd(&lds.sums[at[j] / SM_RUN], s);
+      }
       __syncthreads();
       total = 0;
       for (int i = tid; i < SM_BINS; i += SM_FINAL) total += lds.sums[i];
@@ -524,7 +637,7 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
       const u64 want = drawn_at(a, row, total);
       u64 before;
       const int run = crossing(lds, want, before), i = run * SM_RUN + tid;
-      const u64 s = tid < SM_RUN && i < a.V ? r.steps(r.kept(taken(logit(logits, i)), i)) : 0;
+      const u64 s = tid < SM_RUN && i < a.V ? r.steps(r.kept(r.seen(logit(logits, i)), i)) : 0;
       token = run * SM_RUN + (int)select(lds, 9, want - before, [&](const auto& f) { f((u64)tid, s); });
     }
   }
@@ -538,17 +651,17 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
 template <class X>
 __global__ __launch_bounds__(SM_T) void sample_probs_kernel(const SampleArgs a, const Work w) {
   const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts;
-  Row r = row_of(a, row);
-  r.top = top_of(w, row);
+  Row r = row_of<X>(a, row);
+  r.begin(top_of(w, row));
   r.cut = w.rows[row].cut;
   const double f = w.rows[row].share;
   float* out = a.probs + row * a.p_stride;
-  each_run<X>(a, w, row, part, [&](const float (&x)[8], int i, int) {
+  each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int) {
     float p[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = f > 0.0 ? (float)(r.kept(x[e], i + e) * f) : 0.f;
     if (i + 8 <= a.V) {
-      typedef Eight<float>::v4 v4;
+      typedef __attribute__((ext_vector_type(4), aligned(4))) float v4;
       *(v4*)(out + i) = v4{p[0], p[1], p[2], p[3]};
       *(v4*)(out + i + 4) = v4{p[4], p[5], p[6], p[7]};
     } else {
