@@ -19,11 +19,12 @@ namespace sna {
 typedef unsigned long long u64;
 constexpr int SM_BINS = 2048;      // values of a digit; distances told apart; runs of a row, at most
 constexpr int SM_SMALL = 4096;     // logits of a row that one block takes in one launch
-constexpr int SM_LIST = 4096;      // logits at a row's cut
+constexpr int SM_LIST = 2048;      // logits at a row's cut
 constexpr int SM_MOST = SM_LIST / 2;             // top_k up to which a row's list is to hold all that it keeps
 constexpr int SM_RUN = 512;        // logits of a wave's turn, and of a sum
+constexpr int SM_STAGE = 1024;     // logits at the cut that a block writes out at once
 constexpr int SM_T = 512;          // threads of the blocks that share a row
-constexpr int SM_FINAL = 1024;     // of the one that ends it
+constexpr int SM_FINAL = 512;     // of the one that ends it
 
 __device__ __forceinline__ float logit(const float* p, long i) { return p[i]; }
 __device__ __forceinline__ float logit(const __bf16* p, long i) { return (float)p[i]; }
@@ -500,11 +501,12 @@ __global__ __launch_bounds__(SM_T) void sample_sums_kernel(const SampleArgs a, c
   }
 }
 
-// The distance that the row's cut lies at, and what is wanted of it there; SM_BINS: it is not cut
-template <int NT>
-__device__ __forceinline__ int cut_at(SampleLds<NT>& lds, const Row& r, Kind kind, const RowWork& rw, u64& want) {
+// The distance that the row's cut lies at, and what is wanted of it there; SM_BINS: it is not cut.  of(j): sum j of the thread's
+template <int NT, class Of>
+__device__ __forceinline__ int cut_at(SampleLds<NT>& lds, const Row& r, Kind kind, u64& want, const Of& of) {
   u64 all = 0;
-  for (int i = threadIdx.x; i < SM_BINS; i += NT) all += lds.sums[i] = kind == CUT_COUNT ? rw.counts[i] : rw.weights[i];
+#pragma unroll
+  for (int i = 0; i < SM_BINS / NT; ++i) all += lds.sums[i * NT + threadIdx.x] = of(i);
   all = sum_of_block(lds, all);                                      // and the sums are there
   want = kind == CUT_COUNT ? (u64)r.top_k : part_of(r.top_p, all);
   if (kind == CUT_COUNT && all <= want) return SM_BINS;
@@ -517,9 +519,9 @@ __device__ __forceinline__ int cut_at(SampleLds<NT>& lds, const Row& r, Kind kin
 template <class X>
 __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, const Work w) {
   __shared__ SampleLds<SM_T> lds;
-  __shared__ u64 list[SM_LIST];
+  __shared__ u64 list[SM_STAGE];
   __shared__ unsigned listed, first;
-  const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts, tid = threadIdx.x;
+  const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts, tid = threadIdx.x, lane = tid & 63;
   Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
   if (kind == CUT_SLOWLY) return;
@@ -528,45 +530,58 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
   int at = SM_BINS;
   u64 want;
   if (tid == 0) listed = 0;
-  if (kind != CUT_NONE) at = cut_at(lds, r, kind, rw, want);
+  if (kind != CUT_NONE) at = cut_at(lds, r, kind, want, [&](int j) { return kind == CUT_COUNT ? (u64)rw.counts[j * SM_T + tid] : rw.weights[j * SM_T + tid]; });
   __syncthreads();
   const auto add = [&](float x, int i) {
+    const u64 v = (u64)__float_as_uint(x) << 32 | (unsigned)i;
     const unsigned n = atomicAdd(&listed, 1u);
-    if (n < SM_LIST) list[n] = (u64)__float_as_uint(x) << 32 | (unsigned)i;
+    if (n < SM_STAGE) list[n] = v;
+    else {                                                           // more than are written out together
+      const unsigned m = atomicAdd(&rw.listed, 1u);
+      if (m < SM_LIST) rw.list[m] = v;
+    }
   };
   const auto end_run = [&](u64 sum, int run) {
     sum = sum_of_wave(sum);
-    if ((tid & 63) == 0) w.runs[(long)row * w.n_runs + run] = sum;
+    if (lane == 0) w.runs[(long)row * w.n_runs + run] = sum;
   };
-  if (kind == CUT_COUNT)
+  if (kind == CUT_COUNT) {
     each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (r.distance(x[e]) <= at && x[e] > -INFINITY) add(x[e], i + e);
     });
-  else if (kind == CUT_WEIGHT)
+  } else if (kind == CUT_WEIGHT) {
+    // The ones above the cut move together first: of 512 logits they are fewer than half as a rule, and the weights are what takes time
+    float* above = (float*)lds.sums + (tid >> 6) * SM_RUN;
+    static_assert(sizeof(lds.sums) >= SM_T / 64 * SM_RUN * sizeof(float), "a wave's run");
     each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int run) {
-      u64 sum = 0;
+      int n = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int d = r.distance(x[e]);
-        if (d < at) sum += r.steps(r.left(r.weight(x[e])));
+        const u64 yes = __ballot(d < at);
+        if (d < at) above[n + __builtin_amdgcn_mbcnt_hi((unsigned)(yes >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)yes, 0))] = x[e];
+        n += __popcll(yes);
         if (d == at && x[e] > -INFINITY) add(x[e], i + e);
       }
+      u64 sum = 0;
+      for (int j = lane; j < n; j += 64) sum += r.steps(r.left(r.weight(above[j])));       // a wave's own: in order without a barrier
       end_run(sum, run);
     });
-  else
+  } else {
     each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int run) {
       u64 sum = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += r.steps(r.left(r.weight(x[e])));
       end_run(sum, run);
     });
+  }
   __syncthreads();
-  if (tid == 0 && listed) first = atomicAdd(&rw.listed, listed);
+  const unsigned n = min(listed, (unsigned)SM_STAGE);
+  if (tid == 0 && n) first = atomicAdd(&rw.listed, n);
   __syncthreads();
-  if (listed && first < SM_LIST)
-    for (unsigned n = tid; n < listed && first + n < SM_LIST; n += SM_T) rw.list[first + n] = list[n];
+  for (unsigned j = tid; j < n && first + j < SM_LIST; j += SM_T) rw.list[first + j] = list[j];
 }
 
 template <class X>
@@ -578,7 +593,18 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   RowWork& rw = w.rows[row];
   Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
-  for (int i = tid; i < SM_BINS; i += SM_FINAL) lds.sums[i] = 0;
+  // everything that the launches before have left, in one round trip
+  u64 held[N], sums[SM_BINS / SM_FINAL], runs[SM_BINS / SM_FINAL];
+#pragma unroll
+  for (int j = 0; j < N; ++j) held[j] = rw.list[j * SM_FINAL + tid];
+#pragma unroll
+  for (int j = 0; j < SM_BINS / SM_FINAL; ++j) {
+    const int i = j * SM_FINAL + tid;
+    sums[j] = rw.weights[i];
+    runs[j] = i < w.n_runs ? w.runs[(long)row * w.n_runs + i] : 0;
+    lds.sums[i] = 0;
+  }
+  const unsigned listed = rw.listed;
   __syncthreads();
   if (!r.begin(top_of(w, row))) {                                    // nothing to draw from
     if (tid == 0) {
@@ -590,7 +616,7 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   }
   u64 total;
   int token;
-  const unsigned m = kind == CUT_COUNT || kind == CUT_WEIGHT ? rw.listed : 0;
+  const unsigned m = kind == CUT_COUNT || kind == CUT_WEIGHT ? listed : 0;
   if (kind == CUT_SLOWLY || m > SM_LIST) {
     const auto each = [&](const auto& f) {
       for (int i = tid; i < a.V; i += SM_FINAL) f(r.seen(logit(logits, i)), i);
@@ -603,9 +629,8 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const bool is = j * SM_FINAL + tid < m;
-      const u64 p = is ? rw.list[j * SM_FINAL + tid] : 0;
-      x[j] = is ? __uint_as_float((unsigned)(p >> 32)) : -INFINITY;
-      at[j] = (int)p;
+      x[j] = is ? __uint_as_float((unsigned)(held[j] >> 32)) : -INFINITY;
+      at[j] = is ? (int)held[j] : 0;
     }
     if (kind == CUT_COUNT) {
       double left[N];
@@ -613,7 +638,7 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
     } else {
       if (kind == CUT_WEIGHT) {
         u64 want, p[N], s[N];
-        cut_at(lds, r, kind, rw, want);
+        cut_at(lds, r, kind, want, [&](int j) { return sums[j]; });
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           p[j] = r.place(x[j], at[j]);
@@ -623,7 +648,8 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
       }
       // the runs' sums with what is kept of the list; then the run that the draw falls into
       __syncthreads();
-      for (int i = tid; i < SM_BINS; i += SM_FINAL) lds.sums[i] = i < w.n_runs ? w.runs[(long)row * w.n_runs + i] : 0;
+#pragma unroll
+      for (int j = 0; j < SM_BINS / SM_FINAL; ++j) lds.sums[j * SM_FINAL + tid] = runs[j];
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < N; ++j) {
@@ -636,9 +662,18 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
       total = sum_of_block(lds, total);
       const u64 want = drawn_at(a, row, total);
       u64 before;
-      const int run = crossing(lds, want, before), i = run * SM_RUN + tid;
-      const u64 s = tid < SM_RUN && i < a.V ? r.steps(r.kept(r.seen(logit(logits, i)), i)) : 0;
-      token = run * SM_RUN + (int)select(lds, 9, want - before, [&](const auto& f) { f((u64)tid, s); });
+      const int run = crossing(lds, want, before);
+      constexpr int M = SM_RUN / SM_FINAL;
+      u64 s[M], o[M];
+#pragma unroll
+      for (int j = 0; j < M; ++j) {
+        const int i = run * SM_RUN + j * SM_FINAL + tid;
+        s[j] = i < a.V ? r.steps(r.kept(r.seen(logit(logits, i)), i)) : 0;
+        o[j] = j * SM_FINAL + tid;
+      }
+      token = run * SM_RUN + (int)select(lds, 9, want - before, [&](const auto& f) {
+        for (int j = 0; j < M; ++j) f(o[j], s[j]);
+      });
     }
   }
   if (tid == 0) {
