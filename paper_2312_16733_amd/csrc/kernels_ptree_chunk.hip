@@ -1,8 +1,59 @@
-// Attention of the tokens of drafted trees over the paged cache, many rows of queries per key / value head: kernels in pprefill_kernel.h.
+// Attention of the tokens of drafted trees over the paged cache, many rows of queries per key / value head: pprefill_kernel.h's walk,
+// 128 rows a block.
 #include "pprefill_kernel.h"
 
 namespace sna {
 
-hipError_t launch_tree_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) { return launch_chunks<true>(a, dtype, head_dim, s); }
+// The keys of all sequences and heads, laid end to end, in equal shares, as where rows are few: trees of a step differ in length and
+// size, and shares of each would not fill the last round of blocks (16 trees of up to 32 tokens over up to 4096 keys, 32 heads over
+// 8 of 128: 66 us in five shares each, 58 in equal ones).  A tree of more than 128 rows has a block for each 128 of them on every
+// share: they walk the same keys side by side on one XCD, whose L2 reads them once.  Block j of a share is one of plane j, which has parts of
+// its own, plane after plane.
+template <class T, int D, int W>
+__global__ __launch_bounds__(64 * W, 2) void tree_split_kernel(const PagedAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) PrefillLds<D> lds;
+  const int planes = gridDim.x / a.blocks, group = blockIdx.x / (8 * planes), in = blockIdx.x % (8 * planes), plane = in >> 3, p = group * 8 + (in & 7);
+  First* first = (First*)a.parts;
+  const long part_size = part_floats(a.rows_cap, D);
+  float* parts = (float*)(first + a.blocks * planes) + 2 * a.blocks * plane * part_size;
+  const auto tiles = [&](const Seq& sq, int b) { return rows_of_sequence<PF_K, true>(a, sq, b, 0, a.max_new).tiles; };
+  walk_share(a, p, first + a.blocks * plane, a.max_new, [&](int b) { return tiles(sequence(a.s, b), b); },
+             [&](const Seq& sq, int b, int) {
+               RowTile r = rows_of_sequence<PF_K, true>(a, sq, b, plane * a.tpt, a.tpt);
+               r.tiles = tiles(sq, b);                               // also where the tree has no rows here
+               r.n = max(r.n, 0);
+               return r;
+             },
+             [&](const RowTile& r, int h, int t0, int t1, int part) { chunk_rows<T, D, W, true>(a, lds, r, h, t0, t1, 0, part < 0 ? nullptr : parts + part * part_size); });
+}
+
+template <class T, int D>
+static hipError_t tree_grid(PagedAttnArgs a, hipStream_t s) {
+  constexpr int W = 4;
+  a.tpt = 32 * W / a.G;
+  if (a.parts) {
+    if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
+    a.rows_cap = a.tpt * a.G;
+    a.least = kTreeLeast;
+    const int planes = tree_planes(a.max_new, a.G);
+    hipLaunchKernelGGL((tree_split_kernel<T, D, W>), dim3(a.blocks * planes), dim3(64 * W), 0, s, a);
+    // rows of a (sequence, head) that a block of the join takes at once, as many as its parts allow
+    const int per = std::max(1, (int)(a.blocks / std::max(1l, (long)a.s.B * a.kv.heads))), at_once = std::max(1, 1024 / D / std::max(1, (per + 7) / 8));
+    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.blocks * planes, (a.rows_cap + at_once - 1) / at_once), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  a.waves = W;
+  a.splits = 1;
+  a.by_tpt = FastDiv::by(a.tpt);
+  const long blocks = chunk_blocks(a);
+  if (!fits_a_launch(blocks, 64 * W)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((paged_chunk_kernel<T, D, W, true>), dim3((unsigned)blocks), dim3(64 * W), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == SNA_DTYPE_FP16) return head_dim == 64 ? tree_grid<Fp16, 64>(a, s) : tree_grid<Fp16, 128>(a, s);
+  return head_dim == 64 ? tree_grid<Bf16, 64>(a, s) : tree_grid<Bf16, 128>(a, s);
+}
 
 }  // namespace sna

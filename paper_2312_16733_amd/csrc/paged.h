@@ -269,6 +269,7 @@ size_t paged_attention_workspace(int n_seqs, int n_tokens, int kv_heads, int gro
 bool chunks_fit_a_launch(const PagedAttnArgs& a);
 hipError_t launch_paged_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_paged_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
+size_t tree_attention_workspace(const PagedSeqs& s, int kv_heads, int group, int max_new, int max_len, int window, int words, int head_dim);
 hipError_t launch_tree_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_tree_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, void* workspace, hipStream_t s);
 

@@ -75,6 +75,7 @@ struct AttnPlan {
   ChunkPlan chunk;
   size_t parts, chunk_parts;       // bytes of the workspace, for either
 };
+inline size_t parts_of(int blocks, int rows, int head_dim) { return (blocks * (sizeof(First) + 2 * part_floats(rows, head_dim) * sizeof(float)) + 255) & ~(size_t)255; }
 inline AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
   const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
   const bool equal = (long)n_seqs * max_new == n_tokens;               // all sequences bring max_new tokens
@@ -102,7 +103,34 @@ inline AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
       p.most = 16 / group;
     }
   }
-  if (p.blocks) p.parts = (p.blocks * (sizeof(First) + 2 * part_floats((long)std::min(16 * p.mb / group, max_new) * group, head_dim) * sizeof(float)) + 255) & ~(size_t)255;
+  if (p.blocks) p.parts = parts_of(p.blocks, std::min(16 * p.mb / group, max_new) * group, head_dim);
+  return p;
+}
+
+// ---- trees of drafted tokens ----
+// Up to kTreeFew rows a key / value head the few-rows kernel takes them in one tile of rows, and up to twice that in two where the keys
+// are few: the many-rows kernel has 20 us before and behind its turns, if its keys are shared out.  In us, 32 heads over 8 of 128: 16
+// tokens over 8192 keys 22 (few rows) and 37; 16 trees of up to 12 over up to 4096 57 and 46, 64 of up to 13 over up to 2048 99 and 97.
+// More rows are walked by blocks of kTreeRows, whole, or their keys shared out over kTreeBlocks (two on a CU; 256 took 64 us for 58, 180
+// for 127), whichever a count of the turns says is sooner, a turn being 2 us, 1.24 with heads of 64, and three quarters where most CUs have
+// one block.
+constexpr int kTreeFew = 32, kTreeRows = 128, kTreeBlocks = 512, kTreeLeast = 6, kTreeTurns = 2048;
+inline int tree_planes(int max_new, int group) { return (max_new + kTreeRows / group - 1) / (kTreeRows / group); }
+inline AttnPlan plan_of_tree(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
+  const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len, tiles = (keys + PF_K - 1) / PF_K;
+  const long turns = (long)n_seqs * kv_heads * tiles * (n_seqs == 1 ? 10 : 7) / 10;    // sequences of 0.7 of the longest on average
+  if (rows <= kTreeFew || (rows <= 2 * kTreeFew && group <= kTreeFew && turns < kTreeTurns)) return plan_of(n_seqs, n_tokens, kv_heads, group, max_new, max_len, window, head_dim);
+  AttnPlan p = {};
+  p.most = max_new;
+  const int planes = tree_planes(max_new, group), shares = kTreeBlocks / planes & ~7;
+  const long units = (n_tokens / (kTreeRows / group) + n_seqs) * (long)kv_heads;
+  const double turn = head_dim == 128 ? 2.0 : 1.24;
+  const double whole = (double)((units + kTreeBlocks - 1) / kTreeBlocks * tiles) * turn * (units <= 256 ? 0.75 : 1.0);
+  const double shared = shares ? std::max((double)turns / shares, (double)kTreeLeast) * turn + 20.0 : 1e30;
+  if (planes <= 16 && shared < whole && (long)n_seqs * kv_heads * (tiles + 2) < 1l << 30) {
+    p.blocks = shares;
+    p.parts = parts_of(shares * planes, std::min(kTreeRows / group, max_new) * group, head_dim);
+  }
   return p;
 }
 

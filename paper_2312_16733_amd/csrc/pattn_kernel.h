@@ -440,21 +440,18 @@ __device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) 
 // The keys of all tiles of rows and heads, laid end to end, in equal shares over the blocks: what a share cuts off of a
 // (tile of rows, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what
 // a later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
-template <class T, int D, int MB, bool ONE, bool TREE>
-__global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
-  __shared__ JoinLds<D, MB, kSplitW> lds;
-  constexpr int KT = tile_keys(D, MB);
-  const int p = blockIdx.x, lane = threadIdx.x & 63, heads = a.kv.heads;
-  First* first = (First*)a.parts;
-  float* parts = (float*)(first + a.blocks);
-  const long part_size = part_floats(a.rows_cap, D);
+// tiles(sequence): of all its tiles of rows, of `tpt` tokens each; rows(sequence, number, first token): one of these;
+// attend(rows, head, first tile of their keys, end, part or -1: all of them are this block's)
+template <class Tiles, class Rows, class F>
+__device__ __forceinline__ void walk_share(const PagedAttnArgs& a, int p, First* first, int tpt, const Tiles& tiles, const Rows& rows, const F& attend) {
+  const int lane = threadIdx.x & 63, heads = a.kv.heads;
   // this share's first sequence: every wave sums the tiles of all, 64 runs of sequences at a time
   // (the host has seen to it that all of them fit 31 bits)
   int lo = 0, count = a.s.B, before = 0, share = 0, x = 0;
   for (bool top = true;; top = false) {
     const int per = (count + 63) >> 6, b0 = lo + lane * per, b1 = min(lo + count, b0 + per);
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles_of_sequence<KT, TREE>(a, b);
+    for (int b = b0; b < b1; ++b) mine += tiles(b);
     int up = mine;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
@@ -463,7 +460,7 @@ __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_ke
     }
     if (top) {
       const int all = uniform(__shfl(up, 63, 64)) * heads;
-      share = max((all + a.blocks - 1) / a.blocks, a.least);          // blocks: a power of two
+      share = max((all + a.blocks - 1) / a.blocks, a.least);
       x = p * share;
       if (x >= all) {
         if (threadIdx.x == 0) first[p].n = 0;
@@ -479,12 +476,12 @@ __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_ke
   // its first tile of rows, head and tile of keys
   int b = uniform(lo), i0 = 0;
   Seq sq = uniform(sequence(a.s, b));
-  RowTile r = rows_of_sequence<KT, TREE>(a, sq, b, 0, a.tpt);
+  RowTile r = rows(sq, b, 0);
   int rel = x - before * heads;
-  while (rel >= r.tiles * heads && i0 + a.tpt < sq.n) {
+  while (rel >= r.tiles * heads && i0 + tpt < sq.n) {
     rel -= r.tiles * heads;
-    i0 += a.tpt;
-    r = rows_of_sequence<KT, TREE>(a, sq, b, i0, a.tpt);
+    i0 += tpt;
+    r = rows(sq, b, i0);
   }
   int h = clamped(rel / max(r.tiles, 1), 0, heads - 1), t = clamped(rel - h * r.tiles, 0, max(r.tiles - 1, 0)), left = share, at = 0;     // at: tiles done, of this share
   bool begun = false;
@@ -495,14 +492,14 @@ __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_ke
       begun = true;
       if (threadIdx.x == 0) first[p] = First{r.row0, r.n, h, min((x + at + r.tiles - 1) / share, a.blocks - 1)};
     }
-    if (r.n > 0) attend_rows<T, D, MB, kSplitW, ONE, TREE>(a, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size, a.rows_cap, lds);
+    if (r.n > 0) attend(r, h, r.t0 + t, r.t0 + t + n, whole ? -1 : 2 * p + (t == 0));
     left -= n;
     at += n;
     t = 0;
     if (left == 0) break;
     if (++h == heads) {
       h = 0;
-      i0 += a.tpt;
+      i0 += tpt;
       if (i0 >= sq.n) {
         i0 = 0;
         do {
@@ -511,11 +508,24 @@ __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_ke
         } while (sq.n <= 0 || sq.n > a.most);
         if (b >= a.s.B) break;
       }
-      r = rows_of_sequence<KT, TREE>(a, sq, b, i0, a.tpt);
+      r = rows(sq, b, i0);
     }
     __syncthreads();                                                 // the next part's joining
   }
   if (!begun && threadIdx.x == 0) first[p].n = 0;
+}
+template <class T, int D, int MB, bool ONE, bool TREE>
+__global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
+  __shared__ JoinLds<D, MB, kSplitW> lds;
+  First* first = (First*)a.parts;
+  float* parts = (float*)(first + a.blocks);
+  const long part_size = part_floats(a.rows_cap, D);
+  constexpr int KT = tile_keys(D, MB);
+  walk_share(a, blockIdx.x, first, a.tpt, [&](int b) { return tiles_of_sequence<KT, TREE>(a, b); },
+             [&](const Seq& sq, int b, int i0) { return rows_of_sequence<KT, TREE>(a, sq, b, i0, a.tpt); },
+             [&](const RowTile& r, int h, int t0, int t1, int part) {
+               attend_rows<T, D, MB, kSplitW, ONE, TREE>(a, r, h, t0, t1, part < 0 ? nullptr : parts + part * part_size, a.rows_cap, lds);
+             });
 }
 
 // Parts joined: JN_Y blocks for each (tile of rows, head) that was cut.  A thread has four dims of a row; the 256 / (D / 4)
@@ -527,15 +537,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) 
   constexpr int W = D / 4, N = 256 / W, U = 8;                       // threads of a row; groups; parts under way
   __shared__ __attribute__((aligned(16))) float so[N][D];
   __shared__ float2 ss[N];
-  const int p = blockIdx.x, g = threadIdx.x / W, d = threadIdx.x % W * 4;
+  const int p = blockIdx.x, planes = gridDim.x / a.blocks, g = threadIdx.x / W, d = threadIdx.x % W * 4;       // planes: see tree_split_kernel
   const First f = ((const First*)a.parts)[p];
   if (f.n == 0) return;
-  const int n = f.last - p + 1, rows = f.n * a.G;
+  const int n = f.last - p % a.blocks + 1, rows = f.n * a.G;
   int share = 1;                                                     // groups that share a row
   while (share < N && n > U * share) share *= 2;
   const int at_once = N / share;
   const long part_size = part_floats(a.rows_cap, D);
-  const float* parts = (const float*)((const First*)a.parts + a.blocks) + (2 * p + 1) * part_size;       // part 0; part j > 0 lies 2 j - 1 further on
+  const float* parts = (const float*)((const First*)a.parts + a.blocks * planes) + (2 * p + 1) * part_size;       // part 0; part j > 0 lies 2 j - 1 further on
   for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {       // the same turns for the block
     const int row = row0 + g / share, row_in = min(row, rows - 1);
     float top = -INFINITY, sum = 0.f;
@@ -612,29 +622,15 @@ static hipError_t rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
   if constexpr (!TREE)             // one token's keys are the same for all of its rows, but for a tree's, whose masks leave out some between
     if (mb == 1 && a.max_new == 1) return rows_grid<T, D, 1, true, false>(a, s);
   if (mb == 1) return rows_grid<T, D, 1, false, TREE>(a, s);
-  return mb == 2 ? rows_grid<T, D, 2, false, TREE>(a, s) : rows_grid<T, D, 4, false, TREE>(a, s);
+  if constexpr (!TREE)             // of trees more than 32 rows go to the many-rows kernel
+    if (mb == 4) return rows_grid<T, D, 4, false, false>(a, s);
+  return rows_grid<T, D, 2, false, TREE>(a, s);
 }
 
-// `window`: as it is planned for
 template <bool TREE>
-static hipError_t launch_attention(PagedAttnArgs a, int dtype, int head_dim, int max_len, int window, void* workspace, hipStream_t s) {
-  const AttnPlan p = plan_of(a.s.B, a.s.T, a.kv.heads, a.G, a.max_new, max_len, window, head_dim);
-  a.most = p.most;
-  a.waves = p.chunk.waves;
-  a.splits = p.chunk.splits;
-  if (p.chunks && !chunks_fit_a_launch(a)) return hipErrorInvalidConfiguration;        // before anything is launched
-  if (p.mb) {
-    PagedAttnArgs r = a;
-    r.parts = p.blocks ? workspace : nullptr;
-    r.blocks = p.blocks;
-    r.waves = p.waves;
-    hipError_t e;
-    if (dtype == SNA_DTYPE_FP16) e = head_dim == 64 ? rows_of<Fp16, 64, TREE>(r, p.mb, s) : rows_of<Fp16, 128, TREE>(r, p.mb, s);
-    else e = head_dim == 64 ? rows_of<Bf16, 64, TREE>(r, p.mb, s) : rows_of<Bf16, 128, TREE>(r, p.mb, s);
-    if (e != hipSuccess || !p.chunks) return e;
-  }
-  a.parts = (char*)workspace + p.parts;
-  return TREE ? launch_tree_chunks(a, dtype, head_dim, s) : launch_paged_chunks(a, dtype, head_dim, s);
+static hipError_t launch_rows(const PagedAttnArgs& a, int mb, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == SNA_DTYPE_FP16) return head_dim == 64 ? rows_of<Fp16, 64, TREE>(a, mb, s) : rows_of<Fp16, 128, TREE>(a, mb, s);
+  return head_dim == 64 ? rows_of<Bf16, 64, TREE>(a, mb, s) : rows_of<Bf16, 128, TREE>(a, mb, s);
 }
 
 }  // namespace sna

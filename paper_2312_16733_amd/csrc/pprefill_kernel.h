@@ -8,7 +8,7 @@
 // reads and vector instructions cost 2 %, four waves a block instead of eight 4 %.  As where rows are few, the scores are formed transposed: a lane has one row, and the keys of a product's 32
 // rows are chosen so (row 16 s + 8 a + 4 h + c is key 16 s + 8 h + 4 a + c) that its scores are what the second product wants.
 #pragma once
-#include "paged.h"
+#include "pattn_kernel.h"
 
 namespace sna {
 
@@ -34,31 +34,16 @@ __device__ __forceinline__ void fetch16(const char* from, lds_char* to) {
 #endif
 }
 
+// Tiles t0 .. t1 - 1 of the keys of the rows of `r` and head h.  Sums leave as results, as share `share` of a.splits, or, of a tree's
+// rows, as a part [rows_cap][D] sums and [rows_cap][2] reference and sum (part != nullptr)
 template <class T, int D, int W, bool TREE>
-__global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnArgs a) {
+__device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, PrefillLds<D>& lds, const RowTile& r, int h, int t0, int t1, int share, float* part) {
   constexpr int S = D / 16, J = D / 32, KI = PF_K * D * 2 / 1024 / W, VI = KI;   // fetches of a wave and tile, 1 KB each
-  __shared__ __attribute__((aligned(1024))) PrefillLds<D> lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hi = lane >> 5;
-  // heads change fastest: where there are 8 of them, each XCD reads one and keeps it in its L2; the last tiles of rows, which
-  // see the most keys, first
-  const int h = blockIdx.x % a.kv.heads, rest = blockIdx.x / a.kv.heads, part = rest % a.splits, tile = gridDim.x / (a.kv.heads * a.splits) - 1 - rest / a.splits;
-  const auto tile0 = [&](int i) { return a.by_tpt.div(clamped(a.s.starts[i], 0, a.s.T)) + i; };
-  const int b = last_at_most(a.s.B, tile, tile0);
-  const Seq sq = sequence(a.s, b);
-  const int i0 = (tile - tile0(b)) * a.tpt, n = i0 < 0 ? 0 : min(sq.n - i0, a.tpt);
-  if (n <= 0 || sq.n <= a.most) return;                              // few rows: not taken here
-  const int row0 = sq.row0 + i0, pos0 = sq.len - sq.n + i0, rows = n * a.G;
+  const int row0 = r.row0, pos0 = r.pos0, rows = r.n * a.G, first = r.keys.lo, last = r.keys.hi - 1;
   TreeMask tree;
-  if constexpr (TREE) tree = tree_of(a, sq, b);
-  const int last = TREE ? tree.last : min(pos0 + n - 1, (a.s.width << a.kv.lps) - 1);
-  const int first = TREE ? first_in_window(a.window, tree.base) : max(a.window <= pos0 ? pos0 - a.window + 1 : 0, 0);
-  int t0 = first / PF_K, t1 = last < 0 ? t0 : last / PF_K + 1;
-  if (a.splits > 1) {                                                // this block's share of the keys
-    const int per = (t1 - t0 + a.splits - 1) / a.splits;
-    t0 = min(t0 + part * per, t1);
-    t1 = min(t0 + per, t1);
-  }
-  const int* table = a.s.table + (long)b * a.s.tstride;
+  if constexpr (TREE) tree = tree_of(a, uniform(sequence(a.s, r.b)), r.b);
+  const int* table = a.s.table + (long)r.b * a.s.tstride;
   const int c_lo = first >> a.kv.lps, c_hi = max(last, 0) >> a.kv.lps, ps = 1 << a.kv.lps;
   const auto page = [&](int key) { return table[clamped(key >> a.kv.lps, c_lo, c_hi)]; };
   const auto in_pool = [&](int id) { return clamped(id, 0, a.kv.n_pages - 1); };   // where the page is used: a look at it any earlier would wait for the fetches, too
@@ -278,8 +263,17 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
   }
   sum = sum_of_2(sum);
   if (!mine) return;
-  if (a.splits > 1) {                                                // a part: sums, then reference and sum
-    const long r = ((long)part * a.s.T + qi) * (a.kv.heads * a.G) + qh;
+  if (TREE && part) {
+    float* out = part + row * D + hi * 4;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *(f32x4*)(out + 32 * j + 8 * i) = f32x4{o[j][4 * i], o[j][4 * i + 1], o[j][4 * i + 2], o[j][4 * i + 3]};
+    if (hi == 0) *(float2*)(part + a.rows_cap * D + 2 * row) = make_float2(ref.at, sum);
+    return;
+  }
+  if (!TREE && a.splits > 1) {                                       // a share: sums, then reference and sum
+    const long r = ((long)share * a.s.T + qi) * (a.kv.heads * a.G) + qh;
     float* out = (float*)a.parts + r * D + hi * 4;
     if (sum != 0.f)
 #pragma unroll
@@ -300,60 +294,28 @@ __global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnA
     }
 }
 
-// The parts of a token's rows joined: four dims a thread, all of a token's over gridDim.y blocks, four parts under way
-template <class T, int D>
-__global__ __launch_bounds__(256) void paged_chunk_join_kernel(const PagedAttnArgs a) {
-  constexpr int U = 4;
-  const int t = blockIdx.x, heads = a.kv.heads * a.G, i = blockIdx.y * 256 + threadIdx.x, h = i / (D / 4), d = i % (D / 4) * 4;
-  const int b = last_at_most(a.s.B, t, [&](int k) { return clamped(a.s.starts[k], 0, a.s.T); });
+template <class T, int D, int W, bool TREE>
+__global__ __launch_bounds__(64 * W, 2) void paged_chunk_kernel(const PagedAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) PrefillLds<D> lds;
+  // heads change fastest: where there are 8 of them, each XCD reads one and keeps it in its L2; the last tiles of rows, which
+  // see the most keys, first
+  const int splits = TREE ? 1 : a.splits;
+  const int h = blockIdx.x % a.kv.heads, rest = blockIdx.x / a.kv.heads, share = rest % splits, tile = gridDim.x / (a.kv.heads * splits) - 1 - rest / splits;
+  const auto tile0 = [&](int i) { return a.by_tpt.div(clamped(a.s.starts[i], 0, a.s.T)) + i; };
+  const int b = last_at_most(a.s.B, tile, tile0);
   const Seq sq = sequence(a.s, b);
-  if (t >= sq.row0 + sq.n || sq.n <= a.most || h >= heads) return;   // nobody's row, or one that the other kernel has written
-  const long step = (long)a.s.T * heads, r = (long)t * heads + h;
-  const float* parts = (const float*)a.parts;
-  const float2* stats = (const float2*)(parts + a.splits * step * D);
-  float top = -INFINITY, sum = 0.f;
-  f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int p0 = 0; p0 < a.splits; p0 += U) {
-    f32x4 y[U];
-    float2 st[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long at = min(p0 + u, a.splits - 1) * step + r;
-      st[u] = stats[at];
-      y[u] = *(const f32x4*)(parts + at * D + d);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (p0 + u < a.splits && st[u].y != 0.f) {                     // 0: no key of the part is seen, and its sums are not written
-        const float now = fmaxf(top, st[u].x), ref = now == -INFINITY ? 0.f : now;
-        const float keep = __builtin_amdgcn_exp2f(top - ref), w = __builtin_amdgcn_exp2f(st[u].x - ref);
-        x = x * keep + y[u] * w;
-        sum = sum * keep + st[u].y * w;
-        top = now;
-      }
+  const RowTile r = rows_of_sequence<PF_K, TREE>(a, sq, b, (tile - tile0(b)) * a.tpt, a.tpt);
+  if (r.n <= 0 || (!TREE && sq.n <= a.most)) return;                 // few rows: not taken here
+  const int last = r.keys.hi - 1;
+  int t0 = r.keys.lo / PF_K, t1 = last < 0 ? t0 : last / PF_K + 1;
+  if (splits > 1) {                                                  // this block's share of the keys
+    const int per = (t1 - t0 + splits - 1) / splits;
+    t0 = min(t0 + share * per, t1);
+    t1 = min(t0 + per, t1);
   }
-  x *= sum == 0.f ? 0.f : 1.f / sum;
-  *(uint2*)(a.o + t * a.o_t + h * a.o_h + d * 2) = __builtin_bit_cast(uint2, __builtin_convertvector(x, typename T::v4));
+  chunk_rows<T, D, W, TREE>(a, lds, r, h, t0, t1, share, nullptr);
 }
 
 inline long chunk_blocks(const PagedAttnArgs& a) { return (a.s.T / (32 * a.waves / a.G) + a.s.B) * (long)a.kv.heads * a.splits; }
-
-template <class T, int D, int W, bool TREE>
-static void chunk_grid(PagedAttnArgs a, hipStream_t s) {
-  a.tpt = 32 * W / a.G;
-  a.by_tpt = FastDiv::by(a.tpt);
-  hipLaunchKernelGGL((paged_chunk_kernel<T, D, W, TREE>), dim3((unsigned)chunk_blocks(a)), dim3(64 * W), 0, s, a);
-  if (a.splits > 1) hipLaunchKernelGGL((paged_chunk_join_kernel<T, D>), dim3(a.s.T, (a.kv.heads * a.G * (D / 4) + 255) / 256), dim3(256), 0, s, a);
-}
-template <class T, int D, bool TREE>
-static void chunk_of(const PagedAttnArgs& a, hipStream_t s) {
-  a.waves == 4 ? chunk_grid<T, D, 4, TREE>(a, s) : chunk_grid<T, D, 8, TREE>(a, s);
-}
-template <bool TREE>
-static hipError_t launch_chunks(const PagedAttnArgs& a, int dtype, int head_dim, hipStream_t s) {
-  if (dtype == SNA_DTYPE_FP16) head_dim == 64 ? chunk_of<Fp16, 64, TREE>(a, s) : chunk_of<Fp16, 128, TREE>(a, s);
-  else head_dim == 64 ? chunk_of<Bf16, 64, TREE>(a, s) : chunk_of<Bf16, 128, TREE>(a, s);
-  return hipGetLastError();
-}
 
 }  // namespace sna

@@ -162,9 +162,12 @@ sna_status sna_paged_attention(const sna_paged_cache* cache, const sna_paged_bat
 }
 
 int64_t sna_tree_attention_workspace_bytes(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, int32_t mask_words, int32_t window) {
+  sna_status st;
   if (mask_words < 1 || mask_words > 64) return fail(SNA_E_CFG_RANGE, "masks of %d words (1 to 64 are supported)", mask_words);
+  if ((st = check_cache(cache)) != SNA_OK || (st = check_batch(batch)) != SNA_OK || (st = check_heads(cache, batch, q_heads)) != SNA_OK) return st;
   if (window < 0) return fail(SNA_E_CFG_RANGE, "window %d", window);
-  return sna_paged_attention_workspace_bytes(cache, batch, q_heads, window ? tree_window(window, mask_words) : 0);
+  if (batch->n_tokens == 0) return 0;
+  return (int64_t)tree_attention_workspace(seqs_of(batch), cache->kv_heads, q_heads / cache->kv_heads, batch->max_new, batch->max_len, window ? window : INT32_MAX, mask_words, cache->head_dim);
 }
 
 sna_status sna_tree_attention(const sna_paged_cache* cache, const sna_paged_batch* batch, int32_t q_heads, const sna_rows* q, const sna_rows* out,
