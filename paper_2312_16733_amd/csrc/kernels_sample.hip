@@ -148,6 +148,7 @@ __device__ __forceinline__ u64 last_lane(u64 v) {
 }
 struct Add { __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a + b; } };
 struct Or { __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a | b; } };
+struct Most { __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a > b ? a : b; } };
 struct And { __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a & b; } };
 __device__ __forceinline__ u64 scan_up(u64 v) { return scan_of(v, 0, Add()); }
 __device__ __forceinline__ u64 sum_of_wave(u64 v) { return last_lane(scan_up(v)); }
@@ -162,10 +163,13 @@ __device__ __forceinline__ float max_of_wave(float v) {
   return __uint_as_float((unsigned)last_lane(__float_as_uint(v)));
 }
 
+constexpr int SM_FEW = 128;        // logits that one wave ends a row with
 template <int NT>
 struct SampleLds {
   u64 sums[SM_BINS], waves[NT / 64], ups[NT / 64], before, found;
-  int digit, n;
+  u64 place[SM_FEW], steps[SM_FEW];
+  double weight[SM_FEW];
+  int digit, n, few;
   float top[NT / 64];
 };
 template <int NT>
@@ -189,10 +193,11 @@ __device__ __forceinline__ float max_of_block(SampleLds<NT>& lds, float v) {
   return v;
 }
 
-// The bin of lds.sums at which their running sum reaches `want` (1 or more, at most the sum of all), and what comes before it.
-// All threads get both; the sums are complete when it is called, and zero when it returns.
-template <int NT>
-__device__ __forceinline__ int crossing(SampleLds<NT>& lds, u64 want, u64& before) {
+// The bin of lds.sums at which their running sum reaches want(the sum of all), which is 1 .. that, and what comes before it and is
+// wanted of it.  All threads get them; the sums are complete when it is called, and zero when it returns.
+struct Crossing { int bin; u64 want, total; };
+template <int NT, class Want>
+__device__ __forceinline__ Crossing crossing(SampleLds<NT>& lds, const Want& want_of) {
   constexpr int N = SM_BINS / NT;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   u64 v[N], mine = 0;
@@ -205,9 +210,15 @@ __device__ __forceinline__ int crossing(SampleLds<NT>& lds, u64 want, u64& befor
   if (lane == 63) lds.ups[wave] = up;
   __syncthreads();
   if (tid == 0) lds.n = 0;
+  Crossing c;
+  c.total = 0;
   u64 at = up - mine;
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w) at += w < wave ? lds.ups[w] : 0;
+  for (int w = 0; w < NT / 64; ++w) {
+    at += w < wave ? lds.ups[w] : 0;
+    c.total += lds.ups[w];
+  }
+  const u64 want = want_of(c.total);
   if (at < want && want <= at + mine)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -215,7 +226,21 @@ __device__ __forceinline__ int crossing(SampleLds<NT>& lds, u64 want, u64& befor
       at += v[i];
     }
   __syncthreads();
-  before = lds.before;
+  c.bin = lds.digit;
+  c.want = want - lds.before;
+  return c;
+}
+// The thread at whose value the running sum of the threads' reaches `want`, which is 1 .. the sum of all
+template <int NT>
+__device__ __forceinline__ int reached_at(SampleLds<NT>& lds, u64 v, u64 want) {
+  const int tid = threadIdx.x, wave = tid >> 6;
+  u64 up = scan_up(v);
+  if ((tid & 63) == 63) lds.ups[wave] = up;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) up += w < wave ? lds.ups[w] : 0;
+  if (up >= want && up - v < want) lds.digit = tid;
+  __syncthreads();
   return lds.digit;
 }
 
@@ -231,9 +256,9 @@ __device__ __forceinline__ u64 select(SampleLds<NT>& lds, int bits, u64 want, co
       if (w && ((order ^ lo) & known) == 0) atomicAdd(&lds.sums[(order & mask) >> shift], w);
     });
     __syncthreads();
-    u64 before;
-    const u64 digit = crossing(lds, want, before);
-    want -= before;
+    const Crossing c = crossing(lds, [&](u64) { return want; });
+    const u64 digit = c.bin;
+    want = c.want;
     known |= mask & ~((1ull << shift) - 1);
     lo |= digit << shift;
     each([&](u64 order, u64 w) {
@@ -344,6 +369,68 @@ __device__ __forceinline__ int draw_held(SampleLds<NT>& lds, const SampleArgs& a
   return (int)select_held(lds, drawn_at(a, row, total), i, s);
 }
 
+// The same for up to SM_FEW of them, whose places and weights are in LDS, by the first wave alone, two a lane: each adds up what
+// stands before it in the order of falling logits, and then what of the kept ones stands before it in the vocabulary's
+template <int NT>
+__device__ __forceinline__ int draw_few(SampleLds<NT>& lds, const SampleArgs& a, int row, Row& r, int n, u64& total) {
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    const u64 index = (1ull << r.bits) - 1;
+    u64 p[2], s[2], before[2] = {}, last = 0;
+    double w[2];
+    int rank[2] = {};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int i = lane + 64 * j;
+      p[j] = i < n ? lds.place[i] : ~0ull;
+      w[j] = i < n ? lds.weight[i] : 0.0;
+      s[j] = r.steps(w[j]);
+      lds.steps[i] = s[j];
+    }
+    for (int i = 0; i < n; ++i) {
+      const u64 pi = lds.place[i], si = lds.steps[i];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        rank[j] += pi < p[j];
+        before[j] += pi < p[j] ? si : 0;
+      }
+    }
+    bool kept[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) kept[j] = lane + 64 * j < n && (!r.top_k || rank[j] < r.top_k);
+    if (r.top_p < 1.f) {
+      const u64 want = part_of(r.top_p, sum_of_wave((kept[0] ? s[0] : 0) + (kept[1] ? s[1] : 0)));
+#pragma unroll
+      for (int j = 0; j < 2; ++j) kept[j] = kept[j] && before[j] < want;
+    }
+    u64 up[2] = {};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      last = kept[j] && p[j] > last ? p[j] : last;
+      s[j] = kept[j] ? r.steps(r.left(w[j])) : 0;
+      lds.steps[lane + 64 * j] = s[j];
+    }
+    last = last_lane(scan_of(last, 0, Most()));
+    const u64 sum = sum_of_wave(s[0] + s[1]), want = drawn_at(a, row, sum);
+    for (int i = 0; i < n; ++i) {
+      const u64 pi = lds.place[i] & index, si = lds.steps[i];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) up[j] += pi <= (p[j] & index) ? si : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (up[j] >= want && up[j] - s[j] < want) lds.digit = (int)(p[j] & index);
+    if (lane == 0) {
+      lds.before = sum;
+      lds.found = last;
+    }
+  }
+  __syncthreads();
+  total = lds.before;
+  r.cut = lds.found;
+  return lds.digit;
+}
+
 // ---- rows of a block -----------------------------------------------------------------------------------------------------------
 template <class X, int NT>
 __global__ __launch_bounds__(NT) void sample_small_kernel(const SampleArgs a) {
@@ -352,6 +439,7 @@ __global__ __launch_bounds__(NT) void sample_small_kernel(const SampleArgs a) {
   const int tid = threadIdx.x, row = blockIdx.x, V = a.V;
   const X* logits = (const X*)a.logits + row * a.stride;
   for (int i = tid; i < SM_BINS; i += NT) lds.sums[i] = 0;
+  if (tid == 0) lds.few = 0;
   float x[N], top = -INFINITY;
   int at[N];
 #pragma unroll
@@ -369,7 +457,36 @@ __global__ __launch_bounds__(NT) void sample_small_kernel(const SampleArgs a) {
   if (some) {
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] = r.seen(x[j]);
-    token = draw_held(lds, a, row, r, total, x, at, w);
+    // what may be kept, where that is little: all of a small row, or what is no further from the largest than the last of top_k
+    int at_most = -1;
+    if (V <= SM_FEW) at_most = SM_BINS;
+    else if (r.top_k && r.top_k < SM_FEW) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (x[j] > -INFINITY) atomicAdd(&lds.sums[r.distance(x[j])], 1ull);
+      __syncthreads();
+      at_most = crossing(lds, [&](u64 n) { return n < (u64)r.top_k ? n : (u64)r.top_k; }).bin;
+    }
+    if (at_most >= 0) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (x[j] > -INFINITY && r.distance(x[j]) <= at_most) {
+          const int n = atomicAdd(&lds.few, 1);
+          if (n < SM_FEW) {
+            lds.place[n] = r.place(x[j], at[j]);
+            lds.weight[n] = r.weight(x[j]);
+          }
+        }
+      __syncthreads();
+    }
+    if (at_most >= 0 && lds.few <= SM_FEW) {
+      token = draw_few(lds, a, row, r, lds.few, total);
+      if (a.probs)
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[j] = r.kept(x[j], at[j]);
+    } else {
+      token = draw_held(lds, a, row, r, total, x, at, w);
+    }
   }
   if (tid == 0) a.tokens[row] = token;
   if (a.probs) {
@@ -504,16 +621,12 @@ __global__ __launch_bounds__(SM_T) void sample_sums_kernel(const SampleArgs a, c
 // The distance that the row's cut lies at, and what is wanted of it there; SM_BINS: it is not cut.  of(j): sum j of the thread's
 template <int NT, class Of>
 __device__ __forceinline__ int cut_at(SampleLds<NT>& lds, const Row& r, Kind kind, u64& want, const Of& of) {
-  u64 all = 0;
 #pragma unroll
-  for (int i = 0; i < SM_BINS / NT; ++i) all += lds.sums[i * NT + threadIdx.x] = of(i);
-  all = sum_of_block(lds, all);                                      // and the sums are there
-  want = kind == CUT_COUNT ? (u64)r.top_k : part_of(r.top_p, all);
-  if (kind == CUT_COUNT && all <= want) return SM_BINS;
-  u64 before;
-  const int d = crossing(lds, want, before);
-  want -= before;
-  return d;
+  for (int i = 0; i < SM_BINS / NT; ++i) lds.sums[i * NT + threadIdx.x] = of(i);
+  __syncthreads();
+  const Crossing c = crossing(lds, [&](u64 all) { return kind == CUT_WEIGHT ? part_of(r.top_p, all) : all < (u64)r.top_k ? all : (u64)r.top_k; });
+  want = c.want;
+  return kind == CUT_COUNT && c.total <= (u64)r.top_k ? SM_BINS : c.bin;
 }
 
 template <class X>
@@ -632,7 +745,14 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
       x[j] = is ? __uint_as_float((unsigned)(held[j] >> 32)) : -INFINITY;
       at[j] = is ? (int)held[j] : 0;
     }
-    if (kind == CUT_COUNT) {
+    if (kind == CUT_COUNT && m <= SM_FEW) {
+      if (tid < (int)m) {
+        lds.place[tid] = r.place(x[0], at[0]);
+        lds.weight[tid] = r.weight(x[0]);
+      }
+      __syncthreads();
+      token = draw_few(lds, a, row, r, (int)m, total);
+    } else if (kind == CUT_COUNT) {
       double left[N];
       token = draw_held(lds, a, row, r, total, x, at, left);
     } else {
@@ -657,23 +777,11 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
         if (s) atomicAdd(&lds.sums[at[j] / SM_RUN], s);
       }
       __syncthreads();
-      total = 0;
-      for (int i = tid; i < SM_BINS; i += SM_FINAL) total += lds.sums[i];
-      total = sum_of_block(lds, total);
-      const u64 want = drawn_at(a, row, total);
-      u64 before;
-      const int run = crossing(lds, want, before);
-      constexpr int M = SM_RUN / SM_FINAL;
-      u64 s[M], o[M];
-#pragma unroll
-      for (int j = 0; j < M; ++j) {
-        const int i = run * SM_RUN + j * SM_FINAL + tid;
-        s[j] = i < a.V ? r.steps(r.kept(r.seen(logit(logits, i)), i)) : 0;
-        o[j] = j * SM_FINAL + tid;
-      }
-      token = run * SM_RUN + (int)select(lds, 9, want - before, [&](const auto& f) {
-        for (int j = 0; j < M; ++j) f(o[j], s[j]);
-      });
+      const Crossing c = crossing(lds, [&](u64 all) { return drawn_at(a, row, all); });
+      total = c.total;
+      static_assert(SM_FINAL == SM_RUN, "a logit of the run a thread");
+      const int i = c.bin * SM_RUN + tid;
+      token = c.bin * SM_RUN + reached_at(lds, i < a.V ? r.steps(r.kept(r.seen(logit(logits, i)), i)) : 0, c.want);
     }
   }
   if (tid == 0) {
