@@ -92,10 +92,9 @@ struct Row {                       // of logits, and what is wanted of it
     return x > -INFINITY && place(x, i) <= cut ? left(weight(x)) : 0.0;
   }
   // Rises as x falls, in SM_BINS steps: 256 even ones of 1 / 64 of the temperature, then twice as wide from 4 temperatures on, and
-  // again from 12, 28, .. on: what 1 and more has of bits behind the leading ones
-  __device__ __forceinline__ int distance(float x) const {
-    return (int)min((__float_as_uint(fmaf(top32 - x, near, 1.f)) >> 15) - (0x3f800000u >> 15), (unsigned)SM_BINS - 1);
-  }
+  // again from 12, 28, .. on: what a number from 2 on has of bits behind the leading ones
+  __device__ __forceinline__ int distance(float x) const { return (int)min(far(x) >> 15, (unsigned)SM_BINS - 1); }
+  __device__ __forceinline__ unsigned far(float x) const { return __float_as_uint(fmaf(top32 - x, near, 2.f)) & 0x3fffffff; }        // from 2 on: the exponent begins with zeros
 };
 template <class X>
 __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
@@ -105,7 +104,7 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
   const int k = a.top_k_of ? a.top_k_of[row] : a.top_k;
   const double inv = t > 0.f ? 1.0 / (double)fminf(t, 1e33f) : 1.0;
   r.per = inv * 1.44269504088896340736;
-  r.near = fmaxf((float)fmin(inv * 0.25, 1e38), 1e-38f);
+  r.near = fmaxf((float)fmin(inv * 0.5, 1e38), 1e-38f);
   r.min_p = fmin(fmax((double)(a.min_p_of ? a.min_p_of[row] : a.min_p), 0.0), 1.0);       // what is no number cuts nothing, and the largest stays
   r.magic = __longlong_as_double((long long)(1023 + 52 - a.scale_bits) << 52);
   r.top_p = a.top_p_of ? a.top_p_of[row] : a.top_p;
@@ -658,6 +657,16 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
     sum = sum_of_wave(sum);
     if (lane == 0) w.runs[(long)row * w.n_runs + run] = sum;
   };
+  // of n logits, a lane's
+  const auto sum_of = [&](int n, const auto& logit_at) {
+    u64 sum = 0;
+    int adds = 0;
+    if (r.min_p > 0.0)
+      for (int j = lane; j < n; j += 64) sum += r.steps(r.left(r.weight(logit_at(j))));
+    else
+      for (int j = lane; j < n; j += 64, ++adds) sum += (u64)__double_as_longlong(r.weight(logit_at(j)) + r.magic);       // the power of two that carries the steps comes off together
+    return sum - (u64)adds * (u64)__double_as_longlong(r.magic);
+  };
   if (kind == CUT_COUNT) {
     each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int) {
 #pragma unroll
@@ -668,19 +677,18 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
     // The ones above the cut move together first: of 512 logits they are fewer than half as a rule, and the weights are what takes time
     float* above = (float*)lds.sums + (tid >> 6) * SM_RUN;
     static_assert(sizeof(lds.sums) >= SM_T / 64 * SM_RUN * sizeof(float), "a wave's run");
+    const unsigned from = (unsigned)at << 15, width = at < SM_BINS - 1 ? 1u << 15 : ~0u - from;
     each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int run) {
       int n = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int d = r.distance(x[e]);
-        const u64 yes = __ballot(d < at);
-        if (d < at) above[n + __builtin_amdgcn_mbcnt_hi((unsigned)(yes >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)yes, 0))] = x[e];
+        const unsigned d = r.far(x[e]);
+        const u64 yes = __ballot(d < from);
+        if (d < from) above[n + __builtin_amdgcn_mbcnt_hi((unsigned)(yes >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)yes, 0))] = x[e];
         n += __popcll(yes);
-        if (d == at && x[e] > -INFINITY) add(x[e], i + e);
+        if (d - from < width && x[e] > -INFINITY) add(x[e], i + e);
       }
-      u64 sum = 0;
-      for (int j = lane; j < n; j += 64) sum += r.steps(r.left(r.weight(above[j])));       // a wave's own: in order without a barrier
-      end_run(sum, run);
+      end_run(sum_of(n, [&](int j) { return above[j]; }), run);      // a wave's own: in order without a barrier
     });
   } else {
     each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int run) {
