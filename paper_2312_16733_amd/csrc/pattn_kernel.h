@@ -622,7 +622,7 @@ static hipError_t rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
   if constexpr (!TREE)             // one token's keys are the same for all of its rows, but for a tree's, whose masks leave out some between
     if (mb == 1 && a.max_new == 1) return rows_grid<T, D, 1, true, false>(a, s);
   if (mb == 1) return rows_grid<T, D, 1, false, TREE>(a, s);
-  if constexpr (!TREE)             // of trees more than 32 rows go to the many-rows kernel
+  if constexpr (!TREE)             // trees come in one tile of up to 32 rows or two of 32, and with more to the many-rows kernel
     if (mb == 4) return rows_grid<T, D, 4, false, false>(a, s);
   return rows_grid<T, D, 2, false, TREE>(a, s);
 }

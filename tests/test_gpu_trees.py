@@ -117,6 +117,26 @@ def test_values_that_are_no_numbers_reach_only_those_that_see_them(heads, seqs, 
         assert not torch.isfinite(out[hit].float()).any()
 
 
+@pytest.mark.parametrize("heads,seqs", [((8, 2, 128), [(100, 5), (60, 3)]), ((8, 2, 128), [(900, 90), (500, 1)]), ((32, 8, 128), [(4000, 70), (3000, 64)]), ((4, 4, 64), [(400, 60), (90, 9)])])
+def test_arrays_that_do_not_fit(heads, seqs):
+    """Pages that are none, lengths beyond the table, prefixes and positions of any value, masks full of ones: whatever comes back for
+    those sequences, the last is right."""
+    s = tree.make(seqs * 2 + [(70, 1), (200, 40)], *heads, 16, torch.bfloat16, seed=30, earlier=0)
+    want, err = tree.attention(s)
+    n = s["seqs"][-1][1]
+    prefix = torch.tensor(s["base"], dtype=torch.int32, device="cuda")
+    prefix[:4] = torch.tensor([-5, 2 ** 31 - 1, -2 ** 31, 17], dtype=torch.int32)
+    s["positions"][:3] = torch.tensor([2 ** 31 - 1, -2 ** 31, -1], dtype=torch.int32)
+    s["masks"][: -n] = -1
+    s["table"][0, 1], s["table"][0, 2] = -5, 2 ** 31 - 1
+    s["lens"][1], s["lens"][2], s["lens"][4] = 10 ** 9, -7, 0
+    s["prefix"] = prefix
+    for window in (0, 300):
+        out = attend(s, window)
+        torch.cuda.synchronize()
+        within(out[-n:], want[-n:], err[-n:], "the last sequence")
+
+
 def test_positions_of_the_tree():
     """kv_append rotates by the positions it is given and stores by slots."""
     s = tree.make([(40, 13), (100003, 7), (9, 0)], 9, 3, 64, 16, torch.float16, seed=14, junk=False)

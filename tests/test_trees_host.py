@@ -44,6 +44,24 @@ def test_tree_attention_is_refused():
     assert tree(b=batch(n_seqs=0)) == RANGE
 
 
+def test_launches_of_trees():
+    """What the workspace tells of them: none where a block walks whole rows, the causal form's up to 32 rows a key / value head, parts of
+    128 rows for more, from keys on whose sharing pays."""
+    bytes_of = lambda n, nodes, length, words=1, window=0: sna.lib().sna_tree_attention_workspace_bytes(  # noqa: E731
+        cache(kv_heads=8, k_page_stride=8 * 16 * 64, v_page_stride=8 * 16 * 64), batch(n_seqs=n, n_tokens=n * nodes, max_new=nodes, max_len=length, table_width=length), 32, words, window)
+    causal = lambda n, nodes, length: sna.lib().sna_paged_attention_workspace_bytes(  # noqa: E731
+        cache(kv_heads=8, k_page_stride=8 * 16 * 64, v_page_stride=8 * 16 * 64), batch(n_seqs=n, n_tokens=n * nodes, max_new=nodes, max_len=length, table_width=length), 32, 0)
+    for nodes in (1, 4, 8):
+        for length in (100, 5000, 50000):
+            assert bytes_of(3, nodes, length) == causal(3, nodes, length)
+    assert bytes_of(16, 30, 300) == 0 and bytes_of(1, 60, 300) == 0
+    for nodes, planes in ((32, 1), (33, 2), (77, 3), (500, 16)):
+        shares = 512 // planes // 8 * 8
+        assert bytes_of(4, nodes, 60000, 8) == -(-shares * planes * (16 + 2 * 4 * (min(nodes, 32) * 4 * 66)) // 256) * 256, nodes
+    assert bytes_of(4, 600, 60000, 10) == 0                                          # rows enough to fill the chip
+    assert bytes_of(4, 77, 60000, 2, 100) == 0                                       # few keys in the window
+
+
 def test_positions_are_refused():
     at = lambda p: sna.lib().sna_kv_append_at(cache(), batch(), 4, rows(), rows(), rows(), rows(), AT, 64, 0, None, None, 1e-6, p, None)  # noqa: E731
     assert at(AT + 2) == ALIGN
