@@ -39,10 +39,12 @@ static hipError_t tree_grid(PagedAttnArgs a, hipStream_t s) {
     a.rows_cap = a.tpt * a.G;
     a.least = kTreeLeast;
     const int planes = tree_planes(a.max_new, a.G);
+    const long pairs = (long)a.s.B * a.kv.heads;                     // (tree, head)s
     hipLaunchKernelGGL((tree_split_kernel<T, D, W>), dim3(a.blocks * planes), dim3(64 * W), 0, s, a);
     // rows of a (sequence, head) that a block of the join takes at once, as many as its parts allow
-    const int per = std::max(1, (int)(a.blocks / std::max(1l, (long)a.s.B * a.kv.heads))), at_once = std::max(1, 1024 / D / std::max(1, (per + 7) / 8));
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.blocks * planes, (a.rows_cap + at_once - 1) / at_once), dim3(256), 0, s, a);
+    const int per = std::max(1, (int)(a.blocks / pairs)), at_once = std::max(1, 1024 / D / std::max(1, (per + 7) / 8));
+    a.cut = 8 * pairs <= a.blocks ? (int)pairs : a.blocks;           // see paged_join_kernel
+    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.cut * planes, (a.rows_cap + at_once - 1) / at_once), dim3(256), 0, s, a);
     return hipGetLastError();
   }
   a.waves = W;

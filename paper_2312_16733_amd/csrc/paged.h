@@ -228,7 +228,7 @@ struct PagedAttnArgs {
   int waves;                                     // of a block (few rows: of one that walks all keys of its rows)
   int tpt;                                       // tokens of a tile of rows
   FastDiv by_tpt;
-  int rows_cap, least, blocks;                   // rows of a part; least tiles of a share; blocks that share
+  int rows_cap, least, blocks, cut;              // rows of a part; least tiles of a share; blocks that share; (tile of rows, head)s at most that are cut
   int splits;                                    // many rows: shares of the keys
   // of trees only
   const unsigned long long* masks;               // [T][words]

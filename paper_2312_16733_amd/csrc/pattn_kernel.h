@@ -528,19 +528,44 @@ __global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_ke
              });
 }
 
+// The k-th block that began a part, of those that firsts tells of, or -1 (a wave's work)
+__device__ __forceinline__ int begun_at(const First* firsts, int blocks, int k) {
+  constexpr int TURNS = kTreeBlocks / 64;                            // of 64 blocks; no launch has more
+  const int lane = threadIdx.x & 63;
+  int n[TURNS], at = -1;
+#pragma unroll
+  for (int i = 0; i < TURNS; ++i) n[i] = 64 * i + lane < blocks ? firsts[64 * i + lane].n : 0;
+#pragma unroll
+  for (int i = 0; i < TURNS; ++i) {
+    const unsigned long long some = __ballot(n[i] > 0), here = __ballot(n[i] > 0 && __popcll(some & ((1ull << lane) - 1)) == k);
+    if (at < 0 && here) at = 64 * i + __ffsll((long long)here) - 1;
+    k -= __popcll(some);
+  }
+  return at;
+}
+
 // Parts joined: JN_Y blocks for each (tile of rows, head) that was cut.  A thread has four dims of a row; the 256 / (D / 4)
 // groups of a row's threads take that many rows at a time where the parts are few, or share a row's parts where they are many.
 // Sums, maximum and statistics of a part are asked for together: with the statistics first, a row of 64 parts took 5 us.
+// No more parts are begun than there are (tile of rows, head)s.  Where these are far fewer (cut) than the blocks that share the keys, most of
+// this launch's would only come to end, and a block looks for its part among what they began instead: one tree of 77 tokens, 8 heads and
+// 168 shares, 13.3 us and 9.6; 16 trees, 128 cut and 512 shares, 10.3 and 13.2, so not there.
 constexpr int JN_Y = 8;
 template <class T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) {
   constexpr int W = D / 4, N = 256 / W, U = 8;                       // threads of a row; groups; parts under way
   __shared__ __attribute__((aligned(16))) float so[N][D];
   __shared__ float2 ss[N];
-  const int p = blockIdx.x, planes = gridDim.x / a.blocks, g = threadIdx.x / W, d = threadIdx.x % W * 4;       // planes: see tree_split_kernel
+  const int planes = gridDim.x / a.cut, plane = blockIdx.x / a.cut, g = threadIdx.x / W, d = threadIdx.x % W * 4;       // planes: see tree_split_kernel
+  int at = blockIdx.x % a.cut;
+  if (a.cut < a.blocks) {
+    at = begun_at((const First*)a.parts + plane * a.blocks, a.blocks, at);
+    if (at < 0) return;
+  }
+  const int p = plane * a.blocks + at;
   const First f = ((const First*)a.parts)[p];
   if (f.n == 0) return;
-  const int n = f.last - p % a.blocks + 1, rows = f.n * a.G;
+  const int n = f.last - at + 1, rows = f.n * a.G;
   int share = 1;                                                     // groups that share a row
   while (share < N && n > U * share) share *= 2;
   const int at_once = N / share;
@@ -601,6 +626,7 @@ static hipError_t rows_grid(PagedAttnArgs a, hipStream_t s) {
     if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
     a.rows_cap = a.tpt * a.G;
     a.least = kSplitLeast;
+    a.cut = a.blocks;
     hipLaunchKernelGGL((paged_split_kernel<T, D, MB, ONE, TREE>), dim3(a.blocks), dim3(64 * kSplitW), 0, s, a);
     hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
     return hipGetLastError();
