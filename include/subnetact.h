@@ -442,10 +442,10 @@ sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, 
 /* Which tokens of drafted trees stand.  A step's tokens of sequence b are its tree: the first is the root, which stands (the last
  * token that is known); token i > 0 is a child of parents[i] (its number within the sequence, less than i; others are nobody's
  * child).  sampled[i] is the token drawn behind token i (from the target's probabilities there), and of the children of a token
- * that stands the first one with tokens[child] == sampled[i] stands, too; a sampled token below 0 matches none.  kept[b]
- * (int32 [n_seqs][max_new]): the numbers of those that stand, rising, then -1; counts[b]: how many; next[b] (int32): sampled behind
- * the last of them, -1 where the sequence brings no tokens.  Tokens of 4 or 8 bytes; max_new is at most 4096.  Of the batch, starts,
- * lens, the sizes and max_new are used.
+ * that stands the first one with tokens[child] == sampled[i] stands, too; a sampled token below 0 matches none.  Written are
+ * kept[b] (int32 [n_seqs][max_new]): the numbers of those that stand, rising, then -1; counts[b] (int32): how many; next[b] (int32):
+ * sampled behind the last of them, -1 where the sequence brings no tokens; all apart from each other and from what is read.  Tokens
+ * of 4 or 8 bytes; max_new is at most 4096.  Of the batch, starts, lens, the sizes and max_new are used.
  * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_HIP. */
 sna_status sna_verify_tree(const sna_paged_batch* batch, const void* sampled_dev, int32_t sampled_bytes, const void* tokens_dev, int32_t token_bytes,
                            const int32_t* parents_dev, int32_t* kept_dev, int32_t* counts_dev, int32_t* next_dev, void* hip_stream);
@@ -471,8 +471,8 @@ sna_status sna_copy_pages(const sna_paged_cache* cache, const int32_t* source_de
  * which the weights that are left make more than uniforms[r] (of [0, 1)) of all of them.  Temperature 0: the first of the largest.
  * A logit that is no number counts as -inf, weight 0; where +inf is the largest, only those have weight.  A row without weight gives
  * -1.  Weights are formed in 64 bits and held in steps of 2^-44 of the largest, or finer below 2^18 logits and up to
- * 2^-42 at 2^20: one below half a step is never drawn.  probs (fp32 [n_rows][vocab], may be NULL): what is left, each weight over
- * their sum.  The settings are one number for all rows or, where the pointer is given, fp32 (top_k: int32) [n_rows] in device
+ * 2^-42 at 2^20: one below half a step is never drawn.  probs (fp32 [n_rows][vocab], may be NULL, no element of it a logit's): what is
+ * left, each weight over their sum.  The settings are one number for all rows or, where the pointer is given, fp32 (top_k: int32) [n_rows] in device
  * memory; there a temperature that is not positive is 0 and one above 1e33 is that, and a top_k below 1, a top_p of 1 or more and
  * what is no number cut nothing.  Workspace as for attention.
  * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_WORKSPACE, SNA_E_HIP. */

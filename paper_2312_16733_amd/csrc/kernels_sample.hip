@@ -27,7 +27,7 @@ constexpr int SM_MOST = SM_LIST / 2;             // top_k up to which a row's li
 constexpr int SM_RUN = 512;        // logits of a wave's turn, and of a sum
 constexpr int SM_STAGE = 1024;     // logits at the cut that a block writes out at once
 constexpr int SM_T = 512;          // threads of the blocks that share a row
-constexpr int SM_FINAL = 512;     // of the one that ends it
+constexpr int SM_FINAL = 512;      // of the one that ends it
 
 __device__ __forceinline__ float logit(const float* p, long i) { return p[i]; }
 __device__ __forceinline__ float logit(const __bf16* p, long i) { return (float)p[i]; }

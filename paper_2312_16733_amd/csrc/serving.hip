@@ -206,6 +206,13 @@ sna_status sna_verify_draft(const float* target_dev, int64_t target_seq_stride, 
   return launched(e, "verify_draft");
 }
 
+// No byte of both
+struct Bytes { const void* at; int64_t n; };
+static bool apart(const Bytes& a, const Bytes& b) {
+  const uintptr_t p = (uintptr_t)a.at, q = (uintptr_t)b.at;
+  return a.n <= 0 || b.n <= 0 || (p <= q ? q - p >= (uintptr_t)a.n : p - q >= (uintptr_t)b.n);
+}
+
 sna_status sna_verify_tree(const sna_paged_batch* batch, const void* sampled_dev, int32_t sampled_bytes, const void* tokens_dev, int32_t token_bytes,
                            const int32_t* parents_dev, int32_t* kept_dev, int32_t* counts_dev, int32_t* next_dev, void* hip_stream) {
   if (!batch) return fail(SNA_E_NULL, "paged batch: NULL");
@@ -218,6 +225,15 @@ sna_status sna_verify_tree(const sna_paged_batch* batch, const void* sampled_dev
     return fail(SNA_E_NULL, "verify_tree: a required pointer is NULL");
   if (((uintptr_t)parents_dev | (uintptr_t)kept_dev | (uintptr_t)counts_dev | (uintptr_t)next_dev) & 3 || (uintptr_t)sampled_dev & (sampled_bytes - 1) || (uintptr_t)tokens_dev & (token_bytes - 1))
     return fail(SNA_E_CFG_ALIGN, "verify_tree: a pointer is not aligned to its elements");
+  const int64_t n = batch->n_seqs, tokens = batch->n_tokens;
+  const Bytes out[] = {{kept_dev, 4 * n * batch->max_new}, {counts_dev, 4 * n}, {next_dev, 4 * n}};
+  const Bytes in[] = {{batch->starts_dev, 4 * n + 4}, {batch->lens_dev, 4 * n}, {sampled_dev, sampled_bytes * tokens}, {tokens_dev, token_bytes * tokens}, {parents_dev, 4 * tokens}};
+  for (int i = 0; i < 3; ++i) {
+    bool free = true;
+    for (const Bytes& x : in) free = free && apart(out[i], x);
+    for (int j = 0; j < i; ++j) free = free && apart(out[i], out[j]);
+    if (!free) return fail(SNA_E_CFG_RANGE, "verify_tree: a result is written over another or over what is read");
+  }
   const TreeWalkArgs a = {seqs_of(batch), sampled_dev, tokens_dev, sampled_bytes, token_bytes, parents_dev, kept_dev, counts_dev, next_dev, batch->max_new};
   return launched(launch_verify_tree(a, (hipStream_t)hip_stream), "verify_tree");
 }
@@ -233,8 +249,10 @@ sna_status sna_kv_compact(const sna_paged_cache* cache, const sna_paged_batch* b
   if (!batch->starts_dev || !batch->lens_dev || !batch->page_table_dev || (kept_width && !kept_dev) || !counts_dev || !lens_dev)
     return fail(SNA_E_NULL, "kv_compact: a required pointer is NULL");
   if (batch->table_width < 1 || batch->table_stride < 0 || batch->table_stride > INT32_MAX) return fail(SNA_E_CFG_RANGE, "paged batch: page table of %d columns", batch->table_width);
-  if (lens_dev == batch->lens_dev || lens_dev == batch->starts_dev || lens_dev == counts_dev || lens_dev == kept_dev)
-    return fail(SNA_E_CFG_RANGE, "kv_compact: the new lengths are written over what is read");
+  const int64_t n = batch->n_seqs;
+  for (const Bytes& x : {Bytes{batch->lens_dev, 4 * n}, Bytes{batch->starts_dev, 4 * n + 4}, Bytes{batch->page_table_dev, 4 * ((n - 1) * batch->table_stride + batch->table_width)},
+                         Bytes{counts_dev, 4 * n}, Bytes{kept_dev, 4 * n * kept_width}})
+    if (!apart(Bytes{lens_dev, 4 * n}, x)) return fail(SNA_E_CFG_RANGE, "kv_compact: the new lengths are written over what is read");
   if (((uintptr_t)kept_dev | (uintptr_t)counts_dev | (uintptr_t)lens_dev) & 3) return fail(SNA_E_CFG_ALIGN, "kv_compact: a pointer is not aligned to its elements");
   CompactArgs a = {};
   a.s = seqs_of(batch);

@@ -82,6 +82,22 @@ def test_walks_are_refused():
     assert walk(b=batch(n_seqs=0, n_tokens=0)) == 0
 
 
+def test_results_over_what_is_read_are_refused():
+    at = lambda i: 0x100000 * (i + 1)  # noqa: E731
+    b = dict(n_seqs=3, n_tokens=40, max_new=20, starts_dev=at(0), lens_dev=at(1), page_table_dev=at(2), table_stride=50, table_width=7)
+    read = dict(starts=(at(0), 16), lens=(at(1), 12), sampled=(at(3), 8 * 40), tokens=(at(4), 4 * 40), parents=(at(5), 4 * 40))
+    results = dict(kept=(at(6), 4 * 60), counts=(at(7), 12), following=(at(8), 12))
+    good = dict(sampled=at(3), sb=8, tokens=at(4), parents=at(5), **{k: p for k, (p, _) in results.items()})
+    for name, (_, size) in results.items():
+        for other, (p, n) in (read | results).items():
+            if other != name:
+                for over in (p, p + n - 4, p - size + 4):
+                    assert walk(b=batch(**b), **(good | {name: over})) == RANGE, (name, other)
+    for p, n in (read["starts"], read["lens"], (at(2), 4 * (2 * 50 + 7)), (at(4), 4 * 3 * 5), (at(5), 12)):
+        for over in (p, p + n - 4, p - 8):
+            assert compact(b=batch(**b), kept=at(4), width=5, counts=at(5), lens=over) == RANGE
+
+
 def compact(c=None, b=None, kept=AT, width=3, counts=2 * AT, lens=3 * AT):
     return sna.lib().sna_kv_compact(c or cache(), b or batch(), kept, width, counts, lens, None)
 
@@ -101,7 +117,7 @@ def test_compaction_is_refused():
         assert compact(**over) == RANGE, over
     assert compact(b=batch(n_seqs=0)) == 0
     wide = dict(c=cache(kv_heads=4096, k_page_stride=4096 * 16 * 64, v_page_stride=4096 * 16 * 64), b=batch(n_seqs=1 << 20))
-    assert compact(**wide) == RANGE and b"more blocks than a launch has" in sna.lib().sna_last_error()
+    assert compact(**wide, lens=1 << 40) == RANGE and b"more blocks than a launch has" in sna.lib().sna_last_error()
 
 
 def test_copies_are_refused():
