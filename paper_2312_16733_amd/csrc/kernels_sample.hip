@@ -22,10 +22,11 @@ namespace sna {
 typedef unsigned long long u64;
 constexpr int SM_BINS = 2048;      // values of a digit; distances told apart; runs of a row, at most
 constexpr int SM_SMALL = 4096;     // logits of a row that one block takes in one launch
-constexpr int SM_LIST = 2048;      // logits at a row's cut
+constexpr int SM_LIST = 8192;      // logits at a row's cut
+constexpr int SM_HELD = 2048;      // of them that are held in registers
 constexpr int SM_MOST = SM_LIST / 2;             // top_k up to which a row's list is to hold all that it keeps
 constexpr int SM_RUN = 512;        // logits of a wave's turn, and of a sum
-constexpr int SM_STAGE = 1024;     // logits at the cut that a block writes out at once
+constexpr int SM_STAGE = 2048;     // logits at the cut that a block writes out at once
 constexpr int SM_T = 512;          // threads of the blocks that share a row
 constexpr int SM_FINAL = 512;      // of the one that ends it
 
@@ -84,6 +85,12 @@ struct Row {                       // of logits, and what is wanted of it
     top = top32;
     return x > -INFINITY;
   }
+  // and the smallest: a row of less than 4 temperatures has its 256 even steps over what it spans
+  __device__ __forceinline__ bool begin(float2 ends) {
+    const bool some = begin(ends.x);
+    near = fmaxf(near, fminf(2.f / (ends.x - ends.y), 1e38f));       // where all are the same, any will do
+    return some;
+  }
   __device__ __forceinline__ float seen(float x) const { return infinite ? x == INFINITY ? 0.f : -INFINITY : taken(x); }
   // Where it stands among the row's
   __device__ __forceinline__ u64 place(float x, int i) const { return (u64)(falling(x) >> spare) << bits | (unsigned)i; }
@@ -94,7 +101,7 @@ struct Row {                       // of logits, and what is wanted of it
   __device__ __forceinline__ double kept(float x, int i) const {       // the weight of one that is left
     return x > -INFINITY && place(x, i) <= cut ? left(weight(x)) : 0.0;
   }
-  // Rises as x falls, in SM_BINS steps: 256 even ones of 1 / 64 of the temperature, then twice as wide from 4 temperatures on, and
+  // Rises as x falls, in SM_BINS steps: 256 even ones of 1 / 64 of the temperature (see begin), then twice as wide from 4 temperatures on, and
   // again from 12, 28, .. on: what a number from 2 on has of bits behind the leading ones
   __device__ __forceinline__ int distance(float x) const { return (int)min(far(x) >> 15, (unsigned)SM_BINS - 1); }
   __device__ __forceinline__ unsigned far(float x) const { return __float_as_uint(fmaf(top32 - x, near, 2.f)) & 0x3fffffff; }        // from 2 on: the exponent begins with zeros
@@ -517,7 +524,7 @@ __device__ __forceinline__ Kind kind_of(const Row& r) {
 }
 struct Work {                      // of a call
   RowWork* rows;                   // [n]
-  float* tops;                     // [n][parts]
+  float2* ends;                    // [n][parts]: the largest and the smallest but -inf
   u64* runs;                       // [n][runs]
   int parts, len, n_runs;          // blocks of a row, logits of one, sums of a row
 };
@@ -553,10 +560,13 @@ __device__ __forceinline__ void each_run(const SampleArgs& a, const Work& w, int
     i0 = i1;
   }
 }
-__device__ __forceinline__ float top_of(const Work& w, int row) {
-  float top = -INFINITY;
-  for (int p = threadIdx.x & 63; p < w.parts; p += 64) top = fmaxf(top, w.tops[row * w.parts + p]);
-  return max_of_wave(top);
+__device__ __forceinline__ float2 ends_of(const Work& w, int row) {
+  float2 ends = {-INFINITY, INFINITY};
+  for (int p = threadIdx.x & 63; p < w.parts; p += 64) {
+    const float2 x = w.ends[row * w.parts + p];
+    ends = float2{fmaxf(ends.x, x.x), fminf(ends.y, x.y)};
+  }
+  return float2{max_of_wave(ends.x), -max_of_wave(-ends.y)};
 }
 
 template <class X>
@@ -570,15 +580,20 @@ __global__ __launch_bounds__(SM_T) void sample_top_kernel(const SampleArgs a, co
       rw.counts[i] = 0;
     }
   if (part == 0 && threadIdx.x == 0) rw.listed = 0;
-  float top = -INFINITY;
+  float top = -INFINITY, low = INFINITY;
   Row r;
   r.infinite = false;
   each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
+    for (int e = 0; e < 8; ++e) {
+      top = fmaxf(top, x[e]);
+      low = fminf(low, x[e] > -INFINITY ? x[e] : INFINITY);
+    }
   });
   top = max_of_block(lds, top);
-  if (threadIdx.x == 0) w.tops[blockIdx.x] = top;
+  __syncthreads();
+  low = -max_of_block(lds, -low);
+  if (threadIdx.x == 0) w.ends[blockIdx.x] = float2{top, low};
 }
 
 template <class X>
@@ -589,7 +604,7 @@ __global__ __launch_bounds__(SM_T) void sample_sums_kernel(const SampleArgs a, c
   Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
   if (kind != CUT_COUNT && kind != CUT_WEIGHT) return;
-  if (!r.begin(top_of(w, row))) return;
+  if (!r.begin(ends_of(w, row))) return;
   RowWork& rw = w.rows[row];
   for (int i = threadIdx.x; i < SM_BINS; i += SM_T) {
     if (kind == CUT_COUNT) counts[i] = 0;
@@ -640,7 +655,7 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
   Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
   if (kind == CUT_SLOWLY) return;
-  if (!r.begin(top_of(w, row))) return;
+  if (!r.begin(ends_of(w, row))) return;
   RowWork& rw = w.rows[row];
   int at = SM_BINS;
   u64 want;
@@ -710,7 +725,7 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
 
 template <class X>
 __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs a, const Work w) {
-  constexpr int N = SM_LIST / SM_FINAL;
+  constexpr int N = SM_HELD / SM_FINAL;
   __shared__ SampleLds<SM_FINAL> lds;
   const int tid = threadIdx.x, row = blockIdx.x;
   const X* logits = (const X*)a.logits + row * a.stride;
@@ -730,7 +745,7 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   }
   const unsigned listed = rw.listed;
   __syncthreads();
-  if (!r.begin(top_of(w, row))) {                                    // nothing to draw from
+  if (!r.begin(ends_of(w, row))) {                                    // nothing to draw from
     if (tid == 0) {
       a.tokens[row] = -1;
       rw.cut = 0;
@@ -744,6 +759,12 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   if (kind == CUT_SLOWLY || m > SM_LIST) {
     const auto each = [&](const auto& f) {
       for (int i = tid; i < a.V; i += SM_FINAL) f(r.seen(logit(logits, i)), i);
+    };
+    cut_row(lds, r, each);
+    token = draw_row(lds, a, row, r, total, each);
+  } else if (kind == CUT_COUNT && m > SM_HELD) {
+    const auto each = [&](const auto& f) {
+      for (unsigned i = tid; i < m; i += SM_FINAL) f(__uint_as_float((unsigned)(rw.list[i] >> 32)), (int)rw.list[i]);
     };
     cut_row(lds, r, each);
     token = draw_row(lds, a, row, r, total, each);
@@ -770,12 +791,21 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
       if (kind == CUT_WEIGHT) {
         u64 want, p[N], s[N];
         cut_at(lds, r, kind, want, [&](int j) { return sums[j]; });
+        if (m > SM_HELD) {
+          r.cut = select(lds, 32 - r.spare + r.bits, want, [&](const auto& f) {
+            for (unsigned i = tid; i < m; i += SM_FINAL) {
+              const float l = __uint_as_float((unsigned)(rw.list[i] >> 32));
+              f(r.place(l, (int)rw.list[i]), r.steps(r.weight(l)));
+            }
+          });
+        } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          p[j] = r.place(x[j], at[j]);
-          s[j] = x[j] > -INFINITY ? r.steps(r.weight(x[j])) : 0;
+          for (int j = 0; j < N; ++j) {
+            p[j] = r.place(x[j], at[j]);
+            s[j] = x[j] > -INFINITY ? r.steps(r.weight(x[j])) : 0;
+          }
+          r.cut = select_held(lds, want, p, s);
         }
-        r.cut = select_held(lds, want, p, s);
       }
       // the runs' sums with what is kept of the list; then the run that the draw falls into
       __syncthreads();
@@ -786,6 +816,10 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
       for (int j = 0; j < N; ++j) {
         const u64 s = r.steps(r.kept(x[j], at[j]));
         if (s) atomicAdd(&lds.sums[at[j] / SM_RUN], s);
+      }
+      for (unsigned i = SM_HELD + tid; i < m; i += SM_FINAL) {
+        const u64 s = r.steps(r.kept(__uint_as_float((unsigned)(rw.list[i] >> 32)), (int)rw.list[i]));
+        if (s) atomicAdd(&lds.sums[(int)rw.list[i] / SM_RUN], s);
       }
       __syncthreads();
       const Crossing c = crossing(lds, [&](u64 all) { return drawn_at(a, row, all); });
@@ -806,7 +840,7 @@ template <class X>
 __global__ __launch_bounds__(SM_T) void sample_probs_kernel(const SampleArgs a, const Work w) {
   const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts;
   Row r = row_of<X>(a, row);
-  r.begin(top_of(w, row));
+  r.begin(ends_of(w, row));
   r.cut = w.rows[row].cut;
   const double f = w.rows[row].share;
   float* out = a.probs + row * a.p_stride;
@@ -835,13 +869,13 @@ static Work work_of(int n, int V, void* at) {
   w.n_runs = (V + SM_RUN - 1) / SM_RUN;
   w.rows = (RowWork*)at;
   w.runs = (u64*)(w.rows + n);
-  w.tops = (float*)(w.runs + (long)n * w.n_runs);
+  w.ends = (float2*)(w.runs + (long)n * w.n_runs);
   return w;
 }
 size_t sample_workspace(int n, int vocab, int) {
   if (vocab <= SM_SMALL) return 0;
   const Work w = work_of(n, vocab, nullptr);
-  return n * (sizeof(RowWork) + w.n_runs * sizeof(u64) + w.parts * sizeof(float));
+  return n * (sizeof(RowWork) + w.n_runs * sizeof(u64) + w.parts * sizeof(float2));
 }
 
 template <class X>

@@ -152,6 +152,16 @@ def test_a_large_nucleus_and_outliers():
         checked(logits, u, close=True, **settings)
 
 
+@pytest.mark.parametrize("dtype,V,scale", [("fp32", 50257, 0.05), ("fp32", 131072, 0.02), ("bf16", 16385, 0.3), ("bf16", 131072, 1.0), ("fp32", 30000, 3.0), ("fp16", 65536, 1e-4)])
+def test_lists_of_every_length(dtype, V, scale):
+    """Cuts whose lists a block holds, reads twice, or does not have: large counts, flat rows, ties by the thousand, one logit far below."""
+    logits, u = logits_of(3, V, dtype, V + 7, scale)
+    logits[2, 5] = -60000.0
+    for settings in ({"top_p": 0.9}, {"top_p": 0.4, "min_p": 0.9}, {"top_k": 1500}, {"top_k": 2048}, {"top_k": 2049, "top_p": 0.5}, {"top_k": 4096}, {"top_k": 4097}, {"top_k": 12000, "top_p": 0.7},
+                     {"top_k": 3500, "top_p": 0.999, "min_p": 0.5}, {"temperature": 50.0, "top_p": 0.97}, {"temperature": 0.0}):
+        checked(logits, u, close=True, **settings)
+
+
 def test_the_borders_of_the_draw():
     """u of 0 gives the first token that is kept, the largest u the last; what lies outside [0, 1) counts as its end."""
     logits, _ = logits_of(6, 5000, "fp32", 3)
