@@ -8,11 +8,13 @@
 // the index): sums by digit in LDS, the digit that the wanted sum falls into, then the same among what has that digit.
 // Rows of up to 4096 logits take one launch, a block a row with its logits in registers: 1000 of them, top_k 50 and top_p 0.9, 8.5 us,
 // which a dozen barriers in a row make, and the launch.  Longer ones are read three times, by as many blocks as fill the chip: for the
-// largest; for counts or weights by distance from it (where a row is cut); and for what lies at the cut, a short list, and the sums of
-// what is kept for certain, by runs of 512.  Then one block a row has the list and the sums.  128 rows of 131072 fp32, top_p 0.95 (a third
-// of each is kept): 11.8, 19.7, 26.6 and 10.4 us, 65 in a loop of calls.  The first is bound by memory (5.7 TB/s); the next two by vector
-// instructions, 32 and 38 a logit, at work 84 and 69 % of the cycles, of which a weight is 20; the last by its round trips.
+// largest; for counts or weights by distance from it (where a row is cut); and for what lies at the cut, a list, mostly short, and the
+// sums of what is kept for certain, by runs of 512.  Then one block a row has the list and the sums.  128 rows of 131072 fp32, top_p 0.95 (a third
+// of each is kept): 12, 20, 27 and 11 us, 66 in a loop of calls.  The first is bound by memory (5.5 TB/s); the next two by vector
+// instructions, 32 and 38 a logit, at work 84 and 71 % of the cycles, of which a weight is 20; the last by its round trips.  Where one
+// logit is kept, the first reading finds it: 17 us, and 44 by the others.
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "paged.h"
@@ -85,7 +87,7 @@ struct Row {                       // of logits, and what is wanted of it
     top = top32;
     return x > -INFINITY;
   }
-  // and the smallest: a row of less than 4 temperatures has its 256 even steps over what it spans
+  // and the smallest, of some: a row that spans less than 4 temperatures has its 256 even steps over that
   __device__ __forceinline__ bool begin(float2 ends) {
     const bool some = begin(ends.x);
     near = fmaxf(near, fminf(2.f / (ends.x - ends.y), 1e38f));       // where all are the same, any will do
@@ -517,15 +519,17 @@ struct RowWork {
   double share;
 };
 // How a row is cut
-enum Kind { CUT_NONE, CUT_COUNT, CUT_WEIGHT, CUT_SLOWLY };           // all that is kept in the list; the list at the cut; digit by digit of the whole row
+enum Kind { CUT_NONE, CUT_BEST, CUT_COUNT, CUT_WEIGHT, CUT_SLOWLY }; // to the first of the largest; all that is kept in the list; the list at the cut; digit by digit of the whole row
 __device__ __forceinline__ Kind kind_of(const Row& r) {
+  if (r.top_k == 1) return CUT_BEST;
   if (r.top_k) return r.top_k <= SM_MOST ? CUT_COUNT : CUT_SLOWLY;
   return r.top_p < 1.f ? CUT_WEIGHT : CUT_NONE;
 }
 struct Work {                      // of a call
   RowWork* rows;                   // [n]
-  float2* ends;                    // [n][parts]: the largest and the smallest but -inf
+  float2* ends;                    // [n][parts]: the largest, and of every eighth the smallest but -inf
   u64* runs;                       // [n][runs]
+  int* best;                       // [n][parts]: the first of the largest, for rows of which no other is kept
   int parts, len, n_runs;          // blocks of a row, logits of one, sums of a row
 };
 
@@ -581,19 +585,29 @@ __global__ __launch_bounds__(SM_T) void sample_top_kernel(const SampleArgs a, co
     }
   if (part == 0 && threadIdx.x == 0) rw.listed = 0;
   float top = -INFINITY, low = INFINITY;
-  Row r;
-  r.infinite = false;
-  each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int) {
+  int at = INT_MAX;                                                  // the first of the lane's largest
+  const Row r = row_of<X>(a, row);
+  const bool best = kind_of(r) == CUT_BEST;
+  each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int) {
+    float most = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      top = fmaxf(top, x[e]);
-      low = fminf(low, x[e] > -INFINITY ? x[e] : INFINITY);
-    }
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, x[e]);
+    low = fminf(low, x[0] > -INFINITY ? x[0] : INFINITY);
+    if (best && most > top)
+#pragma unroll
+      for (int e = 7; e >= 0; --e) at = x[e] == most ? i + e : at;
+    top = fmaxf(top, most);
   });
+  const float mine = top;
+  if (threadIdx.x == 0) lds.digit = INT_MAX;
   top = max_of_block(lds, top);
   __syncthreads();
+  if (best && mine == top) atomicMin(&lds.digit, at);
   low = -max_of_block(lds, -low);
-  if (threadIdx.x == 0) w.ends[blockIdx.x] = float2{top, low};
+  if (threadIdx.x == 0) {
+    w.ends[blockIdx.x] = float2{top, low};
+    if (best) w.best[blockIdx.x] = lds.digit;
+  }
 }
 
 template <class X>
@@ -654,7 +668,7 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
   const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts, tid = threadIdx.x, lane = tid & 63;
   Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
-  if (kind == CUT_SLOWLY) return;
+  if (kind == CUT_SLOWLY || kind == CUT_BEST) return;
   if (!r.begin(ends_of(w, row))) return;
   RowWork& rw = w.rows[row];
   int at = SM_BINS;
@@ -745,7 +759,8 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   }
   const unsigned listed = rw.listed;
   __syncthreads();
-  if (!r.begin(ends_of(w, row))) {                                    // nothing to draw from
+  const float2 ends = ends_of(w, row);
+  if (!r.begin(ends)) {                                              // nothing to draw from
     if (tid == 0) {
       a.tokens[row] = -1;
       rw.cut = 0;
@@ -756,7 +771,14 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   u64 total;
   int token;
   const unsigned m = kind == CUT_COUNT || kind == CUT_WEIGHT ? listed : 0;
-  if (kind == CUT_SLOWLY || m > SM_LIST) {
+  if (kind == CUT_BEST) {
+    u64 first = INT_MAX;                                             // the complement of the largest is the smallest
+    for (int p = tid & 63; p < w.parts; p += 64)
+      if (w.ends[row * w.parts + p].x == ends.x) first = min(first, (u64)w.best[row * w.parts + p]);
+    token = (int)~last_lane(scan_of(~first, 0, Most()));
+    r.cut = r.place(r.top32, token);
+    total = r.steps(1.0);
+  } else if (kind == CUT_SLOWLY || m > SM_LIST) {
     const auto each = [&](const auto& f) {
       for (int i = tid; i < a.V; i += SM_FINAL) f(r.seen(logit(logits, i)), i);
     };
@@ -870,12 +892,13 @@ static Work work_of(int n, int V, void* at) {
   w.rows = (RowWork*)at;
   w.runs = (u64*)(w.rows + n);
   w.ends = (float2*)(w.runs + (long)n * w.n_runs);
+  w.best = (int*)(w.ends + (long)n * w.parts);
   return w;
 }
 size_t sample_workspace(int n, int vocab, int) {
   if (vocab <= SM_SMALL) return 0;
   const Work w = work_of(n, vocab, nullptr);
-  return n * (sizeof(RowWork) + w.n_runs * sizeof(u64) + w.parts * sizeof(float2));
+  return n * (sizeof(RowWork) + w.n_runs * sizeof(u64) + w.parts * (sizeof(float2) + sizeof(int)));
 }
 
 template <class X>
@@ -890,9 +913,11 @@ static hipError_t sample_of(const SampleArgs& a, hipStream_t s) {
   const long blocks = (long)a.n * w.parts;
   if (!fits_a_launch(blocks, SM_T) || !fits_a_launch(a.n, SM_FINAL)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(SM_T);
+  // without settings of each row: one logit that is kept needs the first reading only
+  const bool best = (!a.temperature_of && a.temperature == 0.f) || (!a.top_k_of && a.top_k == 1);
   hipLaunchKernelGGL(sample_top_kernel<X>, grid, block, 0, s, a, w);
-  if (a.top_k_of || a.top_p_of || a.temperature_of || a.top_k || a.top_p < 1.f || a.temperature == 0.f) hipLaunchKernelGGL(sample_sums_kernel<X>, grid, block, 0, s, a, w);
-  hipLaunchKernelGGL(sample_list_kernel<X>, grid, block, 0, s, a, w);
+  if (!best && (a.top_k_of || a.top_p_of || a.temperature_of || a.top_k || a.top_p < 1.f)) hipLaunchKernelGGL(sample_sums_kernel<X>, grid, block, 0, s, a, w);
+  if (!best) hipLaunchKernelGGL(sample_list_kernel<X>, grid, block, 0, s, a, w);
   hipLaunchKernelGGL(sample_draw_kernel<X>, dim3(a.n), dim3(SM_FINAL), 0, s, a, w);
   if (a.probs) hipLaunchKernelGGL(sample_probs_kernel<X>, grid, block, 0, s, a, w);
   return hipGetLastError();

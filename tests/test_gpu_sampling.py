@@ -162,6 +162,30 @@ def test_lists_of_every_length(dtype, V, scale):
         checked(logits, u, close=True, **settings)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n,V", [(70, 4097), (9, 50257), (3, 131072), (1, 300001)])
+def test_the_best(dtype, n, V):
+    """One logit that is kept: the first of several, anywhere in a row, behind NaN, infinite, both zeros, alone, or none."""
+    logits, u = logits_of(n, V, dtype, V + n, 0.5)
+    g = torch.Generator().manual_seed(3)
+    for row in range(n):
+        at = torch.randint(0, V, (3,), generator=g).tolist()
+        logits[row, at] = [20.0, math.inf, 19.0, 20.0][row % 4]
+        if row % 5 == 1:
+            logits[row] = -math.inf
+            logits[row, V - 1 - row] = -7.0
+        if row % 5 == 2:
+            logits[row, : V // 2] = math.nan
+            logits[row, V // 2:] = torch.where(torch.arange(V - V // 2, device="cuda") % 3 == 2, 0.0, -0.0).to(logits.dtype)
+        if row % 7 == 6:
+            logits[row] = [-math.inf, math.nan][row % 2]
+    per_row = torch.where(torch.arange(n) % 3 == 0, 0.0, -1.0)
+    for settings in ({"temperature": 0.0}, {"top_k": 1}, {"temperature": 0.0, "top_p": 0.3, "min_p": 1.0, "top_k": 9}, {"top_k": 1, "temperature": 3.0, "top_p": 0.0}):
+        tokens, _ = checked(logits, u, close=True, **settings)
+        alike = sna.sample_tokens(logits, u.cuda(), temperature=per_row.cuda(), top_k=torch.full((n,), 40, dtype=torch.int32, device="cuda"))
+        assert alike.tolist() == tokens.tolist()
+
+
 def test_the_borders_of_the_draw():
     """u of 0 gives the first token that is kept, the largest u the last; what lies outside [0, 1) counts as its end."""
     logits, _ = logits_of(6, 5000, "fp32", 3)
