@@ -184,9 +184,9 @@ def main():
     model = Decoder(pages=a.seqs * max(1, a.samples) * -(-(a.prompt + a.tokens + max(a.drafts, tree)) // PAGE))
     g = torch.Generator().manual_seed(1)
     prompts = [torch.randint(0, model.vocab, (a.prompt - i % 7,), generator=g).tolist() for i in range(a.seqs)]
-    runs = [(f"{drafts} drafts", 1, lambda n, d=drafts: generate(model, prompts, n, d, a.depth)) for drafts in (0, a.drafts)]
-    runs.append((f"trees of {a.tree}", a.samples, lambda n: generate_tree(model, prompts, n, widths, a.depth, a.samples, top_p=0.95)))
-    for name, samples, run in runs:
+    runs = [(f"{drafts} drafts", "drafts accepted", 1, lambda n, d=drafts: generate(model, prompts, n, d, a.depth)) for drafts in (0, a.drafts)]
+    runs.append((f"trees of {a.tree}", "drafted places taken", a.samples, lambda n: generate_tree(model, prompts, n, widths, a.depth, a.samples, top_p=0.95)))
+    for name, what, samples, run in runs:
         run(8)
         torch.cuda.synchronize()
         t = time.perf_counter()
@@ -194,7 +194,7 @@ def main():
         torch.cuda.synchronize()
         t = time.perf_counter() - t
         n = sum(len(d) - len(prompts[i // samples]) for i, d in enumerate(done))
-        print(f"{name}: {n} tokens of {len(done)} sequences in {rounds} rounds, {n / t:.0f} tokens/s, {100 * share:.0f} % of the drafted places taken")
+        print(f"{name}: {n} tokens of {len(done)} sequences in {rounds} rounds, {n / t:.0f} tokens/s, {100 * share:.0f} % of the {what}")
 
 
 if __name__ == "__main__":
