@@ -15,7 +15,7 @@ namespace sna {
 template <class T, int D, int W>
 __global__ __launch_bounds__(64 * W, 2) void tree_split_kernel(const PagedAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) PrefillLds<D> lds;
-  const int planes = gridDim.x / a.blocks, group = blockIdx.x / (8 * planes), in = blockIdx.x % (8 * planes), plane = in >> 3, p = group * 8 + (in & 7);
+  const int planes = gridDim.x / a.blocks, side = min(a.blocks, 8), in = blockIdx.x % (side * planes), plane = in / side, p = blockIdx.x / (side * planes) * side + in % side;
   First* first = (First*)a.parts;
   const long part_size = part_floats(a.rows_cap, D);
   float* parts = (float*)(first + a.blocks * planes) + 2 * a.blocks * plane * part_size;

@@ -76,17 +76,17 @@ struct AttnPlan {
   size_t parts, chunk_parts;       // bytes of the workspace, for either
 };
 inline size_t parts_of(int blocks, int rows, int head_dim) { return (blocks * (sizeof(First) + 2 * part_floats(rows, head_dim) * sizeof(float)) + 255) & ~(size_t)255; }
-inline AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
+inline AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim, bool few_of_tree = false) {
   const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len;
   const bool equal = (long)n_seqs * max_new == n_tokens;               // all sequences bring max_new tokens
   AttnPlan p = {};
-  if (rows <= 64 || (long)n_tokens * group * kv_heads * keys <= (equal && head_dim == 128 ? kFewScoresEqual : kFewScores)) {
+  if (few_of_tree || rows <= 64 || (long)n_tokens * group * kv_heads * keys <= (equal && head_dim == 128 ? kFewScoresEqual : kFewScores)) {
     const auto units_of = [&](int mb) { return (n_tokens / std::max(16 * mb / group, 1) + n_seqs) * (long)kv_heads; };
     p.mb = rows <= 16 ? 1 : group <= 32 ? 2 : 4;
     // Chunks with heads of 64: 64 rows a block instead of 32, which takes 1.45 times as long, where that saves rounds of a block on
     // each CU (500 tokens and 7 single ones, 4 heads: 15.6 and 17.4 us; 600 of 8 sequences and 56: 31 and 44; 500 of 12 heads: 20.4
     // and 16.9).  With heads of 128 there is no second block on a CU then, and 32 rows are faster throughout.
-    if (head_dim == 64 && rows > 64 && p.mb == 2 && (units_of(4) + 255) / 256 * 145 < (units_of(2) + 255) / 256 * 100) p.mb = 4;
+    if (!few_of_tree && head_dim == 64 && rows > 64 && p.mb == 2 && (units_of(4) + 255) / 256 * 145 < (units_of(2) + 255) / 256 * 100) p.mb = 4;
     p.most = max_new;
     const long units = units_of(p.mb), room = 256 * blocks_of(head_dim, p.mb), kt = tile_keys(head_dim, p.mb), tiles = (keys + kt - 1) / kt;
     p.waves = blocks_of(head_dim, p.mb) == 2 && units <= 256 && tiles * kt > 512 ? 8 : 4;
@@ -111,23 +111,30 @@ inline AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
 // Up to kTreeFew rows a key / value head the few-rows kernel takes them in one tile of rows, and up to twice that in two where the keys
 // are few: the many-rows kernel has 20 us before and behind its turns, if its keys are shared out.  In us, 32 heads over 8 of 128: 16
 // tokens over 8192 keys 22 (few rows) and 37; 16 trees of up to 12 over up to 4096 57 and 46, 64 of up to 13 over up to 2048 99 and 97.
-// More rows are walked by blocks of kTreeRows, whole, or their keys shared out over kTreeBlocks (two on a CU; 256 took 64 us for 58, 180
-// for 127), whichever a count of the turns says is sooner, a turn being 2 us, 1.24 with heads of 64, and three quarters where most CUs have
-// one block.
+// So are more rows where the step has few scores (kTreeScores, as for chunks): 32 tokens over 600 keys, 28 heads over 4, 11 to 12 (few rows)
+// and 21.5; 64 x 32 over 600, 8 heads over 1 of 64 (10 M), 27 and 16.5.
+// The rest is walked by blocks of kTreeRows, whole, or their keys shared out over kTreeBlocks (two on a CU; 256 took 64 us for 58, 180
+// for 127; one tree of 128 tokens over 30000 keys, 32 heads over 1, 87 and 606), whichever a count of the turns says is sooner, a turn
+// being 2 us, 1.24 with heads of 64, and three quarters where most CUs have one block; whole where blocks come in many rounds anyway.
 constexpr int kTreeFew = 32, kTreeRows = 128, kTreeBlocks = 512, kTreeLeast = 6, kTreeTurns = 2048;
+constexpr long kTreeScores = 8l << 20;
 inline int tree_planes(int max_new, int group) { return (max_new + kTreeRows / group - 1) / (kTreeRows / group); }
+// Blocks that share the keys, of each plane: eights, which go to the XCDs by turns, where there are as many
+inline int tree_shares(int planes) { return kTreeBlocks / planes < 8 ? kTreeBlocks / planes : kTreeBlocks / planes & ~7; }
 inline AttnPlan plan_of_tree(int n_seqs, int n_tokens, int kv_heads, int group, int max_new, int max_len, int window, int head_dim) {
   const long rows = (long)max_new * group, keys = window ? std::min((long)max_len, (long)window + max_new) : max_len, tiles = (keys + PF_K - 1) / PF_K;
   const long turns = (long)n_seqs * kv_heads * tiles * (n_seqs == 1 ? 10 : 7) / 10;    // sequences of 0.7 of the longest on average
-  if (rows <= kTreeFew || (rows <= 2 * kTreeFew && group <= kTreeFew && turns < kTreeTurns)) return plan_of(n_seqs, n_tokens, kv_heads, group, max_new, max_len, window, head_dim);
+  const long scores = (long)n_tokens * group * kv_heads * keys;
+  if (group <= kTreeFew && (rows <= kTreeFew || (rows <= 2 * kTreeFew && turns < kTreeTurns) || scores <= kTreeScores))
+    return plan_of(n_seqs, n_tokens, kv_heads, group, max_new, max_len, window, head_dim, true);
   AttnPlan p = {};
   p.most = max_new;
-  const int planes = tree_planes(max_new, group), shares = kTreeBlocks / planes & ~7;
+  const int planes = tree_planes(max_new, group), shares = tree_shares(planes);
   const long units = (n_tokens / (kTreeRows / group) + n_seqs) * (long)kv_heads;
   const double turn = head_dim == 128 ? 2.0 : 1.24;
   const double whole = (double)((units + kTreeBlocks - 1) / kTreeBlocks * tiles) * turn * (units <= 256 ? 0.75 : 1.0);
   const double shared = shares ? std::max((double)turns / shares, (double)kTreeLeast) * turn + 20.0 : 1e30;
-  if (planes <= 16 && shared < whole && (long)n_seqs * kv_heads * (tiles + 2) < 1l << 30) {
+  if (shares > 1 && units < 8 * kTreeBlocks && shared < whole && (long)n_seqs * kv_heads * (tiles + 2) < 1l << 30) {
     p.blocks = shares;
     p.parts = parts_of(shares * planes, std::min(kTreeRows / group, max_new) * group, head_dim);
   }

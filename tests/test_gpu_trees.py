@@ -60,6 +60,17 @@ def test_tree_attention_over_long_caches(heads, page, seqs, window):
     within(attend(s, window), want, err, "out")
 
 
+@pytest.mark.parametrize("heads,page,seqs,window,kind", [
+    ((32, 1, 128), 16, [(9000, 128)], 0, "tree"), ((32, 1, 64), 64, [(5000, 300), (2100, 17), (300, 300)], 0, "random"), ((28, 4, 128), 16, [(7000, 512)], 2000, "tree"),
+    ((32, 1, 128), 16, [(600, 13), (90, 2), (333, 40)], 0, "random"), ((28, 4, 128), 16, [(600, 100)], 0, "empty"), ((8, 1, 64), 32, [(4000, 400)], 0, "chain"),
+    ((8, 1, 64), 16, [(500, 500), (40, 7), (0, 0)], 0, "tree"), ((16, 16, 64), 16, [(700, 90), (650, 33)], 100, "random"), ((64, 1, 128), 16, [(20000, 160)], 0, "random")])
+def test_many_rows_of_few_heads(heads, page, seqs, window, kind):
+    """Planes by the dozen over few shares of the keys, and steps small enough for many tiles of few rows."""
+    s = tree.make(seqs, *heads, page, torch.bfloat16, seed=31, kind=kind)
+    want, err = tree.attention(s, window)
+    within(attend(s, window), want, err, "out")
+
+
 @pytest.mark.parametrize("i", range(len(launches.STEPS)))
 def test_every_launch(i):
     """The steps that get each launch of attention, as trees of random masks over all of a chunk, 4096 tokens at most."""

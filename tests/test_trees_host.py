@@ -55,10 +55,12 @@ def test_launches_of_trees():
         for length in (100, 5000, 50000):
             assert bytes_of(3, nodes, length) == causal(3, nodes, length)
     assert bytes_of(16, 30, 300) == 0 and bytes_of(1, 60, 300) == 0
-    for nodes, planes in ((32, 1), (33, 2), (77, 3), (500, 16)):
+    for nodes, planes in ((32, 1), (33, 2), (77, 3), (500, 16), (600, 19)):
         shares = 512 // planes // 8 * 8
-        assert bytes_of(4, nodes, 60000, 8) == -(-shares * planes * (16 + 2 * 4 * (min(nodes, 32) * 4 * 66)) // 256) * 256, nodes
-    assert bytes_of(4, 600, 60000, 10) == 0                                          # rows enough to fill the chip
+        assert bytes_of(4, nodes, 60000, 10) == -(-shares * planes * (16 + 2 * 4 * (min(nodes, 32) * 4 * 66)) // 256) * 256, nodes
+    assert bytes_of(1, 2100, 60000, 60) == -(-7 * 66 * (16 + 2 * 4 * (32 * 4 * 66)) // 256) * 256     # fewer shares than there are XCDs
+    assert bytes_of(64, 600, 60000, 10) == 0                                         # rows enough to fill the chip
+    assert bytes_of(1, 40, 5000) == causal(1, 40, 5000) > 0                          # little to do: blocks of few rows
     assert bytes_of(4, 77, 60000, 2, 100) == 0                                       # few keys in the window
 
 
