@@ -172,23 +172,47 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, PrefillLds<D>
         for (int i = 0; i < 16; ++i) o[j][i] *= keep;
     }
     const float from = -ref.from();
-    u32x4 p[4];
+    if constexpr (TREE) {
+      // What rounding leaves of the probabilities goes through a second product, so that a token is off by its own rounding alone, as in the
+      // few-rows kernel, and does not lose bits to how many others its step brings (rounded once: 1.39 times as much, 2.3e-3 of the norm
+      // instead of 1.7e-3 in bf16, 2.9e-4 instead of 2.1e-4 in fp16).  A third more of the matrix pipe's work and 96 vector instructions a
+      // turn: 77 tokens over 65519 keys, 32 heads over 8 of 128, 158 us instead of 127; 16 trees of up to 32 over up to 4096 67 and 60.
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      f32x8 e;
+      for (int s = 0; s < 4; ++s) {
+        f32x8 e;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + i], a.scale2, from));
-        sum += e[i];
+        for (int i = 0; i < 8; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + i], a.scale2, from));
+          sum += e[i];
+        }
+        const u32x4 p = to_16<T>(e), p_rest = to_16<T>(e - to_f32<T>(p));
+        u32x4 v[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) v[j] = *(const u32x4*)(vt + j * (32 * 128) + v_at[s ^ 2 * (j & 1)]);
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[j] = T::mma32(v[j], p, o[j]);
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[j] = T::mma32(v[j], p_rest, o[j]);
       }
-      // off by half a step of the operand type, which adds as much to the result as its own rounding (2.3e-3 of the norm in bf16
-      // instead of 1.7e-3); a second product with what the rounding leaves took 542 us instead of 396 for 4096 tokens over 8192
-      p[s] = to_16<T>(e);
+    } else {
+      u32x4 p[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        f32x8 e;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + i], a.scale2, from));
+          sum += e[i];
+        }
+        // off by half a step of the operand type, which adds as much to the result as its own rounding (2.3e-3 of the norm in bf16
+        // instead of 1.7e-3); a second product with what the rounding leaves took 542 us instead of 396 for 4096 tokens over 8192
+        p[s] = to_16<T>(e);
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[j] = T::mma32(*(const u32x4*)(vt + j * (32 * 128) + v_at[s ^ 2 * (j & 1)]), p[s], o[j]);
     }
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int j = 0; j < J; ++j) o[j] = T::mma32(*(const u32x4*)(vt + j * (32 * 128) + v_at[s ^ 2 * (j & 1)]), p[s], o[j]);
   }
   // The same again, at leisure and straight from the pages, for a wave whose sums are no numbers: see `Odd`
   float left = 0.f;                                                  // 0 x is 0 for a number, and only then
@@ -236,7 +260,7 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, PrefillLds<D>
           e[i] = __builtin_amdgcn_exp2f(fmaf(s ? sc[8 + i] : sc[i], a.scale2, from));
           sum += e[i];
         }
-        const u32x4 p = to_16<T>(e);
+        const u32x4 p = to_16<T>(e), p_rest = to_16<T>(e - to_f32<T>(p));
         const int key = key0 + 16 * s + 8 * hi;
         const char* vp = a.kv.v + in_pool(page(key)) * a.kv.vstride + (((long)h * D + l32) * ps + (key & (ps - 1))) * 2;
 #pragma unroll
@@ -246,6 +270,7 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, PrefillLds<D>
           for (int w = 0; w < 4; ++w)
             v[w] &= (key + 2 * w >= first && key + 2 * w <= last ? 0xffffu : 0u) | (key + 2 * w + 1 >= first && key + 2 * w + 1 <= last ? 0xffff0000u : 0u);
           o[j] = T::mma32(without_odd<T>(v), p, o[j]);
+          if (TREE) o[j] = T::mma32(without_odd<T>(v), p_rest, o[j]);
 #pragma unroll 1
           for (int kind = 0; kind < ODD_KINDS; ++kind) {
             f32x16 n;
