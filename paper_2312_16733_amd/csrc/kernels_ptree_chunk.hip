@@ -12,27 +12,27 @@ namespace sna {
 // 8 of 128: 66 us in five shares each, 58 in equal ones).  A tree of more than 128 rows has a block for each 128 of them on every
 // share: they walk the same keys side by side on one XCD, whose L2 reads them once.  Block j of a share is one of plane j, which has parts of
 // its own, plane after plane.
-template <class T, int D, int W>
-__global__ __launch_bounds__(64 * W, 2) void tree_split_kernel(const PagedAttnArgs a) {
-  __shared__ __attribute__((aligned(1024))) PrefillLds<D> lds;
-  const int planes = gridDim.x / a.blocks, side = min(a.blocks, 8), in = blockIdx.x % (side * planes), plane = in / side, p = blockIdx.x / (side * planes) * side + in % side;
-  First* first = (First*)a.parts;
-  const long part_size = part_floats(a.rows_cap, D);
-  float* parts = (float*)(first + a.blocks * planes) + 2 * a.blocks * plane * part_size;
-  const auto tiles = [&](const Seq& sq, int b) { return sq.n > a.most ? 0 : rows_of_sequence<PF_K, true>(a, sq, b, 0, a.max_new).tiles; };
-  walk_share(a, p, first + a.blocks * plane, a.max_new, [&](int b) { return tiles(sequence(a.s, b), b); },
-             [&](const Seq& sq, int b, int) {
-               RowTile r = rows_of_sequence<PF_K, true>(a, sq, b, plane * a.tpt, a.tpt);
-               r.tiles = tiles(sq, b);                               // also where the tree has no rows here
-               r.n = max(r.n, 0);
-               return r;
-             },
-             [&](const RowTile& r, int h, int t0, int t1, int part) { chunk_rows<T, D, W, true>(a, lds, r, h, t0, t1, 0, part < 0 ? nullptr : parts + part * part_size); });
-}
+template <class T, int D>
+struct TreeRows {
+  typedef PrefillLds<D> Lds;
+  static constexpr int W = 4, kBlocks = 2, kAlign = 1024, kDim = D;
+  static constexpr bool PLANES = true;
+  static __device__ __forceinline__ int tpt(const PagedAttnArgs& a) { return a.max_new; }
+  static __device__ __forceinline__ int tiles(const PagedAttnArgs& a, const Seq& sq, int b) { return sq.n > a.most ? 0 : rows_of_sequence<PF_K, true>(a, sq, b, 0, a.max_new).tiles; }
+  static __device__ __forceinline__ RowTile rows(const PagedAttnArgs& a, const Seq& sq, int b, int, int plane) {
+    RowTile r = rows_of_sequence<PF_K, true>(a, sq, b, plane * a.tpt, a.tpt);
+    r.tiles = tiles(a, sq, b);                                       // also where the tree has no rows here
+    r.n = max(r.n, 0);
+    return r;
+  }
+  static __device__ __forceinline__ void attend(const PagedAttnArgs& a, Lds& lds, const RowTile& r, int h, int t0, int t1, float* part) {
+    chunk_rows<T, D, W, true>(a, lds, r, h, t0, t1, 0, part);
+  }
+};
 
 template <class T, int D>
 static hipError_t tree_grid(PagedAttnArgs a, hipStream_t s) {
-  constexpr int W = 4;
+  constexpr int W = TreeRows<T, D>::W;
   a.tpt = 32 * W / a.G;
   if (a.parts) {
     if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
@@ -40,11 +40,11 @@ static hipError_t tree_grid(PagedAttnArgs a, hipStream_t s) {
     a.least = kTreeLeast;
     const int planes = tree_planes(a.max_new, a.G);
     const long pairs = (long)a.s.B * a.kv.heads;                     // (tree, head)s
-    hipLaunchKernelGGL((tree_split_kernel<T, D, W>), dim3(a.blocks * planes), dim3(64 * W), 0, s, a);
+    hipLaunchKernelGGL((paged_split_kernel<TreeRows<T, D>>), dim3(a.blocks * planes), dim3(64 * W), 0, s, a);
     // rows of a (sequence, head) that a block of the join takes at once, as many as its parts allow
     const int per = std::max(1, (int)(a.blocks / pairs)), at_once = std::max(1, 1024 / D / std::max(1, (per + 7) / 8));
     a.cut = 8 * pairs <= a.blocks ? (int)pairs : a.blocks;           // see paged_join_kernel
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.cut * planes, (a.rows_cap + at_once - 1) / at_once), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_join_kernel<T, D, true>), dim3(a.cut * planes, (a.rows_cap + at_once - 1) / at_once), dim3(256), 0, s, a);
     return hipGetLastError();
   }
   a.waves = W;

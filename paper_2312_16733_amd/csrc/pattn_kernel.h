@@ -430,8 +430,7 @@ __global__ __launch_bounds__(64 * W, blocks_of(D, MB)) void paged_rows_kernel(co
 
 // Tiles of keys of all tiles of a sequence's rows, for one head; none where the sequence has more rows than are taken here
 template <int KT, bool TREE>
-__device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) {
-  const Seq sq = sequence(a.s, b);
+__device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, const Seq& sq, int b) {
   if (sq.n > a.most) return 0;
   int n = 0;
   for (int i0 = 0; i0 < sq.n; i0 += a.tpt) n += rows_of_sequence<KT, TREE>(a, sq, b, i0, a.tpt).tiles;
@@ -440,10 +439,23 @@ __device__ __forceinline__ int tiles_of_sequence(const PagedAttnArgs& a, int b) 
 // The keys of all tiles of rows and heads, laid end to end, in equal shares over the blocks: what a share cuts off of a
 // (tile of rows, head) leaves as a part.  Part 2 p of block p continues what an earlier block began, part 2 p + 1 begins what
 // a later one continues; whoever begins one writes down in first[p] what it was and which block ends it.
-// tiles(sequence): of all its tiles of rows, of `tpt` tokens each; rows(sequence, number, first token): one of these;
-// attend(rows, head, first tile of their keys, end, part or -1: all of them are this block's)
-template <class Tiles, class Rows, class F>
-__device__ __forceinline__ void walk_share(const PagedAttnArgs& a, int p, First* first, int tpt, const Tiles& tiles, const Rows& rows, const F& attend) {
+// Of (FewRows, TreeRows): tiles of keys of all of a sequence's tiles of rows, of tpt tokens each; one of these; and the sums of some of its
+// keys, which leave as a part where there is one.  The walk is the kernel's own body and a flag tells the two apart: as a function of
+// closures it cost causal steps registers (four spilled with heads of 64) and, with the join's search, up to 0.6 us of 18.
+template <class Of>
+__global__ __launch_bounds__(64 * Of::W, Of::kBlocks) void paged_split_kernel(const PagedAttnArgs a) {
+  __shared__ __attribute__((aligned(Of::kAlign))) typename Of::Lds lds;
+  int p = blockIdx.x, plane = 0, planes = 1;
+  if constexpr (Of::PLANES) {
+    planes = gridDim.x / a.blocks;
+    const int side = min(a.blocks, 8), in = blockIdx.x % (side * planes);
+    plane = in / side;
+    p = blockIdx.x / (side * planes) * side + in % side;
+  }
+  First* first = (First*)a.parts + plane * a.blocks;
+  float* parts = (float*)((First*)a.parts + a.blocks * planes);
+  const long part_size = part_floats(a.rows_cap, Of::kDim);
+  if constexpr (Of::PLANES) parts += 2 * a.blocks * plane * part_size;
   const int lane = threadIdx.x & 63, heads = a.kv.heads;
   // this share's first sequence: every wave sums the tiles of all, 64 runs of sequences at a time
   // (the host has seen to it that all of them fit 31 bits)
@@ -451,7 +463,7 @@ __device__ __forceinline__ void walk_share(const PagedAttnArgs& a, int p, First*
   for (bool top = true;; top = false) {
     const int per = (count + 63) >> 6, b0 = lo + lane * per, b1 = min(lo + count, b0 + per);
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles(b);
+    for (int b = b0; b < b1; ++b) mine += Of::tiles(a, sequence(a.s, b), b);
     int up = mine;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
@@ -476,12 +488,12 @@ __device__ __forceinline__ void walk_share(const PagedAttnArgs& a, int p, First*
   // its first tile of rows, head and tile of keys
   int b = uniform(lo), i0 = 0;
   Seq sq = uniform(sequence(a.s, b));
-  RowTile r = rows(sq, b, 0);
+  RowTile r = Of::rows(a, sq, b, 0, plane);
   int rel = x - before * heads;
-  while (rel >= r.tiles * heads && i0 + tpt < sq.n) {
+  while (rel >= r.tiles * heads && i0 + Of::tpt(a) < sq.n) {
     rel -= r.tiles * heads;
-    i0 += tpt;
-    r = rows(sq, b, i0);
+    i0 += Of::tpt(a);
+    r = Of::rows(a, sq, b, i0, plane);
   }
   int h = clamped(rel / max(r.tiles, 1), 0, heads - 1), t = clamped(rel - h * r.tiles, 0, max(r.tiles - 1, 0)), left = share, at = 0;     // at: tiles done, of this share
   bool begun = false;
@@ -492,14 +504,14 @@ __device__ __forceinline__ void walk_share(const PagedAttnArgs& a, int p, First*
       begun = true;
       if (threadIdx.x == 0) first[p] = First{r.row0, r.n, h, min((x + at + r.tiles - 1) / share, a.blocks - 1)};
     }
-    if (r.n > 0) attend(r, h, r.t0 + t, r.t0 + t + n, whole ? -1 : 2 * p + (t == 0));
+    if (r.n > 0) Of::attend(a, lds, r, h, r.t0 + t, r.t0 + t + n, whole ? nullptr : parts + (2 * p + (t == 0)) * part_size);
     left -= n;
     at += n;
     t = 0;
     if (left == 0) break;
     if (++h == heads) {
       h = 0;
-      i0 += tpt;
+      i0 += Of::tpt(a);
       if (i0 >= sq.n) {
         i0 = 0;
         do {
@@ -508,25 +520,24 @@ __device__ __forceinline__ void walk_share(const PagedAttnArgs& a, int p, First*
         } while (sq.n <= 0 || sq.n > a.most);
         if (b >= a.s.B) break;
       }
-      r = rows(sq, b, i0);
+      r = Of::rows(a, sq, b, i0, plane);
     }
     __syncthreads();                                                 // the next part's joining
   }
   if (!begun && threadIdx.x == 0) first[p].n = 0;
 }
 template <class T, int D, int MB, bool ONE, bool TREE>
-__global__ __launch_bounds__(64 * kSplitW, blocks_of(D, MB)) void paged_split_kernel(const PagedAttnArgs a) {
-  __shared__ JoinLds<D, MB, kSplitW> lds;
-  First* first = (First*)a.parts;
-  float* parts = (float*)(first + a.blocks);
-  const long part_size = part_floats(a.rows_cap, D);
-  constexpr int KT = tile_keys(D, MB);
-  walk_share(a, blockIdx.x, first, a.tpt, [&](int b) { return tiles_of_sequence<KT, TREE>(a, b); },
-             [&](const Seq& sq, int b, int i0) { return rows_of_sequence<KT, TREE>(a, sq, b, i0, a.tpt); },
-             [&](const RowTile& r, int h, int t0, int t1, int part) {
-               attend_rows<T, D, MB, kSplitW, ONE, TREE>(a, r, h, t0, t1, part < 0 ? nullptr : parts + part * part_size, a.rows_cap, lds);
-             });
-}
+struct FewRows {
+  typedef JoinLds<D, MB, kSplitW> Lds;
+  static constexpr int W = kSplitW, kBlocks = blocks_of(D, MB), kAlign = 16, kDim = D, KT = tile_keys(D, MB);
+  static constexpr bool PLANES = false;
+  static __device__ __forceinline__ int tpt(const PagedAttnArgs& a) { return a.tpt; }
+  static __device__ __forceinline__ int tiles(const PagedAttnArgs& a, const Seq& sq, int b) { return tiles_of_sequence<KT, TREE>(a, sq, b); }
+  static __device__ __forceinline__ RowTile rows(const PagedAttnArgs& a, const Seq& sq, int b, int i0, int) { return rows_of_sequence<KT, TREE>(a, sq, b, i0, a.tpt); }
+  static __device__ __forceinline__ void attend(const PagedAttnArgs& a, Lds& lds, const RowTile& r, int h, int t0, int t1, float* part) {
+    attend_rows<T, D, MB, W, ONE, TREE>(a, r, h, t0, t1, part, a.rows_cap, lds);
+  }
+};
 
 // The k-th block that began a part, of those that firsts tells of, or -1 (a wave's work)
 __device__ __forceinline__ int begun_at(const First* firsts, int blocks, int k) {
@@ -551,14 +562,14 @@ __device__ __forceinline__ int begun_at(const First* firsts, int blocks, int k) 
 // this launch's would only come to end, and a block looks for its part among what they began instead: one tree of 77 tokens, 8 heads and
 // 168 shares, 13.3 us and 9.6; 16 trees, 128 cut and 512 shares, 10.3 and 13.2, so not there.
 constexpr int JN_Y = 8;
-template <class T, int D>
+template <class T, int D, bool PLANES>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttnArgs a) {
   constexpr int W = D / 4, N = 256 / W, U = 8;                       // threads of a row; groups; parts under way
   __shared__ __attribute__((aligned(16))) float so[N][D];
   __shared__ float2 ss[N];
-  const int planes = gridDim.x / a.cut, plane = blockIdx.x / a.cut, g = threadIdx.x / W, d = threadIdx.x % W * 4;       // planes: see tree_split_kernel
-  int at = blockIdx.x % a.cut;
-  if (a.cut < a.blocks) {
+  const int planes = PLANES ? gridDim.x / a.cut : 1, plane = PLANES ? blockIdx.x / a.cut : 0, g = threadIdx.x / W, d = threadIdx.x % W * 4;
+  int at = PLANES ? blockIdx.x % a.cut : blockIdx.x;
+  if (PLANES && a.cut < a.blocks) {
     at = begun_at((const First*)a.parts + plane * a.blocks, a.blocks, at);
     if (at < 0) return;
   }
@@ -626,9 +637,8 @@ static hipError_t rows_grid(PagedAttnArgs a, hipStream_t s) {
     if (a.tpt > a.max_new) a.tpt = a.max_new;                        // of rows_cap rows
     a.rows_cap = a.tpt * a.G;
     a.least = kSplitLeast;
-    a.cut = a.blocks;
-    hipLaunchKernelGGL((paged_split_kernel<T, D, MB, ONE, TREE>), dim3(a.blocks), dim3(64 * kSplitW), 0, s, a);
-    hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(a.blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_split_kernel<FewRows<T, D, MB, ONE, TREE>>), dim3(a.blocks), dim3(64 * kSplitW), 0, s, a);
+    hipLaunchKernelGGL((paged_join_kernel<T, D, false>), dim3(a.blocks, std::min(a.rows_cap, JN_Y)), dim3(256), 0, s, a);
     return hipGetLastError();
   }
   a.by_tpt = FastDiv::by(a.tpt);
