@@ -174,6 +174,14 @@ __device__ __forceinline__ float max_of_wave(float v) {
   return __uint_as_float((unsigned)last_lane(__float_as_uint(v)));
 }
 
+// What lanes of a wave leave in LDS for each other: all of it is written before any of it is read behind this, and read before it is
+// written anew.  The wave's accesses are in order anyway, so this keeps the compiler from moving them, and is no instruction
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 constexpr int SM_FEW = 128;        // logits that one wave ends a row with
 template <int NT>
 struct SampleLds {
@@ -398,6 +406,7 @@ __device__ __forceinline__ int draw_few(SampleLds<NT>& lds, const SampleArgs& a,
       s[j] = r.steps(w[j]);
       lds.steps[i] = s[j];
     }
+    wave_sync();
     for (int i = 0; i < n; ++i) {
       const u64 pi = lds.place[i], si = lds.steps[i];
 #pragma unroll
@@ -415,12 +424,14 @@ __device__ __forceinline__ int draw_few(SampleLds<NT>& lds, const SampleArgs& a,
       for (int j = 0; j < 2; ++j) kept[j] = kept[j] && before[j] < want;
     }
     u64 up[2] = {};
+    wave_sync();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       last = kept[j] && p[j] > last ? p[j] : last;
       s[j] = kept[j] ? r.steps(r.left(w[j])) : 0;
       lds.steps[lane + 64 * j] = s[j];
     }
+    wave_sync();
     last = last_lane(scan_of(last, 0, Most()));
     const u64 sum = sum_of_wave(s[0] + s[1]), want = drawn_at(a, row, sum);
     for (int i = 0; i < n; ++i) {
@@ -720,7 +731,9 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
         n += __popcll(yes);
         if (d - from < width && x[e] > -INFINITY) add(x[e], i + e);
       }
-      end_run(sum_of(n, [&](int j) { return above[j]; }), run);      // a wave's own: in order without a barrier
+      wave_sync();                                                   // a wave's own
+      end_run(sum_of(n, [&](int j) { return above[j]; }), run);
+      wave_sync();
     });
   } else {
     each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int, int run) {
