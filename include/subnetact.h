@@ -471,10 +471,11 @@ sna_status sna_copy_pages(const sna_paged_cache* cache, const int32_t* source_de
  * which the weights that are left make more than uniforms[r] (of [0, 1)) of all of them.  Temperature 0: the first of the largest.
  * A logit that is no number counts as -inf, weight 0; where +inf is the largest, only those have weight.  A row without weight gives
  * -1.  Weights are formed in 64 bits and held in steps of 2^-44 of the largest, or finer below 2^18 logits and up to
- * 2^-42 at 2^20: one below half a step is never drawn.  probs (fp32 [n_rows][vocab], may be NULL, no element of it a logit's): what is
- * left, each weight over their sum.  The settings are one number for all rows or, where the pointer is given, fp32 (top_k: int32) [n_rows] in device
- * memory; there a temperature that is not positive is 0 and one above 1e33 is that, and a top_k below 1, a top_p of 1 or more and
- * what is no number cut nothing.  Workspace as for attention.
+ * 2^-42 at 2^20: one below half a step is never drawn.  probs (fp32 [n_rows][vocab], may be NULL): what is left, each weight over their
+ * sum.  Tokens and probs share no byte with each other or with what is read; rows of probs may lie between rows of logits.  The
+ * settings are one number for all rows or, where the pointer is given, fp32 (top_k: int32) [n_rows] in device memory; there a
+ * temperature that is not positive is 0 and one above 1e33 is that, and a top_k below 1, a top_p of 1 or more and what is no number
+ * cut nothing.  Workspace as for attention.
  * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_WORKSPACE, SNA_E_HIP. */
 typedef struct {
   const void* logits_dev;         /* [n_rows][vocab] of any stride between rows; rows may overlap */

@@ -7,6 +7,8 @@
 
 namespace sna {
 
+typedef __int128 wide;                                               // strides are any 64-bit numbers
+
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 static sna_status check_cache(const sna_paged_cache* c) {
@@ -56,7 +58,6 @@ static sna_status check_rows(const sna_rows* r, const char* name) {
 static sna_status check_out(const sna_rows* r, const char* name, int64_t tokens, int64_t heads, int64_t dim) {
   const sna_status st = check_rows(r, name);
   if (st != SNA_OK) return st;
-  typedef __int128 wide;                                             // strides are any 64-bit numbers
   const wide far = (wide)1 << 100, ts = r->token_stride, hs = r->head_stride;
   const wide t = tokens == 1 ? far : ts < 0 ? -ts : ts, h = heads == 1 ? far : hs < 0 ? -hs : hs;
   const wide inner = t < h ? t : h, outer = t < h ? h : t, rows = t < h ? tokens : heads;
@@ -212,6 +213,19 @@ static bool apart(const Bytes& a, const Bytes& b) {
   const uintptr_t p = (uintptr_t)a.at, q = (uintptr_t)b.at;
   return a.n <= 0 || b.n <= 0 || (p <= q ? q - p >= (uintptr_t)a.n : p - q >= (uintptr_t)b.n);
 }
+// The same of rows of bytes, which may lie between each other's
+struct ByteRows { Bytes row; int64_t n; wide stride; };
+static bool apart(const ByteRows& a, const ByteRows& b) {
+  const auto last = [](const ByteRows& x) { return (wide)(uintptr_t)x.row.at + (x.n - 1) * x.stride; };
+  const auto first = [](const ByteRows& x) { return (wide)(uintptr_t)x.row.at; };
+  if (!a.row.at || !b.row.at || last(a) + a.row.n <= first(b) || last(b) + b.row.n <= first(a)) return true;
+  for (int64_t i = 0; i < a.n; ++i) {
+    const wide x = first(a) + i * a.stride, before = x - first(b) - b.row.n;                   // a row of b that begins no later ends before this one
+    const wide j = before < 0 ? 0 : b.stride ? before / b.stride + 1 : b.n;
+    if (j < b.n && first(b) + j * b.stride < x + a.row.n) return false;
+  }
+  return true;
+}
 
 sna_status sna_verify_tree(const sna_paged_batch* batch, const void* sampled_dev, int32_t sampled_bytes, const void* tokens_dev, int32_t token_bytes,
                            const int32_t* parents_dev, int32_t* kept_dev, int32_t* counts_dev, int32_t* next_dev, void* hip_stream) {
@@ -309,6 +323,12 @@ sna_status sna_sample_tokens(const sna_sampling* s, int32_t* tokens_dev, float* 
     return fail(SNA_E_CFG_ALIGN, "sample_tokens: a pointer is not aligned to its elements");
   if (need > 0 && (!workspace_dev || workspace_bytes < (size_t)need || !aligned16(workspace_dev)))
     return fail(SNA_E_WORKSPACE, "sample_tokens: a workspace of %lld bytes, 16-byte aligned, is needed", (long long)need);
+  const int64_t n = s->n_rows, size = s->dtype == SNA_DTYPE_FP32 ? 4 : 2;
+  const ByteRows tokens = {{tokens_dev, 4 * n}, 1, 0}, probs = {{probs_dev, 4l * s->vocab}, n, (wide)4 * probs_stride}, logits = {{s->logits_dev, size * s->vocab}, n, (wide)size * s->row_stride};
+  bool free = apart(tokens, probs) && apart(tokens, logits) && apart(probs, logits);
+  for (const void* x : {(const void*)s->uniforms_dev, (const void*)s->temperature_dev, (const void*)s->top_p_dev, (const void*)s->min_p_dev, (const void*)s->top_k_dev})
+    free = free && apart(tokens, ByteRows{{x, 4 * n}, 1, 0}) && apart(ByteRows{{x, 4 * n}, 1, 0}, probs);
+  if (!free) return fail(SNA_E_CFG_RANGE, "sample_tokens: a result is written over another or over what is read");
   SampleArgs a = {};
   a.logits = s->logits_dev; a.stride = s->row_stride;
   a.u = s->uniforms_dev;

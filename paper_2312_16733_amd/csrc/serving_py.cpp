@@ -722,7 +722,8 @@ PyMethodDef methods[] = {
      "all; ties go to the lower token) the fewest that make top_p of their weights exp(logit / temperature), of these the ones with\n"
      "at least min_p of the largest's; drawn by running sums in token order.  Temperature 0: the largest.  -1 where no logit is more\n"
      "than -inf (NaN counts as that).  Each setting is a number or a tensor [n] (top_k int32, the others fp32).  probs: True, or an\n"
-     "fp32 [n][V] to write to: (tokens, probs) is returned, the probabilities that the token was drawn by."},
+     "fp32 [n][V] to write to: (tokens, probs) is returned, the probabilities that the token was drawn by.  What is written to, out\n"
+     "(int32 [n]) or probs, is none of what is read."},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

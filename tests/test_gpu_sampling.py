@@ -276,3 +276,22 @@ def test_a_sampled_token_is_what_verification_takes():
     target = torch.cat((probs.view(n, K, V), probs.view(n, K, V)[:, :1]), 1)
     out, accepted = sna.verify_draft(target, tokens.view(n, K), torch.rand(n, K + 1, generator=g).cuda(), draft_probs=probs.view(n, K, V).contiguous())
     assert accepted.tolist() == [K] * n and torch.equal(out[:, :K], tokens.view(n, K))
+
+
+@pytest.mark.parametrize("V", [1000, 5003])
+def test_results_beside_what_is_read(V):
+    """Probabilities in the gaps between the logits' rows are written there; what would be written over what is read is refused."""
+    n = 7
+    both = torch.full((n, 2 * V + 5), 3.0, device="cuda")
+    logits, u = logits_of(n, V, "fp32", 12)
+    both[:, :V] = logits
+    u = u.cuda()
+    want, p = sna.sample_tokens(logits, u, top_p=0.8, probs=True)
+    got = sna.sample_tokens(both[:, :V], u, top_p=0.8, probs=both[:, V + 2: 2 * V + 2])
+    assert torch.equal(got[0], want) and torch.equal(both[:, V + 2: 2 * V + 2], p)
+    assert torch.equal(both[:, :V], logits) and (both[:, V: V + 2] == 3).all() and (both[:, 2 * V + 2:] == 3).all()
+    k = torch.full((n,), 9, dtype=torch.int32, device="cuda")
+    for bad in (dict(probs=both[:, V - 1: 2 * V - 1]), dict(probs=both[:, :V]), dict(out=k, top_k=k), dict(out=u.view(torch.int32)), dict(out=both.view(torch.int32)[1, :n]),
+                dict(out=p.view(torch.int32)[2, :n], probs=p), dict(probs=torch.zeros(n * V, device="cuda").as_strided((n, V), (1, 1)))):
+        with pytest.raises(sna.SnaError):
+            sna.sample_tokens(both[:, :V], u, **bad)

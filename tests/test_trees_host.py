@@ -234,3 +234,32 @@ def test_no_page_is_lost_or_given_twice():
         except ValueError:
             pass
         assert pool.n_free == 40 - len({p for s in live for p in s})
+
+
+def test_samples_over_what_is_read_are_refused():
+    """Tokens and probabilities share no byte with each other, the logits, the random numbers or the settings; rows may lie between rows.
+    What passes is refused for its size, behind every other check: no call here is launched."""
+    n, V, at = 1 << 22, 1000, lambda i: (i + 1) << 40
+    given = dict(n_rows=n, vocab=V, uniforms_dev=at(1), temperature_dev=at(2), top_p_dev=at(3), min_p_dev=at(4), top_k_dev=at(5), tokens=at(6))
+    launched = lambda **k: (sample(**k), b"more blocks than a launch has" in sna.lib().sna_last_error())  # noqa: E731
+    for dtype, size in ((0, 4), (1, 2), (2, 2)):
+        good = dict(given, dtype=dtype, logits_dev=at(0), row_stride=V, probs=at(7), stride=V)
+        assert launched(**good) == (RANGE, True)
+        read = {"logits_dev": (at(0), n * V * size), **{name: (at(i), 4 * n) for name, i in (("uniforms_dev", 1), ("temperature_dev", 2), ("top_p_dev", 3), ("min_p_dev", 4), ("top_k_dev", 5))}}
+        for name, other, mine in (("tokens", "probs", 4 * n), ("probs", "tokens", 4 * n * V)):
+            for what, (p, m) in {**read, other: (good[other], 4 * n * V if other == "probs" else 4 * n)}.items():
+                for over in (p, p + m - 4, p - mine + 4):
+                    assert launched(**dict(good, **{name: over})) == (RANGE, False), (dtype, name, what, over)
+                for beside in (p + m, p - mine):
+                    assert launched(**dict(good, **{name: beside})) == (RANGE, True), (dtype, name, what, beside)
+        # rows of both in one array: logits, then probabilities, and a gap between; one row for all
+        step = V * size + 4 * V + 64
+        rows = dict(good, row_stride=step // size, stride=step // 4)
+        assert launched(**dict(rows, probs=at(0) + V * size)) == (RANGE, True) and launched(**dict(rows, probs=at(0) + step - 4 * V)) == (RANGE, True)
+        assert launched(**dict(rows, probs=at(0) + V * size - 4)) == (RANGE, False) and launched(**dict(rows, probs=at(0) + step - 4 * V + 4)) == (RANGE, False)
+        assert launched(**dict(rows, probs=at(0) - 5 * step + V * size + 64)) == (RANGE, True)
+        assert launched(**dict(rows, stride=step // 4 + 1, probs=at(0) + V * size)) == (RANGE, False)      # further on they meet
+        assert launched(**dict(good, row_stride=0, probs=at(0) + V * size)) == (RANGE, True) and launched(**dict(good, row_stride=0, probs=at(0) - 4 * V + 4)) == (RANGE, False)
+        assert launched(**dict(rows, tokens=at(0) + V * size + 32)) == (RANGE, False)
+    none = dict(given, temperature_dev=None, top_p_dev=None, min_p_dev=None, top_k_dev=None, probs=None, logits_dev=at(0), row_stride=V)
+    assert launched(**none) == (RANGE, True)
