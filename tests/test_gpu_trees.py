@@ -399,3 +399,30 @@ def test_calls_on_another_stream():
     torch.cuda.current_stream().wait_stream(other)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and counts.tolist() == [2, 2]        # the root, and of its children the first
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("seqs", [[(1, 1)], [(300, 1), (16, 1), (17, 1), (129, 1)], [(40, 0), (33, 1), (0, 0), (200, 1)], [(83, 83), (150, 37), (64, 64), (9, 1)], [(40, 13), (1000, 4), (21, 21)]])
+@pytest.mark.parametrize("heads,page,rot,interleaved,norm", [
+    ((12, 12, 64), 16, 64, False, False), ((9, 3, 64), 32, 32, True, True), ((32, 8, 128), 16, 128, True, False), ((7, 1, 128), 64, 48, False, True), ((40, 8, 128), 16, 64, True, True)])
+def test_positions_of_any_number(dtype, seqs, heads, page, rot, interleaved, norm):
+    """Every form of the append, single tokens a sequence among them, by positions that are no slots': rotation goes by them, the place
+    in the cache by the slot."""
+    s = ref.make(seqs, *heads, page, ref.DT[dtype], seed=19, layers=2)
+    g = torch.Generator().manual_seed(6)
+    T = s["q"].shape[0]
+    positions = torch.randint(0, 200, (T,), generator=g, dtype=torch.int32)
+    positions[::5] = torch.randint(0, 1 << 17, (len(positions[::5]),), generator=g, dtype=torch.int32)
+    positions[3::7] = -3
+    inv = (10000.0 ** (-torch.arange(0, rot, 2).double() / rot)).float().cuda()
+    w = [torch.rand(heads[2], generator=g).cuda() + 0.5 if norm else None for _ in range(2)]
+    (wq, eq), (wk, ek), wv = ref.append(dict(s, seqs=[(p + 1, 1) for p in positions.tolist()]), inv, interleaved, *w, eps=1e-5)
+    old_k, old_v = s["k_pages"].clone(), s["v_pages"].clone()
+    got = sna.kv_append(*parts(s), s["q"], s["k"], s["v"], inv_freq=inv, interleaved=interleaved, q_norm=w[0], k_norm=w[1], eps=1e-5, positions=positions.cuda())
+    within(got, wq, eq, "q")
+    where = [(b, l - n + i) for b, (l, n) in enumerate(seqs) for i in range(n)]
+    pages, slots = torch.tensor([int(s["table"][b, p // page]) for b, p in where], device="cuda"), torch.tensor([p % page for _, p in where], device="cuda")
+    within(s["k_pages"][pages, :, slots], wk, ek, "k")
+    assert torch.equal(s["v_pages"][pages, :, :, slots], wv)
+    old_k[pages, :, slots], old_v[pages, :, :, slots] = s["k_pages"][pages, :, slots], s["v_pages"][pages, :, :, slots]
+    assert same_bits(old_k, s["k_pages"]) and same_bits(old_v, s["v_pages"])
