@@ -475,7 +475,7 @@ sna_status sna_copy_pages(const sna_paged_cache* cache, const int32_t* source_de
  * sum.  Tokens and probs share no byte with each other or with what is read; rows of probs may lie between rows of logits.  The
  * settings are one number for all rows or, where the pointer is given, fp32 (top_k: int32) [n_rows] in device memory; there a
  * temperature that is not positive is 0 and one above 1e33 is that, and a top_k below 1, a top_p of 1 or more and what is no number
- * cut nothing.  Workspace as for attention.
+ * cut nothing.  Workspace as for attention; it goes by rows and vocabulary alone, and one for more rows serves fewer.
  * Errors: SNA_E_NULL, SNA_E_CFG_RANGE, SNA_E_CFG_ALIGN, SNA_E_WORKSPACE, SNA_E_HIP. */
 typedef struct {
   const void* logits_dev;         /* [n_rows][vocab] of any stride between rows; rows may overlap */

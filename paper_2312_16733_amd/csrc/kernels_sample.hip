@@ -520,15 +520,14 @@ __global__ __launch_bounds__(NT) void sample_small_kernel(const SampleArgs a) {
 }
 
 // ---- rows of several blocks ------------------------------------------------------------------------------------------------------
-// What a row needs between launches
+// What a row needs between launches where it may be cut
 struct RowWork {
   u64 weights[SM_BINS];            // by distance from the largest
   unsigned counts[SM_BINS];
   u64 list[SM_LIST];               // logits and, behind them, their indexes
   unsigned listed, pad;            // more than SM_LIST: not all of them are there
-  u64 cut;                         // what the row comes to
-  double share;
 };
+struct RowEnd { u64 cut; double share; };        // what it comes to
 // How a row is cut
 enum Kind { CUT_NONE, CUT_BEST, CUT_COUNT, CUT_WEIGHT, CUT_SLOWLY }; // to the first of the largest; all that is kept in the list; the list at the cut; digit by digit of the whole row
 __device__ __forceinline__ Kind kind_of(const Row& r) {
@@ -537,7 +536,8 @@ __device__ __forceinline__ Kind kind_of(const Row& r) {
   return r.top_p < 1.f ? CUT_WEIGHT : CUT_NONE;
 }
 struct Work {                      // of a call
-  RowWork* rows;                   // [n]
+  RowWork* rows;                   // [n], or nullptr: none is cut
+  RowEnd* done;                    // [n]
   float2* ends;                    // [n][parts]: the largest, and of every eighth the smallest but -inf
   u64* runs;                       // [n][runs]
   int* best;                       // [n][parts]: the first of the largest, for rows of which no other is kept
@@ -588,13 +588,14 @@ template <class X>
 __global__ __launch_bounds__(SM_T) void sample_top_kernel(const SampleArgs a, const Work w) {
   __shared__ SampleLds<SM_T> lds;
   const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts;
-  RowWork& rw = w.rows[row];
-  if (part == 0)
+  if (part == 0 && w.rows) {
+    RowWork& rw = w.rows[row];
     for (int i = threadIdx.x; i < SM_BINS; i += SM_T) {
       rw.weights[i] = 0;
       rw.counts[i] = 0;
     }
-  if (part == 0 && threadIdx.x == 0) rw.listed = 0;
+    if (threadIdx.x == 0) rw.listed = 0;
+  }
   float top = -INFINITY, low = INFINITY;
   int at = INT_MAX;                                                  // the first of the lane's largest
   const Row r = row_of<X>(a, row);
@@ -681,19 +682,19 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
   const Kind kind = kind_of(r);
   if (kind == CUT_SLOWLY || kind == CUT_BEST) return;
   if (!r.begin(ends_of(w, row))) return;
-  RowWork& rw = w.rows[row];
+  RowWork* const rw = w.rows + row;                                  // looked at only where the row is cut
   int at = SM_BINS;
   u64 want;
   if (tid == 0) listed = 0;
-  if (kind != CUT_NONE) at = cut_at(lds, r, kind, want, [&](int j) { return kind == CUT_COUNT ? (u64)rw.counts[j * SM_T + tid] : rw.weights[j * SM_T + tid]; });
+  if (kind != CUT_NONE) at = cut_at(lds, r, kind, want, [&](int j) { return kind == CUT_COUNT ? (u64)rw->counts[j * SM_T + tid] : rw->weights[j * SM_T + tid]; });
   __syncthreads();
   const auto add = [&](float x, int i) {
     const u64 v = (u64)__float_as_uint(x) << 32 | (unsigned)i;
     const unsigned n = atomicAdd(&listed, 1u);
     if (n < SM_STAGE) list[n] = v;
     else {                                                           // more than are written out together
-      const unsigned m = atomicAdd(&rw.listed, 1u);
-      if (m < SM_LIST) rw.list[m] = v;
+      const unsigned m = atomicAdd(&rw->listed, 1u);
+      if (m < SM_LIST) rw->list[m] = v;
     }
   };
   const auto end_run = [&](u64 sum, int run) {
@@ -745,9 +746,9 @@ __global__ __launch_bounds__(SM_T) void sample_list_kernel(const SampleArgs a, c
   }
   __syncthreads();
   const unsigned n = min(listed, (unsigned)SM_STAGE);
-  if (tid == 0 && n) first = atomicAdd(&rw.listed, n);
+  if (tid == 0 && n) first = atomicAdd(&rw->listed, n);               // none without a cut
   __syncthreads();
-  for (unsigned j = tid; j < n && first + j < SM_LIST; j += SM_T) rw.list[first + j] = list[j];
+  for (unsigned j = tid; j < n && first + j < SM_LIST; j += SM_T) rw->list[first + j] = list[j];
 }
 
 template <class X>
@@ -756,28 +757,31 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   __shared__ SampleLds<SM_FINAL> lds;
   const int tid = threadIdx.x, row = blockIdx.x;
   const X* logits = (const X*)a.logits + row * a.stride;
-  RowWork& rw = w.rows[row];
+  RowWork* const rw = w.rows + row;                                  // looked at only where there are any
   Row r = row_of<X>(a, row);
   const Kind kind = kind_of(r);
   // everything that the launches before have left, in one round trip
-  u64 held[N], sums[SM_BINS / SM_FINAL], runs[SM_BINS / SM_FINAL];
+  u64 held[N] = {}, sums[SM_BINS / SM_FINAL] = {}, runs[SM_BINS / SM_FINAL];
+  unsigned listed = 0;
+  if (w.rows) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) held[j] = rw.list[j * SM_FINAL + tid];
+    for (int j = 0; j < N; ++j) held[j] = rw->list[j * SM_FINAL + tid];
+#pragma unroll
+    for (int j = 0; j < SM_BINS / SM_FINAL; ++j) sums[j] = rw->weights[j * SM_FINAL + tid];
+    listed = rw->listed;
+  }
 #pragma unroll
   for (int j = 0; j < SM_BINS / SM_FINAL; ++j) {
     const int i = j * SM_FINAL + tid;
-    sums[j] = rw.weights[i];
     runs[j] = i < w.n_runs ? w.runs[(long)row * w.n_runs + i] : 0;
     lds.sums[i] = 0;
   }
-  const unsigned listed = rw.listed;
   __syncthreads();
   const float2 ends = ends_of(w, row);
   if (!r.begin(ends)) {                                              // nothing to draw from
     if (tid == 0) {
       a.tokens[row] = -1;
-      rw.cut = 0;
-      rw.share = 0.0;
+      w.done[row] = RowEnd{0, 0.0};
     }
     return;
   }
@@ -799,7 +803,7 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
     token = draw_row(lds, a, row, r, total, each);
   } else if (kind == CUT_COUNT && m > SM_HELD) {
     const auto each = [&](const auto& f) {
-      for (unsigned i = tid; i < m; i += SM_FINAL) f(__uint_as_float((unsigned)(rw.list[i] >> 32)), (int)rw.list[i]);
+      for (unsigned i = tid; i < m; i += SM_FINAL) f(__uint_as_float((unsigned)(rw->list[i] >> 32)), (int)rw->list[i]);
     };
     cut_row(lds, r, each);
     token = draw_row(lds, a, row, r, total, each);
@@ -829,8 +833,8 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
         if (m > SM_HELD) {
           r.cut = select(lds, 32 - r.spare + r.bits, want, [&](const auto& f) {
             for (unsigned i = tid; i < m; i += SM_FINAL) {
-              const float l = __uint_as_float((unsigned)(rw.list[i] >> 32));
-              f(r.place(l, (int)rw.list[i]), r.steps(r.weight(l)));
+              const float l = __uint_as_float((unsigned)(rw->list[i] >> 32));
+              f(r.place(l, (int)rw->list[i]), r.steps(r.weight(l)));
             }
           });
         } else {
@@ -853,8 +857,8 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
         if (s) atomicAdd(&lds.sums[at[j] / SM_RUN], s);
       }
       for (unsigned i = SM_HELD + tid; i < m; i += SM_FINAL) {
-        const u64 s = r.steps(r.kept(__uint_as_float((unsigned)(rw.list[i] >> 32)), (int)rw.list[i]));
-        if (s) atomicAdd(&lds.sums[(int)rw.list[i] / SM_RUN], s);
+        const u64 s = r.steps(r.kept(__uint_as_float((unsigned)(rw->list[i] >> 32)), (int)rw->list[i]));
+        if (s) atomicAdd(&lds.sums[(int)rw->list[i] / SM_RUN], s);
       }
       __syncthreads();
       const Crossing c = crossing(lds, [&](u64 all) { return drawn_at(a, row, all); });
@@ -866,8 +870,7 @@ __global__ __launch_bounds__(SM_FINAL) void sample_draw_kernel(const SampleArgs 
   }
   if (tid == 0) {
     a.tokens[row] = token;
-    rw.cut = r.cut;
-    rw.share = share_of(a, total);
+    w.done[row] = RowEnd{r.cut, share_of(a, total)};
   }
 }
 
@@ -876,8 +879,8 @@ __global__ __launch_bounds__(SM_T) void sample_probs_kernel(const SampleArgs a, 
   const int row = blockIdx.x / w.parts, part = blockIdx.x % w.parts;
   Row r = row_of<X>(a, row);
   r.begin(ends_of(w, row));
-  r.cut = w.rows[row].cut;
-  const double f = w.rows[row].share;
+  r.cut = w.done[row].cut;
+  const double f = w.done[row].share;
   float* out = a.probs + row * a.p_stride;
   each_run<X>(a, w, row, part, r, [&](const float (&x)[8], int i, int) {
     float p[8];
@@ -895,45 +898,66 @@ __global__ __launch_bounds__(SM_T) void sample_probs_kernel(const SampleArgs a, 
   });
 }
 
-// Blocks of a row: as many as make 512 of all rows, two on a CU, with 8 turns of a wave or more each
-static Work work_of(int n, int V, void* at) {
+// What is known of all rows: that one logit is kept of each (temperature 0, top_k 1), which the first reading finds; that none is cut
+static bool keeps_one(const SampleArgs& a) { return (!a.temperature_of && a.temperature == 0.f) || (!a.top_k_of && a.top_k == 1); }
+static bool cuts_none(const SampleArgs& a) { return keeps_one(a) || (!a.top_k_of && !a.top_p_of && !a.top_k && !(a.top_p < 1.f)); }
+
+// Rows of long logits that are worked on at a time, in the same memory: 90 KB and 1 / 64 byte a logit each, which for all rows of a large
+// batch would be more than its logits (65536 of 4097: 5.9 GB beside 1.1).  A turn more costs 12 us, of the 260 that so many rows of 5000 take
+// (with turns of 1024, 4096 rows of 5000 took 169 us instead of 131)
+constexpr int SM_ROWS = 8192;
+
+// Blocks of a row: as many as make 512 of all rows, two on a CU, with 8 turns of a wave or more each.  The memory goes by rows and
+// vocabulary alone, so that a workspace serves calls of other settings, too
+static Work work_of(int n, int V, void* work) {
   Work w = {};
   const long want = ((long)n * V + 511) / 512, turn = SM_T / 64 * SM_RUN;
   w.len = (int)(std::min(std::max((want + turn - 1) / turn, 1l), (V + turn - 1) / turn) * turn);
   w.parts = (V + w.len - 1) / w.len;
   w.n_runs = (V + SM_RUN - 1) / SM_RUN;
-  w.rows = (RowWork*)at;
-  w.runs = (u64*)(w.rows + n);
+  w.rows = (RowWork*)work;
+  w.done = (RowEnd*)(w.rows + n);
+  w.runs = (u64*)(w.done + n);
   w.ends = (float2*)(w.runs + (long)n * w.n_runs);
   w.best = (int*)(w.ends + (long)n * w.parts);
   return w;
 }
-size_t sample_workspace(int n, int vocab, int) {
+size_t sample_workspace(int n, int vocab) {
   if (vocab <= SM_SMALL) return 0;
+  n = std::min(n, SM_ROWS);
   const Work w = work_of(n, vocab, nullptr);
-  return n * (sizeof(RowWork) + w.n_runs * sizeof(u64) + w.parts * (sizeof(float2) + sizeof(int)));
+  return n * (sizeof(RowWork) + sizeof(RowEnd) + w.n_runs * sizeof(u64) + w.parts * (sizeof(float2) + sizeof(int)));
 }
 
 template <class X>
-static hipError_t sample_of(const SampleArgs& a, hipStream_t s) {
+static hipError_t sample_of(SampleArgs a, hipStream_t s) {
   if (a.V <= SM_SMALL) {
     if (!fits_a_launch(a.n, 1024)) return hipErrorInvalidConfiguration;
     if (a.V <= 1024) hipLaunchKernelGGL((sample_small_kernel<X, 256>), dim3(a.n), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((sample_small_kernel<X, 1024>), dim3(a.n), dim3(1024), 0, s, a);
     return hipGetLastError();
   }
-  const Work w = work_of(a.n, a.V, a.work);
-  const long blocks = (long)a.n * w.parts;
-  if (!fits_a_launch(blocks, SM_T) || !fits_a_launch(a.n, SM_FINAL)) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)blocks), block(SM_T);
-  // without settings of each row: one logit that is kept needs the first reading only
-  const bool best = (!a.temperature_of && a.temperature == 0.f) || (!a.top_k_of && a.top_k == 1);
-  hipLaunchKernelGGL(sample_top_kernel<X>, grid, block, 0, s, a, w);
-  if (!best && (a.top_k_of || a.top_p_of || a.temperature_of || a.top_k || a.top_p < 1.f)) hipLaunchKernelGGL(sample_sums_kernel<X>, grid, block, 0, s, a, w);
-  if (!best) hipLaunchKernelGGL(sample_list_kernel<X>, grid, block, 0, s, a, w);
-  hipLaunchKernelGGL(sample_draw_kernel<X>, dim3(a.n), dim3(SM_FINAL), 0, s, a, w);
-  if (a.probs) hipLaunchKernelGGL(sample_probs_kernel<X>, grid, block, 0, s, a, w);
-  return hipGetLastError();
+  Work w = work_of(std::min(a.n, SM_ROWS), a.V, a.work);
+  const bool one = keeps_one(a);
+  if (cuts_none(a)) w.rows = nullptr;
+  for (int left = a.n;;) {
+    a.n = std::min(left, SM_ROWS);
+    const dim3 grid(a.n * w.parts), block(SM_T);
+    hipLaunchKernelGGL(sample_top_kernel<X>, grid, block, 0, s, a, w);
+    if (w.rows) hipLaunchKernelGGL(sample_sums_kernel<X>, grid, block, 0, s, a, w);
+    if (!one) hipLaunchKernelGGL(sample_list_kernel<X>, grid, block, 0, s, a, w);
+    hipLaunchKernelGGL(sample_draw_kernel<X>, dim3(a.n), dim3(SM_FINAL), 0, s, a, w);
+    if (a.probs) hipLaunchKernelGGL(sample_probs_kernel<X>, grid, block, 0, s, a, w);
+    if ((left -= a.n) == 0) return hipGetLastError();
+    a.logits = (const X*)a.logits + a.n * a.stride;
+    a.u += a.n;
+    a.tokens += a.n;
+    if (a.probs) a.probs += a.n * a.p_stride;
+    if (a.temperature_of) a.temperature_of += a.n;
+    if (a.top_p_of) a.top_p_of += a.n;
+    if (a.min_p_of) a.min_p_of += a.n;
+    if (a.top_k_of) a.top_k_of += a.n;
+  }
 }
 hipError_t launch_sample(SampleArgs a, int dtype, hipStream_t s) {
   int bits = 0;

@@ -331,7 +331,7 @@ struct SampleArgs {
   void* work;
   int scale_bits;                                // weights are held in steps of 2^-scale_bits of the largest
 };
-size_t sample_workspace(int n, int vocab, int dtype);
+size_t sample_workspace(int n, int vocab);
 hipError_t launch_sample(SampleArgs a, int dtype, hipStream_t s);
 
 }  // namespace sna

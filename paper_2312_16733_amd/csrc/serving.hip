@@ -308,7 +308,7 @@ static sna_status check_sampling(const sna_sampling* s) {
 
 int64_t sna_sample_tokens_workspace_bytes(const sna_sampling* s) {
   const sna_status st = check_sampling(s);
-  return st != SNA_OK ? st : s->n_rows ? (int64_t)sample_workspace(s->n_rows, s->vocab, s->dtype) : 0;
+  return st != SNA_OK ? st : s->n_rows ? (int64_t)sample_workspace(s->n_rows, s->vocab) : 0;
 }
 
 sna_status sna_sample_tokens(const sna_sampling* s, int32_t* tokens_dev, float* probs_dev, int64_t probs_stride, void* workspace_dev, size_t workspace_bytes,

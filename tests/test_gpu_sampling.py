@@ -295,3 +295,22 @@ def test_results_beside_what_is_read(V):
                 dict(out=p.view(torch.int32)[2, :n], probs=p), dict(probs=torch.zeros(n * V, device="cuda").as_strided((n, V), (1, 1)))):
         with pytest.raises(sna.SnaError):
             sna.sample_tokens(both[:, :V], u, **bad)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_batches_of_thousands(dtype):
+    """Rows that do not fit one workspace's worth: the same bits as in small calls, whatever their settings."""
+    n, V = 8192 + 5, 4099
+    g = torch.Generator(device="cuda").manual_seed(17)
+    logits, u = (torch.randn(n, V + 1, generator=g, device="cuda") * 2).to(DT[dtype])[:, 1:], torch.rand(n, generator=g, device="cuda")
+    logits[8193] = -math.inf
+    pick = lambda *x: torch.tensor(x, device="cuda")[torch.randint(0, len(x), (n,), generator=g, device="cuda")]  # noqa: E731
+    rows = {"temperature": pick(0.0, 0.7, 1.0), "top_k": pick(0, 1, 40, 2000).int(), "top_p": pick(1.0, 0.9), "min_p": pick(0.0, 0.1)}
+    for settings in ({}, {"temperature": 0.0}, {"top_k": 1, "min_p": 0.5}, {"top_k": 60}, {"top_p": 0.9}, rows, {"temperature": rows["temperature"]}):
+        tokens, probs = sna.sample_tokens(logits, u, probs=True, **settings)
+        assert torch.equal(sna.sample_tokens(logits, u, **settings), tokens)
+        for a in range(0, n, 1000):
+            part = {k: v[a: a + 1000] if torch.is_tensor(v) else v for k, v in settings.items()}
+            t, p = sna.sample_tokens(logits[a: a + 1000], u[a: a + 1000], probs=True, **part)
+            assert torch.equal(t, tokens[a: a + 1000]) and torch.equal(p, probs[a: a + 1000]), (list(settings), a)
+        assert tokens[8193] == -1

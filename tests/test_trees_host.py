@@ -263,3 +263,14 @@ def test_samples_over_what_is_read_are_refused():
         assert launched(**dict(rows, tokens=at(0) + V * size + 32)) == (RANGE, False)
     none = dict(given, temperature_dev=None, top_p_dev=None, min_p_dev=None, top_k_dev=None, probs=None, logits_dev=at(0), row_stride=V)
     assert launched(**none) == (RANGE, True)
+
+
+def test_a_large_batch_of_samples_takes_bounded_memory():
+    """A workspace serves calls of any settings and of fewer rows, and does not grow past some thousand rows."""
+    need = lambda **k: sna.lib().sna_sample_tokens_workspace_bytes(C.byref(sampling(**k)))  # noqa: E731
+    assert 0 < need(n_rows=1, vocab=4097) < 128 << 10 and need(n_rows=100000, vocab=4096) == 0
+    for vocab in (4097, 131072, 1 << 20):
+        sizes = [need(n_rows=n, vocab=vocab) for n in (1, 7, 128, 4000, 8192, 8193, 65536, 1 << 24)]
+        assert sizes == sorted(sizes) and sizes[4] == sizes[-1] < 1 << 30
+        for k in (dict(temperature=0.0), dict(top_k=1), dict(top_k=9, top_p=0.5), dict(top_p_dev=AT, dtype=2)):
+            assert need(n_rows=128, vocab=vocab, **k) == sizes[2]
