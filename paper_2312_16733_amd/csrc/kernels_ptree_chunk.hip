@@ -1,15 +1,17 @@
 // Attention of the tokens of drafted trees over the paged cache, many rows of queries per key / value head: pprefill_kernel.h's walk,
 // 128 rows a block.
-//   A turn of a tile, 2 blocks of 4 waves on a CU, takes 4500 cycles, of which products are 2050, vector instructions as much and LDS 2500.
-// What was tried and brought nothing: keys asked for two tiles ahead and values one and a half (three and two buffers, explicit counts; 137 to
-// 143 us for 77 tokens over 65519 keys, 127 to 130 as it is), operands read in fours before their products (129).
+//   A turn of a tile, 2 blocks of 4 waves on a CU, takes 6200 cycles, of which products are 3070, vector instructions as much and LDS 2500
+// (77 tokens over 65519 keys, 32 heads over 8 of 128: 149 to 153 us once the chip has settled).
+// What was tried and brought nothing, when the probabilities had one product (4500 cycles, 127 to 130 us with the join): keys asked for two
+// tiles ahead and values one and a half (three and two buffers, explicit counts; 137 to 143), operands read in fours before their
+// products (129).
 #include "pprefill_kernel.h"
 
 namespace sna {
 
 // The keys of all sequences and heads, laid end to end, in equal shares, as where rows are few: trees of a step differ in length and
 // size, and shares of each would not fill the last round of blocks (16 trees of up to 32 tokens over up to 4096 keys, 32 heads over
-// 8 of 128: 66 us in five shares each, 58 in equal ones).  A tree of more than 128 rows has a block for each 128 of them on every
+// 8 of 128, with one product of the probabilities: 66 us in five shares each, 58 in equal ones).  A tree of more than 128 rows has a block for each 128 of them on every
 // share: they walk the same keys side by side on one XCD, whose L2 reads them once.  Block j of a share is one of plane j, which has parts of
 // its own, plane after plane.
 template <class T, int D>

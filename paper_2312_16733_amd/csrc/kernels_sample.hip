@@ -12,7 +12,7 @@
 // sums of what is kept for certain, by runs of 512.  Then one block a row has the list and the sums.  128 rows of 131072 fp32, top_p 0.95 (a third
 // of each is kept): 12, 20, 27 and 11 us, 66 in a loop of calls.  The first is bound by memory (5.5 TB/s); the next two by vector
 // instructions, 32 and 38 a logit, at work 84 and 71 % of the cycles, of which a weight is 20; the last by its round trips.  Where one
-// logit is kept, the first reading finds it: 17 us, and 44 by the others.
+// logit is kept, the first reading finds it: 15 us, and 44 by the others.
 #include <algorithm>
 #include <climits>
 #include <type_traits>

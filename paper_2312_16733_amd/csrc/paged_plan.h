@@ -110,12 +110,15 @@ inline AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
 // ---- trees of drafted tokens ----
 // Up to kTreeFew rows a key / value head the few-rows kernel takes them in one tile of rows, and up to twice that in two where the keys
 // are few: the many-rows kernel has 20 us before and behind its turns, if its keys are shared out.  In us, 32 heads over 8 of 128: 16
-// tokens over 8192 keys 22 (few rows) and 37; 16 trees of up to 12 over up to 4096 57 and 46, 64 of up to 13 over up to 2048 99 and 97.
-// So are more rows where the step has few scores (kTreeScores, as for chunks): 32 tokens over 600 keys, 28 heads over 4, 11 to 12 (few rows)
-// and 21.5; 64 x 32 over 600, 8 heads over 1 of 64 (10 M), 27 and 16.5.
-// The rest is walked by blocks of kTreeRows, whole, or their keys shared out over kTreeBlocks (two on a CU; 256 took 64 us for 58, 180
-// for 127; one tree of 128 tokens over 30000 keys, 32 heads over 1, 87 and 606), whichever a count of the turns says is sooner, a turn
-// being 2 us, 1.24 with heads of 64, and three quarters where most CUs have one block; whole where blocks come in many rounds anyway.
+// tokens over 8192 keys 23 (few rows) and 30; 16 trees of up to 12 over up to 4096 56 and 49, 64 of up to 13 over up to 2048 109 and 99.
+// So are more rows where the step has few scores (kTreeScores, as for chunks): 32 tokens over 600 keys, 28 heads over 4, 12 (few rows)
+// and 23.5; 64 x 32 over 600, 8 heads over 1 of 64 (10 M), 26 and 20.  Not everywhere is that border the best: 500 tokens over 1500 keys,
+// 12 heads of 64 (9 M), would take 18 and take 44; 300 over 2000, 16 of 128, 29 and 37.
+// The rest is walked by blocks of kTreeRows, whole, or their keys shared out over kTreeBlocks (two on a CU; 256 took 73 us for 68, 198
+// for 161; one tree of 128 tokens over 30000 keys, 32 heads over 1, shared 113 and whole 725), whichever a count of the turns says is sooner,
+// a turn being 2 us, 1.24 with heads of 64, and three quarters where most CUs have one block; whole where blocks come in many rounds anyway.
+// Two things that the count leaves out: what a plane has of rows (33 tokens, 32 heads over 8, are one plane of 128 rows and one of 4, with half
+// of the blocks each: 65 us over 30000 keys, and 32 tokens 52), and the parts' bytes (512 over 4000 keys: 95 us, of which it expects 51).
 constexpr int kTreeFew = 32, kTreeRows = 128, kTreeBlocks = 512, kTreeLeast = 6, kTreeTurns = 2048;
 constexpr long kTreeScores = 8l << 20;
 inline int tree_planes(int max_new, int group) { return (max_new + kTreeRows / group - 1) / (kTreeRows / group); }

@@ -65,7 +65,7 @@ struct Attend {
   // rounding alone (rounded once, the probabilities add as much again: 2.3e-3 of the norm in bf16, not 1.7e-3).  Up to 32 rows, single
   // and drafted tokens, the cache's bytes bound a launch, and this costs little: 16 sequences of up to 4096 keys with five tokens 46.5
   // us with and without, 64 of up to 2048 with eight and heads of 64 18.7 and 17.9.  Blocks of 64 rows are chunks, bound by their
-  // products and exponentials (a mixed step 17.3 and 15.0 us), or groups of more than 32 heads, and round once.
+  // products and exponentials (a mixed step 17.3 and 15.0 us), or groups of more than 32 heads, and round once.  Trees have none of those.
   static constexpr bool PRECISE = MB <= 2;
   const PagedKV kv;
   const int* table;                // the sequence's
@@ -658,7 +658,7 @@ static hipError_t rows_of(const PagedAttnArgs& a, int mb, hipStream_t s) {
   if constexpr (!TREE)             // one token's keys are the same for all of its rows, but for a tree's, whose masks leave out some between
     if (mb == 1 && a.max_new == 1) return rows_grid<T, D, 1, true, false>(a, s);
   if (mb == 1) return rows_grid<T, D, 1, false, TREE>(a, s);
-  if constexpr (!TREE)             // trees come in one tile of up to 32 rows or two of 32, and with more to the many-rows kernel
+  if constexpr (!TREE)             // trees come in tiles of up to 32 rows, any number of them; groups of more than 32 heads go to the many-rows kernel
     if (mb == 4) return rows_grid<T, D, 4, false, false>(a, s);
   return rows_grid<T, D, 2, false, TREE>(a, s);
 }
