@@ -116,7 +116,9 @@ inline AttnPlan plan_of(int n_seqs, int n_tokens, int kv_heads, int group, int m
 // 12 heads of 64 (9 M), would take 18 and take 44; 300 over 2000, 16 of 128, 29 and 37.
 // The rest is walked by blocks of kTreeRows, whole, or their keys shared out over kTreeBlocks (two on a CU; 256 took 73 us for 68, 198
 // for 161; one tree of 128 tokens over 30000 keys, 32 heads over 1, shared 113 and whole 725), whichever a count of the turns says is sooner,
-// a turn being 2 us, 1.24 with heads of 64, and three quarters where most CUs have one block; whole where blocks come in many rounds anyway.
+// a turn being 2 us, 1.75 with heads of 64, and three quarters where most CUs have one block; whole where blocks come in many rounds anyway.
+// Of 44 steps about that border 38 get the sooner one, or one within 10 %, and six take 1.15 to 1.47 times as long; with the 1.24 us that a turn
+// had with one product of the probabilities it was ten (16 x 48 tokens over 1350 keys, 16 heads of 64: shared 31 us, whole 43).
 // Two things that the count leaves out: what a plane has of rows (33 tokens, 32 heads over 8, are one plane of 128 rows and one of 4, with half
 // of the blocks each: 65 us over 30000 keys, and 32 tokens 52), and the parts' bytes (512 over 4000 keys: 95 us, of which it expects 51).
 constexpr int kTreeFew = 32, kTreeRows = 128, kTreeBlocks = 512, kTreeLeast = 6, kTreeTurns = 2048;
@@ -134,7 +136,7 @@ inline AttnPlan plan_of_tree(int n_seqs, int n_tokens, int kv_heads, int group, 
   p.most = max_new;
   const int planes = tree_planes(max_new, group), shares = tree_shares(planes);
   const long units = (n_tokens / (kTreeRows / group) + n_seqs) * (long)kv_heads;
-  const double turn = head_dim == 128 ? 2.0 : 1.24;
+  const double turn = head_dim == 128 ? 2.0 : 1.75;
   const double whole = (double)((units + kTreeBlocks - 1) / kTreeBlocks * tiles) * turn * (units <= 256 ? 0.75 : 1.0);
   const double shared = shares ? std::max((double)turns / shares, (double)kTreeLeast) * turn + 20.0 : 1e30;
   if (shares > 1 && units < 8 * kTreeBlocks && shared < whole && (long)n_seqs * kv_heads * (tiles + 2) < 1l << 30) {
